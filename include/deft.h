@@ -56,6 +56,17 @@ typedef int32_t deft_status;
 #define DEFT_COST_EQ3  0   /* cost_l = size_l * ln(k_l): Eq. 3                                     */
 #define DEFT_COST_SIZE 1   /* cost_l = size_l: the bytes a worker scans (no counterpart in the paper) */
 
+/* Element types of the row operators (embedding, dropout).  The flat gradient vector is fp32 always. */
+#define DEFT_F32  0
+#define DEFT_BF16 1
+#define DEFT_F16  2
+
+/* Parts of the vector deft_layer_norms_part / deft_step_part take. */
+#define DEFT_MAX_PARTS 8
+
+/* Largest table deft_embed_grad accepts (rows; its counters per row live in shared memory). */
+#define DEFT_EMBED_MAX_ROWS 3000000LL
+
 /* Largest layer a plan accepts (a layer's positions are 32-bit).  What one selection launch can
  * scan is smaller on today's devices: see deft_select_launch_max_elems(). */
 #define DEFT_MAX_LAYER_ELEMS 2147483647LL
@@ -257,6 +268,20 @@ DEFT_API deft_status deft_layer_norms(float* resid_acc_d, const float* grad_d, i
                              void* ws_d, size_t ws_bytes, void* stream);
 
 /*
+ * deft_layer_norms for a vector of which some parts hold their gradient already: a row-sparse tensor's
+ * gradient that deft_embed_grad has added to the residual, touched rows only.  In the parts nothing is added and
+ * grad_d is not read (4 bytes per element instead of 12); the norms are those of the whole accumulated vector.
+ *   parts_h[2 * n_parts]  HOST: begin and end of each part (elements; ascending, disjoint, inside [0, n_g];
+ *                         any boundaries, though a tensor's own cost least).  n_parts 0 ..
+ *                         DEFT_MAX_PARTS; with 0 this is deft_layer_norms.
+ * The rest as deft_layer_norms.  Errors: INVALID_ARG, CAPACITY, CUDA.
+ */
+DEFT_API deft_status deft_layer_norms_part(float* resid_acc_d, const float* grad_d, int64_t n_g,
+                                           const int64_t* parts_h, int32_t n_parts,
+                                           const int64_t* layer_start_d, int32_t L, double* norms_d,
+                                           void* ws_d, size_t ws_bytes, void* stream);
+
+/*
  * Layer-wise gradient selection for ONE worker — Algorithm 5, Section 4.4.
  * For each layer l in my_layers_h (ascending ids) selects the k_l entries of largest
  * magnitude.  Magnitudes compare as the IEEE-754 bit pattern with the sign cleared
@@ -435,6 +460,84 @@ DEFT_API deft_status deft_step(float* resid_acc_d, const float* grad_d, int64_t 
                                double* bin_load_h, void* plan_h, size_t plan_bytes_cap, void* plan_d,
                                float* val_d, int64_t* idx_d, int64_t out_cap, void* ws_d, size_t ws_bytes,
                                void* const* events, void* stream);
+
+/* deft_step of a vector whose parts hold their gradient already (parts_h, n_parts as in deft_layer_norms_part). */
+DEFT_API deft_status deft_step_part(float* resid_acc_d, const float* grad_d, int64_t n_g, const int64_t* parts_h,
+                                    int32_t n_parts, const int64_t* layer_start_h,
+                                    const int64_t* layer_start_d, int32_t L, int32_t N, int64_t k, int32_t mode,
+                                    int32_t cost_model, int64_t iteration, int32_t rank, double* norms_d,
+                                    double* norms_h, int64_t* k_l_h, int64_t* sum_k_out, int32_t* bin_of_layer_h,
+                                    double* bin_load_h, void* plan_h, size_t plan_bytes_cap, void* plan_d,
+                                    float* val_d, int64_t* idx_d, int64_t out_cap, void* ws_d, size_t ws_bytes,
+                                    void* const* events, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Row operators: the row-sparse front end of a language model (no counterpart in the paper, whose
+ * language model's embedding gradient they produce).  Matrices are row-major with a pitch (ld, in
+ * elements, >= the row length); pointers need the alignment of their elements only.  Arithmetic is
+ * fp32 whatever the types, with one rounding at the end.
+ *
+ * Dropout.  The mask is a function of (seed, offset, row, column) and is never stored:
+ * Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011) with the counter (column / 8, row, low and
+ * high word of the offset) and the key (low and high word of the seed) gives four words, whose low and
+ * high halves are the 16-bit numbers of the columns 8 c .. 8 c + 7 in order.  An element is kept when
+ * its number is at least t = min(65535, floor(65536 p + 1/2)), and kept elements are multiplied by
+ * 65536 / (65536 - t), so that expectations are exact for the p that is used.  A dropped element is +0
+ * whatever it was (infinities and NaN included).  Calls with different offsets draw independent masks.
+ *   p         0 <= p < 1; p below 2^-17 drops nothing
+ *   offset_d  NULL, or a DEVICE number (8-byte aligned) that is added to offset: a captured graph that
+ *             increments it draws new masks on every replay.  Read only if something is dropped.
+ * ---------------------------------------------------------------------------------------- */
+
+/*
+ * Embedding lookup: out[t, :] = D(scale * table[ids[t], :] + pos[t % pos_rows, :]) for t < n, D = dropout
+ * of row t.  An id outside [0, rows) stands for a row of zeros (the rest of a table that is split by rows).
+ *   table_d  [rows, width], table_type; ids_d int32 or int64 (id_bytes 4 or 8)
+ *   pos_d    NULL, or [pos_rows, width] of table_type: position rows, added before dropout
+ *   out_d    [n, width], out_type; must not overlap the inputs.  n may be 0.
+ * Errors: INVALID_ARG, TOO_LARGE (n, rows or width beyond 2^31 - 1), CUDA.
+ */
+DEFT_API deft_status deft_embed(const void* table_d, int32_t table_type, int64_t rows, int64_t width,
+                                int64_t ld_table, const void* ids_d, int32_t id_bytes, int64_t n, double scale,
+                                const void* pos_d, int64_t pos_rows, int64_t ld_pos, double p, uint64_t seed,
+                                uint64_t offset, const uint64_t* offset_d, void* out_d, int32_t out_type,
+                                int64_t ld_out, void* stream);
+
+/*
+ * Gradient of deft_embed with respect to the table: for every row v
+ *     G[v, :] = scale * (sum over t with ids[t] = v, t ascending, of D'(grad_out[t, :])),
+ * D' = the same mask and gain.  Sums are fp32 in a fixed order (runs of consecutive tokens of a row, then the
+ * runs' sums in order): the same bits on every call.  Tokens whose id is skip_id (padding) or outside
+ * [0, rows) contribute nothing.
+ *   grad_out_d  [n, width], grad_out_type
+ *   grad_d      [rows, width] fp32, contiguous: the table's part of the flat vector.  accumulate = 0: G is
+ *               written, rows without tokens become 0.  accumulate != 0: G is added to the rows that have
+ *               tokens (one fp32 round-to-nearest add per element), the others are neither read nor
+ *               written: the residual itself (see deft_layer_norms_part), or a gradient vector that holds
+ *               a tied output layer's gradient.
+ *   skip_id     a row that gets no gradient; -1: none
+ *   ws_d        deft_embed_workspace_bytes(n, rows, width), 256-byte aligned; holds nothing between
+ *               calls.  Calls that share a workspace must not overlap on the GPU.
+ * The position rows' gradient is the same call with ids[t] = t % pos_rows and scale 1.
+ * Errors: INVALID_ARG, CAPACITY (workspace), TOO_LARGE (n or width beyond 2^31 - 1, rows beyond
+ * DEFT_EMBED_MAX_ROWS), CUDA.
+ */
+DEFT_API size_t deft_embed_workspace_bytes(int64_t n, int64_t rows, int64_t width);
+DEFT_API deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_type, int64_t ld_grad_out,
+                                     const void* ids_d, int32_t id_bytes, int64_t n, int64_t rows, int64_t width,
+                                     int64_t skip_id, double scale, double p, uint64_t seed, uint64_t offset,
+                                     const uint64_t* offset_d, float* grad_d, int32_t accumulate, void* ws_d,
+                                     size_t ws_bytes, void* stream);
+
+/*
+ * Dropout of a [rows, cols] matrix: y = add + D(x).  Its gradient is the same call on the incoming
+ * gradient with add = NULL.  y may be x (same type and pitch) or add, but must not overlap them otherwise.
+ *   add_d  NULL, or [rows, cols] of y_type (a residual stream)
+ * Errors: INVALID_ARG, TOO_LARGE (rows or cols beyond 2^31 - 1), CUDA.
+ */
+DEFT_API deft_status deft_dropout(const void* x_d, int32_t x_type, int64_t ld_x, const void* add_d, int64_t ld_add,
+                                  void* y_d, int32_t y_type, int64_t ld_y, int64_t rows, int64_t cols, double p,
+                                  uint64_t seed, uint64_t offset, const uint64_t* offset_d, void* stream);
 
 /*
  * Comparison sparsifiers of Section 3 (not part of DEFT; they reuse its selection kernel).

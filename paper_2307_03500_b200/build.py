@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_PKG, "libdeft.so")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
+    "--threads", "0",
     "-Xcompiler", "-fPIC,-ffp-contract=off,-fvisibility=hidden", "-shared",
 ]
 

@@ -377,9 +377,34 @@ size_t deft_workspace_bytes(int64_t max_elems, int32_t max_layers) {
     return ws_layout(max_elems, max_layers, max_tiles(max_elems, max_layers)).total;
 }
 
-deft_status deft_layer_norms(float* resid_acc_d, const float* grad_d, int64_t n_g,
-                             const int64_t* layer_start_d, int32_t L, double* norms_d, void* ws_d,
-                             size_t ws_bytes, void* stream) {
+// The parts as the kernel takes them (neighbours merged); false if they are not ascending, disjoint and inside
+// the vector, or too many.
+static bool parts_of(const int64_t* parts_h, int32_t n_parts, int64_t n_g, AddedParts* ap) {
+    if (n_parts < 0 || n_parts > kMaxParts || (n_parts > 0 && !parts_h)) return false;
+    *ap = AddedParts{};
+    int used = 0;
+    int64_t last = 0;
+    for (int32_t i = 0; i < n_parts; ++i) {
+        const int64_t b = parts_h[2 * i], e = parts_h[2 * i + 1];
+        if (b < last || e < b || e > n_g) return false;
+        last = e;
+        if (b == e) continue;
+        if (used && ap->end[used - 1] == b) {
+            ap->end[used - 1] = e;
+        } else {
+            ap->begin[used] = b;
+            ap->end[used] = e;
+            ++used;
+        }
+    }
+    return true;
+}
+
+deft_status deft_layer_norms_part(float* resid_acc_d, const float* grad_d, int64_t n_g, const int64_t* parts_h,
+                                  int32_t n_parts, const int64_t* layer_start_d, int32_t L, double* norms_d, void* ws_d,
+                                  size_t ws_bytes, void* stream) {
+    AddedParts ap;
+    if (n_g < 1 || !parts_of(parts_h, n_parts, n_g, &ap)) return DEFT_ERR_INVALID_ARG;
     if (!resid_acc_d || !layer_start_d || !norms_d || !ws_d || n_g < 1 || L < 1)
         return DEFT_ERR_INVALID_ARG;
     if (!aligned16(resid_acc_d) || (grad_d && !aligned16(grad_d)) || !aligned256(ws_d))
@@ -388,7 +413,13 @@ deft_status deft_layer_norms(float* resid_acc_d, const float* grad_d, int64_t n_
     if (part + norms_ws_bytes(n_g, L) > ws_bytes) return DEFT_ERR_CAPACITY;
     return launch_layer_norms(resid_acc_d, grad_d, n_g, layer_start_d, L, norms_d,
                               reinterpret_cast<double*>(static_cast<char*>(ws_d) + part),
-                              static_cast<cudaStream_t>(stream));
+                              static_cast<cudaStream_t>(stream), nullptr, nullptr, &ap);
+}
+
+deft_status deft_layer_norms(float* resid_acc_d, const float* grad_d, int64_t n_g,
+                             const int64_t* layer_start_d, int32_t L, double* norms_d, void* ws_d,
+                             size_t ws_bytes, void* stream) {
+    return deft_layer_norms_part(resid_acc_d, grad_d, n_g, nullptr, 0, layer_start_d, L, norms_d, ws_d, ws_bytes, stream);
 }
 
 size_t deft_plan_bytes(int32_t L, int32_t N) {
@@ -644,12 +675,14 @@ deft_status deft_select_update_all(float* acc_d, int64_t n_g, const void* plan_h
                                     nullptr, stream);
 }
 
-deft_status deft_step(float* resid_acc_d, const float* grad_d, int64_t n_g, const int64_t* layer_start_h,
-                      const int64_t* layer_start_d, int32_t L, int32_t N, int64_t k, int32_t mode,
-                      int32_t cost_model, int64_t iteration, int32_t rank, double* norms_d, double* norms_h,
-                      int64_t* k_l_h, int64_t* sum_k_out, int32_t* bin_of_layer_h, double* bin_load_h,
-                      void* plan_h, size_t plan_bytes_cap, void* plan_d, float* val_d, int64_t* idx_d,
-                      int64_t out_cap, void* ws_d, size_t ws_bytes, void* const* events, void* stream) {
+deft_status deft_step_part(float* resid_acc_d, const float* grad_d, int64_t n_g, const int64_t* parts_h, int32_t n_parts,
+                           const int64_t* layer_start_h, const int64_t* layer_start_d, int32_t L, int32_t N, int64_t k,
+                           int32_t mode, int32_t cost_model, int64_t iteration, int32_t rank, double* norms_d, double* norms_h,
+                           int64_t* k_l_h, int64_t* sum_k_out, int32_t* bin_of_layer_h, double* bin_load_h,
+                           void* plan_h, size_t plan_bytes_cap, void* plan_d, float* val_d, int64_t* idx_d,
+                           int64_t out_cap, void* ws_d, size_t ws_bytes, void* const* events, void* stream) {
+    AddedParts ap;
+    if (n_g < 1 || !parts_of(parts_h, n_parts, n_g, &ap)) return DEFT_ERR_INVALID_ARG;
     if (!norms_h || rank < -1 || rank >= N) return DEFT_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     auto mark = [&](int i) -> cudaError_t {
@@ -707,7 +740,7 @@ deft_status deft_step(float* resid_acc_d, const float* grad_d, int64_t n_g, cons
     DEFT_CUDA_TRY(mark(0));
     deft_status s = launch_layer_norms(resid_acc_d, grad_d, n_g, layer_start_d, L, norms_d,
                                        reinterpret_cast<double*>(static_cast<char*>(ws_d) + part), st, mapped,
-                                       fused ? &sl : nullptr);
+                                       fused ? &sl : nullptr, &ap);
     if (s != DEFT_OK) return s;
     DEFT_CUDA_TRY(mark(1));
     // the per-layer counters of the selection are cleared while the host plans
@@ -759,6 +792,17 @@ deft_status deft_step(float* resid_acc_d, const float* grad_d, int64_t n_g, cons
     if (s != DEFT_OK) return s;
     DEFT_CUDA_TRY(mark(3));
     return sp;   // DEFT_OK, or the Algorithm 3 warning
+}
+
+deft_status deft_step(float* resid_acc_d, const float* grad_d, int64_t n_g, const int64_t* layer_start_h,
+                      const int64_t* layer_start_d, int32_t L, int32_t N, int64_t k, int32_t mode,
+                      int32_t cost_model, int64_t iteration, int32_t rank, double* norms_d, double* norms_h,
+                      int64_t* k_l_h, int64_t* sum_k_out, int32_t* bin_of_layer_h, double* bin_load_h,
+                      void* plan_h, size_t plan_bytes_cap, void* plan_d, float* val_d, int64_t* idx_d,
+                      int64_t out_cap, void* ws_d, size_t ws_bytes, void* const* events, void* stream) {
+    return deft_step_part(resid_acc_d, grad_d, n_g, nullptr, 0, layer_start_h, layer_start_d, L, N, k, mode, cost_model,
+                          iteration, rank, norms_d, norms_h, k_l_h, sum_k_out, bin_of_layer_h, bin_load_h, plan_h,
+                          plan_bytes_cap, plan_d, val_d, idx_d, out_cap, ws_d, ws_bytes, events, stream);
 }
 
 deft_status deft_select(const float* acc_d, const int64_t* layer_start_h, const int64_t* k_l_h,

@@ -312,10 +312,15 @@ struct StageLaunch {
     uint2* runge;                    // tile table of the all-layers list
     uint2* staging;
 };
+// Parts of the vector that hold their gradient already: ascending, disjoint [begin, end); unused ones are empty.
+constexpr int kMaxParts = DEFT_MAX_PARTS;
+struct AddedParts {
+    int64_t begin[kMaxParts], end[kMaxParts];
+};
 deft_status launch_layer_norms(float* resid_acc_d, const float* grad_d, int64_t n_g,
                                const int64_t* layer_start_d, int32_t L, double* norms_d,
                                double* partial_d, cudaStream_t stream, double* norms_host_mapped = nullptr,
-                               const StageLaunch* stage = nullptr);
+                               const StageLaunch* stage = nullptr, const AddedParts* parts = nullptr);
 deft_status launch_select(const SelParams& p, cudaStream_t stream);
 deft_status launch_select_stream(const SelParams& p, bool has_streamed, bool ring, cudaStream_t stream);
 deft_status launch_residual_update(float* acc_d, const int64_t* idx_d, int64_t count,

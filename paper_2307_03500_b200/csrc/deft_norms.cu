@@ -77,10 +77,22 @@ __device__ __forceinline__ void stage_append(StageShared* ss, int slot, int64_t 
     if (pos < (uint32_t)kStageCap) ss->ent[list][pos] = make_uint2(bits, (uint32_t)(i % kTile));
 }
 
-template <bool kHasGrad, bool kStage>
+// Which part of [lo, hi) lies in the parts: 0 none, 1 all of it (in one part), 2 some.
+__device__ __forceinline__ int in_parts(const AddedParts& ap, int64_t lo, int64_t hi) {
+    int found = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxParts; ++i)
+        if (ap.begin[i] < hi && lo < ap.end[i]) found = ap.begin[i] <= lo && hi <= ap.end[i] ? 1 : 2;
+    return found;
+}
+
+// kParts: the elements of `ap` hold their gradient already (parts ascending and disjoint): g is neither read nor
+// added there, 4 bytes per element instead of 12.  A tile inside one part takes the vector path without the
+// addition; a tile that a part's edge crosses goes element by element.
+template <bool kHasGrad, bool kStage, bool kParts>
 __global__ void __launch_bounds__(kNormThreads, kStage ? 6 : 1)
 k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
-              const int64_t* __restrict__ ls, int L, double* __restrict__ partial, int64_t tiles, const StageArgs sa) {
+              const int64_t* __restrict__ ls, int L, double* __restrict__ partial, int64_t tiles, const StageArgs sa, const AddedParts ap) {
     __shared__ double sh[kNormWarps];
     __shared__ __align__(16) unsigned char ss_raw[kStage ? sizeof(StageShared) : 16];
     StageShared* ss = reinterpret_cast<StageShared*>(ss_raw);
@@ -89,7 +101,8 @@ k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
         const int64_t hi = (lo + kTileA < n) ? lo + kTileA : n;
         int l = layer_of(ls, L, lo);
         const int l_first = l;
-        const bool whole = hi - lo == kTileA && __ldg(ls + l + 1) >= hi;   // the tile lies inside layer l
+        const int part = kParts ? in_parts(ap, lo, hi) : 0;
+        const bool whole = hi - lo == kTileA && __ldg(ls + l + 1) >= hi && part != 2;   // the tile lies inside layer l
         if (kStage) {
             __syncthreads();   // the lists of the previous tile have been written out
             if (threadIdx.x < kStageLists) ss->cnt[threadIdx.x] = 0u;
@@ -128,7 +141,7 @@ k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
             for (int i = 0; i < kTileA / (kNormThreads * 4); i += 2) {
                 const int a = i * kNormThreads + threadIdx.x, b = a + kNormThreads;
                 float4 x = e4[a], y = e4[b];
-                if (kHasGrad) {
+                if (kHasGrad && (!kParts || part == 0)) {
                     const float4 gx = __ldg(g4 + a), gy = __ldg(g4 + b);
                     x.x = __fadd_rn(x.x, gx.x); x.y = __fadd_rn(x.y, gx.y);
                     x.z = __fadd_rn(x.z, gx.z); x.w = __fadd_rn(x.w, gx.w);
@@ -178,7 +191,7 @@ k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
                 }
                 for (int64_t i = ps + threadIdx.x; i < pe; i += kNormThreads) {
                     float x = e[i];
-                    if (kHasGrad) {
+                    if (kHasGrad && (!kParts || in_parts(ap, i, i + 1) == 0)) {
                         x = __fadd_rn(x, __ldg(g + i));
                         e[i] = x;
                     }
@@ -298,7 +311,7 @@ k_norm_finalize(const int64_t* __restrict__ ls, int L, const double* __restrict_
 deft_status launch_layer_norms(float* resid_acc_d, const float* grad_d, int64_t n_g,
                                const int64_t* layer_start_d, int32_t L, double* norms_d,
                                double* partial_d, cudaStream_t stream, double* norms_host_mapped,
-                               const StageLaunch* stage) {
+                               const StageLaunch* stage, const AddedParts* parts) {
     const int64_t tiles = (n_g + kTileA - 1) / kTileA;
     // one CTA per tile: the hardware scheduler keeps the SMs evenly busy to the end, which a
     // resident grid-stride loop did not (0.645 -> 0.600 ms on 333.6 M elements); the loop in the
@@ -313,14 +326,15 @@ deft_status launch_layer_norms(float* resid_acc_d, const float* grad_d, int64_t 
         sa.runge = stage->runge;
         sa.staging = stage->staging;
     }
-    if (grad_d && stage)
-        k_accum_norms<true, true><<<grid, kNormThreads, 0, stream>>>(resid_acc_d, grad_d, n_g, layer_start_d, L, partial_d, tiles, sa);
-    else if (grad_d)
-        k_accum_norms<true, false><<<grid, kNormThreads, 0, stream>>>(resid_acc_d, grad_d, n_g, layer_start_d, L, partial_d, tiles, sa);
-    else if (stage)
-        k_accum_norms<false, true><<<grid, kNormThreads, 0, stream>>>(resid_acc_d, nullptr, n_g, layer_start_d, L, partial_d, tiles, sa);
-    else
-        k_accum_norms<false, false><<<grid, kNormThreads, 0, stream>>>(resid_acc_d, nullptr, n_g, layer_start_d, L, partial_d, tiles, sa);
+    const AddedParts ap = parts ? *parts : AddedParts{};
+    const bool some = parts && parts->end[0] > parts->begin[0];
+    auto run = [&](auto kernel) {
+        kernel<<<grid, kNormThreads, 0, stream>>>(resid_acc_d, grad_d, n_g, layer_start_d, L, partial_d, tiles, sa, ap);
+    };
+    if (grad_d && stage) some ? run(k_accum_norms<true, true, true>) : run(k_accum_norms<true, true, false>);
+    else if (grad_d) some ? run(k_accum_norms<true, false, true>) : run(k_accum_norms<true, false, false>);
+    else if (stage) run(k_accum_norms<false, true, false>);
+    else run(k_accum_norms<false, false, false>);
     DEFT_CUDA_TRY(cudaGetLastError());
     k_norm_finalize<<<L, kNormThreads, 0, stream>>>(layer_start_d, L, partial_d, norms_d, norms_host_mapped);
     DEFT_CUDA_TRY(cudaGetLastError());

@@ -1,0 +1,170 @@
+// Shared device code of the row operators (embedding lookup, its gradient, dropout): element types,
+// eight-column groups of a row, and the counter-based generator of the dropout mask.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "deft_common.cuh"
+
+namespace deft {
+
+constexpr int kGroup = 8;   // columns a thread takes at a time: one call of the generator gives eight 16-bit numbers
+
+// What dropout needs to know.  threshold = t << 16, where an element is kept when its 16-bit number is at
+// least t = round(65536 p); 0 means no dropout.  gain = 65536 / (65536 - t), rounded once to fp32.
+struct DropArgs {
+    uint32_t key0, key1;
+    uint64_t offset;
+    const uint64_t* offset_d;   // added to offset when not NULL (device memory: a replayed graph draws new masks)
+    uint32_t threshold;
+    float gain;
+};
+
+// Philox4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3",
+// SC 2011): counter (c.x, c.y, c.z, c.w), key (k0, k1).
+__device__ __forceinline__ uint4 philox10(uint4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return c;
+}
+
+__device__ __forceinline__ uint64_t drop_offset(const DropArgs& d) {
+    return d.threshold && d.offset_d ? d.offset + *d.offset_d : d.offset;
+}
+
+// Applies the mask of (row, columns 8 * group .. + 7) to v: dropped elements become +0 whatever they were.
+template <bool kScale>
+__device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
+    const uint4 w = philox10(make_uint4(group, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.key0, d.key1);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // the even column goes by a word's low half, the odd one by its high half
+        const float a = kScale ? v[2 * i] * d.gain : v[2 * i], b = kScale ? v[2 * i + 1] * d.gain : v[2 * i + 1];
+        v[2 * i] = (u[i] << 16) >= d.threshold ? a : 0.0f;
+        v[2 * i + 1] = u[i] >= d.threshold ? b : 0.0f;
+    }
+}
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+template <int kBytes> struct Piece;
+template <> struct Piece<16> { using type = uint4; };
+template <> struct Piece<8> { using type = uint2; };
+
+// A group of up to eight consecutive elements.  kAlign: 16 or 8 when every group of the matrix starts on such
+// a boundary (base and row pitch are multiples of it), 0 when only single elements are aligned.
+// count < 8 in the last group of a row: nothing beyond the row is touched.  Plain loads: what is read may be
+// what the same thread writes afterwards (dropout in place, rows added to).
+template <typename T, int kAlign>
+__device__ __forceinline__ void load8(const T* p, int count, float (&v)[kGroup]) {
+    if constexpr (kAlign != 0) {
+        if (count == kGroup) {
+            using P = typename Piece<kAlign>::type;
+            constexpr int per = kAlign / (int)sizeof(T), pieces = kGroup / per;
+            P raw[pieces];
+#pragma unroll
+            for (int i = 0; i < pieces; ++i) raw[i] = reinterpret_cast<const P*>(p)[i];
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) v[i] = to_f32(reinterpret_cast<const T*>(raw)[i]);
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) v[i] = i < count ? to_f32(p[i]) : 0.0f;
+}
+
+template <typename T, int kAlign>
+__device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]) {
+    if constexpr (kAlign != 0) {
+        if (count == kGroup) {
+            using P = typename Piece<kAlign>::type;
+            constexpr int per = kAlign / (int)sizeof(T), pieces = kGroup / per;
+            P raw[pieces];
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) reinterpret_cast<T*>(raw)[i] = from_f32<T>(v[i]);
+#pragma unroll
+            for (int i = 0; i < pieces; ++i) reinterpret_cast<P*>(p)[i] = raw[i];
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+        if (i < count) p[i] = from_f32<T>(v[i]);
+}
+
+// ---- launchers ----
+struct EmbedArgs {
+    const void* table;
+    int64_t rows, ld_table;
+    const void* pos;         // NULL, or [pos_rows, width]: row t % pos_rows is added to token t's row
+    int64_t pos_rows, ld_pos;
+    const void* ids;
+    void* out;
+    int64_t ld_out;
+    int64_t n, width;
+    float scale;
+    DropArgs drop;
+};
+struct DropoutArgs {
+    const void* x;
+    const void* add;         // NULL, or added after dropout (the type of y)
+    void* y;
+    int64_t ld_x, ld_add, ld_y;
+    int64_t rows, cols;
+    DropArgs drop;
+};
+struct EmbedGradArgs {
+    const void* dy;
+    int64_t ld_dy;
+    const void* ids;
+    int64_t n, rows, width;
+    int64_t skip_id;
+    float factor;            // scale x the survivors' gain: applied once to a row's sum
+    DropArgs drop;
+    float* grad;
+    int32_t accumulate;
+    char* ws;
+};
+deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int id_bytes, cudaStream_t stream);
+deft_status launch_dropout(const DropoutArgs& a, int x_type, int y_type, cudaStream_t stream);
+size_t embed_grad_ws_bytes(int64_t n, int64_t rows, int64_t width);
+deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes, cudaStream_t stream);
+
+// Widest boundary every row of a matrix starts on: 16, 8 or 0 (single elements only).
+inline int row_align(const void* p, int64_t ld, size_t elem) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p) | (uintptr_t)((size_t)ld * elem);
+    return (x & 15u) == 0 ? 16 : ((x & 7u) == 0 ? 8 : 0);
+}
+inline size_t type_bytes(int type) { return type == DEFT_F32 ? 4 : 2; }
+
+// Calls f(T{}) with the element type behind a DEFT_* code.
+template <typename F>
+deft_status with_type(int type, F&& f) {
+    switch (type) {
+        case DEFT_F32: return f(float{});
+        case DEFT_BF16: return f(__nv_bfloat16{});
+        default: return f(__half{});
+    }
+}
+template <int kAlign> struct AlignTag { static constexpr int value = kAlign; };
+template <typename F>
+deft_status with_align(int align, F&& f) {
+    switch (align) {
+        case 16: return f(AlignTag<16>{});
+        case 8: return f(AlignTag<8>{});
+        default: return f(AlignTag<0>{});
+    }
+}
+
+}  // namespace deft

@@ -94,6 +94,19 @@ def lib() -> ctypes.CDLL:
         L.deft_step.restype = i32
         L.deft_step.argtypes = [vp, vp, i64, vp, vp, i32, i32, i64, i32, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, sz,
                                 vp, vp, vp, i64, vp, sz, vp, vp]
+        f64, u64 = c.c_double, c.c_uint64
+        L.deft_layer_norms_part.restype = i32
+        L.deft_layer_norms_part.argtypes = [vp, vp, i64, vp, i32, vp, i32, vp, vp, sz, vp]
+        L.deft_step_part.restype = i32
+        L.deft_step_part.argtypes = L.deft_step.argtypes[:3] + [vp, i32] + L.deft_step.argtypes[3:]
+        L.deft_embed.restype = i32
+        L.deft_embed.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, f64, vp, i64, i64, f64, u64, u64, vp, vp, i32, i64, vp]
+        L.deft_embed_workspace_bytes.restype = sz
+        L.deft_embed_workspace_bytes.argtypes = [i64, i64, i64]
+        L.deft_embed_grad.restype = i32
+        L.deft_embed_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, i64, f64, f64, u64, u64, vp, vp, i32, vp, sz, vp]
+        L.deft_dropout.restype = i32
+        L.deft_dropout.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, i64, i64, f64, u64, u64, vp, vp]
         L.deft_workspace_init.restype = i32
         L.deft_workspace_init.argtypes = [vp, sz, i32, vp]
         L.deft_threshold_select.restype = i32
@@ -281,6 +294,26 @@ def deft_layer_norms(resid_acc, grad, layer_start_d, norms_d, ws, stream=None) -
            lib().deft_layer_norms(_dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g,
                                   _dp(layer_start_d, torch.int64), L, _dp(norms_d, torch.float64),
                                   _dp(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _parts(parts) -> np.ndarray:
+    return _np(parts, np.int64).reshape(-1, 2) if len(parts) else np.empty((0, 2), dtype=np.int64)
+
+
+def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, stream=None) -> None:
+    """deft_layer_norms of a vector whose parts [(begin, end), ...] hold their gradient already."""
+    import torch
+    n_g = resid_acc.numel()
+    L = layer_start_d.numel() - 1
+    if grad is not None and grad.numel() != n_g:
+        raise ValueError("grad and resid_acc differ in length")
+    if norms_d.numel() < L:
+        raise ValueError("norms_d too small")
+    pt = _parts(parts)
+    _check("deft_layer_norms_part",
+           lib().deft_layer_norms_part(_dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g, _hp(pt), len(pt),
+                                       _dp(layer_start_d, torch.int64), L, _dp(norms_d, torch.float64),
+                                       _dp(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def deft_layer_norms_static(resid_acc, grad, layer_start_d, norms_d, stream=None) -> None:
@@ -583,3 +616,143 @@ def deft_topk_baseline(acc, k: int, val_d, idx_d, ws, stream=None) -> None:
            lib().deft_topk_baseline(_dp(acc, torch.float32), acc.numel(), int(k), _dp(val_d, torch.float32),
                                     _dp(idx_d, torch.int64), _dp(ws), ws.numel() * ws.element_size(),
                                     _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------
+# row operators: embedding lookup, its gradient, dropout
+# ------------------------------------------------------------------------------------------
+F32, BF16, F16 = 0, 1, 2
+MAX_PARTS = 8
+EMBED_MAX_ROWS = 3000000
+_TYPES = None
+
+
+def _type(t) -> int:
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError("expected float32, bfloat16 or float16, got %s" % t.dtype)
+    return code
+
+
+def _matrix(t, name: str) -> Tuple[int, int, int]:
+    """(rows, columns, pitch) of a tensor whose last dimension is the row and whose others are one list of rows."""
+    if t.dim() == 0:
+        raise ValueError("%s: at least one dimension expected" % name)
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, cols
+    lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+    if any(s0 != n1 * s1 for (_, s0), (n1, s1) in zip(lead, lead[1:])) or (cols > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: the rows must be contiguous and evenly spaced" % name)
+    pitch = lead[-1][1] if lead else cols
+    if pitch < cols:
+        raise ValueError("%s: the rows overlap" % name)
+    return t.numel() // cols, cols, pitch
+
+
+class _OnDevice:
+    """Makes `device` current for a call whose tensors are not on the current one; checks that they share a device."""
+
+    def __init__(self, *tensors):
+        import torch
+        self.index = tensors[0].device.index
+        for t in tensors:
+            if t is not None and (not t.is_cuda or t.device.index != self.index):
+                raise ValueError("expected CUDA tensors on one device")
+        self.guard = None if torch.cuda.current_device() == self.index else torch.cuda.device(self.index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _ids(ids) -> int:
+    import torch
+    if not ids.is_contiguous() or ids.dtype not in (torch.int64, torch.int32):
+        raise ValueError("ids: a contiguous int64 or int32 tensor")
+    return ids.element_size()
+
+
+def _offset(offset_d) -> Optional[int]:
+    if offset_d is None:
+        return None
+    if offset_d.numel() != 1 or offset_d.element_size() != 8 or offset_d.is_floating_point():
+        raise ValueError("offset_d: one 64-bit integer")
+    return offset_d.data_ptr()
+
+
+_U64 = (1 << 64) - 1
+
+
+def deft_embed(table, ids, out, scale: float = 1.0, pos=None, p: float = 0.0, seed: int = 0, offset: int = 0,
+               offset_d=None, stream=None) -> None:
+    """out[t] = D(scale * table[ids[t]] + pos[t % len(pos)]), D = dropout (see deft_dropout)."""
+    n, width, ld_out = _matrix(out, "out")
+    if table.dim() != 2 or table.shape[1] != width or ids.numel() != n:
+        raise ValueError("table, ids and out disagree")
+    rows, _, ld_table = _matrix(table, "table")
+    pos_rows = ld_pos = 0
+    if pos is not None:
+        pos_rows, w, ld_pos = _matrix(pos, "pos")
+        if w != width or pos.dtype != table.dtype:
+            raise ValueError("pos: rows like the table's expected")
+    with _OnDevice(out, table, ids, pos, offset_d):
+        _check("deft_embed",
+               lib().deft_embed(table.data_ptr(), _type(table), rows, width, ld_table, ids.data_ptr(), _ids(ids), n, scale,
+                                None if pos is None else pos.data_ptr(), pos_rows, ld_pos, p, seed & _U64, offset & _U64,
+                                _offset(offset_d), out.data_ptr(), _type(out), ld_out, _stream(stream)))
+
+
+def deft_embed_workspace_bytes(n: int, rows: int, width: int) -> int:
+    return int(lib().deft_embed_workspace_bytes(int(n), int(rows), int(width)))
+
+
+def alloc_embed_workspace(n: int, rows: int, width: int, device="cuda"):
+    """A torch uint8 tensor for deft_embed_grad calls of up to n tokens on a table of [rows, width]."""
+    import torch
+    size = deft_embed_workspace_bytes(n, rows, width)
+    if size == 0:
+        raise DeftError("deft_embed_workspace_bytes", ERR_INVALID_ARG)
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def deft_embed_grad(grad_out, ids, grad, ws, accumulate: bool = False, skip_id: int = -1, scale: float = 1.0, p: float = 0.0,
+                    seed: int = 0, offset: int = 0, offset_d=None, stream=None) -> None:
+    """deft_embed's gradient with respect to the table, written to (or, with accumulate, added to the touched
+    rows of) grad, a contiguous fp32 [rows, width] tensor: usually a view of the flat gradient vector or of the residual."""
+    import torch
+    if grad.dim() != 2 or not grad.is_contiguous() or grad.dtype != torch.float32:
+        raise ValueError("grad: a contiguous float32 [rows, width] tensor")
+    rows, width = grad.shape
+    n, w, ld = _matrix(grad_out, "grad_out")
+    if ids.numel() == 0 and grad_out.numel() == 0:
+        n, w, ld = 0, width, width
+    if w != width or ids.numel() != n:
+        raise ValueError("grad_out, ids and grad disagree")
+    with _OnDevice(grad, grad_out, ids, ws, offset_d):
+        _check("deft_embed_grad",
+               lib().deft_embed_grad(grad_out.data_ptr(), _type(grad_out), ld, ids.data_ptr(), _ids(ids), n, rows, width, skip_id,
+                                     scale, p, seed & _U64, offset & _U64, _offset(offset_d), grad.data_ptr(), 1 if accumulate else 0,
+                                     ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0, offset_d=None, stream=None) -> None:
+    """y = add + D(x) row by row (the last dimension is the row): kept elements times 1 / (1 - p), the mask a function
+    of (seed, offset, row, column) alone.  The gradient is the same call on the incoming gradient without add."""
+    rows, cols, ld_x = _matrix(x, "x")
+    if y.shape != x.shape or (add is not None and (add.shape != x.shape or add.dtype != y.dtype)):
+        raise ValueError("x, y and add disagree")
+    ld_y = _matrix(y, "y")[2]
+    ld_add = 0 if add is None else _matrix(add, "add")[2]
+    with _OnDevice(y, x, add, offset_d):
+        _check("deft_dropout",
+               lib().deft_dropout(x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(),
+                                  _type(y), ld_y, rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d), _stream(stream)))

@@ -66,8 +66,8 @@ class LibdeftOps:
     def new_residual(self) -> torch.Tensor:
         return torch.zeros(self.n_g, dtype=torch.float32, device=self.device)
 
-    def layer_norms(self, e, g) -> np.ndarray:
-        return self.ds.layer_norms(e, g).copy()
+    def layer_norms(self, e, g, rows=()) -> np.ndarray:
+        return self.ds.layer_norms(e, g, rows).copy()
 
     def select(self, e, k_l: np.ndarray, my_layers: np.ndarray):
         n = int(k_l[my_layers].sum()) if my_layers.size else 0
@@ -152,10 +152,11 @@ class DistributedWorker:
         dist.all_reduce(t, op=dist.ReduceOp.SUM, group=self.group)
         return [int(x) for x in t.cpu().tolist()]
 
-    def step(self, grad) -> StepReport:
-        """grad: this worker's gradient (already scaled by the learning rate), on the worker's device."""
+    def step(self, grad, rows=()) -> StepReport:
+        """grad: this worker's gradient (already scaled by the learning rate), on the worker's device.
+        rows: `pipeline.RowGradient`s of this worker's embedding tables; grad is not read in their parts."""
         ops, N, t = self.ops, self.N, self.iteration
-        norms = ops.layer_norms(self.e, grad)                                  # line 5 (+ the norms of Section 4.2)
+        norms = ops.layer_norms(self.e, grad, rows) if rows else ops.layer_norms(self.e, grad)   # line 5 (+ the norms of Section 4.2)
         if self.kind == "deft":
             k_l, bins = self._shared_plan(norms)
             my = deft.deft_bin_layers(bins, deft.deft_rank_bin(t, self.rank, N))

@@ -8,9 +8,10 @@ per-rank part once for every rank.  Every numeric step runs inside libdeft.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 from dataclasses import dataclass
-from typing import List, Optional
+from typing import List, Optional, Sequence
 
 import numpy as np
 import torch
@@ -31,6 +32,22 @@ class StepPlan:
     plan_h: np.ndarray         # the uploaded plan blob (host copy)
 
 
+@dataclass
+class RowGradient:
+    """The gradient of an embedding table by rows: what reaches the table from `deft_embed`'s output.
+    A step that is given it adds it to the touched rows of the residual (`deft_embed_grad`) and does not read the
+    flat gradient vector in that tensor's part: the dense gradient of the table need not exist."""
+    tensor: int                     # position of the table in the step's tensor list
+    ids: torch.Tensor               # int64 / int32 token ids of the lookup
+    grad_out: torch.Tensor          # [len(ids), width]: the gradient of the lookup's output
+    scale: float = 1.0              # the lookup's scale (times the learning rate, like the flat gradient)
+    skip_id: int = -1
+    p: float = 0.0                  # the lookup's dropout
+    seed: int = 0
+    offset: int = 0
+    offset_d: Optional[torch.Tensor] = None
+
+
 class DeftStep:
     def __init__(self, tensor_sizes, n_workers: int, density: float, device="cuda:0",
                  mode: int = deft.MODE_EXACT, k: Optional[int] = None, cost_model: int = deft.COST_EQ3):
@@ -38,6 +55,7 @@ class DeftStep:
         self.N = int(n_workers)
         self.mode = mode
         self.cost_model = cost_model
+        self.tensor_start = np.concatenate([[0], np.cumsum(np.asarray(tensor_sizes, dtype=np.int64))])
         self.layer_start, self.layer_tensor = deft.deft_split_layers(tensor_sizes, n_workers)
         self.layer_size = np.diff(self.layer_start)
         self.L = int(self.layer_size.size)
@@ -57,10 +75,48 @@ class DeftStep:
         self._plan_pin = torch.empty(nbytes, dtype=torch.uint8).pin_memory()
         self.plan_h = self._plan_pin.numpy()
         self.plan_d = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self._ws_rows: Optional[torch.Tensor] = None   # workspace of the row-sparse gradients, grown when needed
+
+    # -- before step 1: row-sparse gradients straight into the residual (device) --------------
+    def add_rows(self, resid: torch.Tensor, rows: Sequence[RowGradient], stream=None) -> np.ndarray:
+        """Adds every RowGradient to its table's part of `resid`, in order; returns the parts that now hold their
+        gradient as int64 [parts, 2] (ascending)."""
+        if not rows:
+            return np.empty((0, 2), dtype=np.int64)
+        todo, parts, need = [], set(), 0
+        if resid.dim() != 1 or resid.numel() != self.n_g:
+            raise ValueError("resid: a flat tensor of n_g elements")
+        for r in rows:                      # everything is checked before anything is added
+            if not 0 <= r.tensor < len(self.tensor_start) - 1:
+                raise ValueError("no tensor %d" % r.tensor)
+            a, b = int(self.tensor_start[r.tensor]), int(self.tensor_start[r.tensor + 1])
+            width = int(r.grad_out.shape[-1])
+            if width < 1 or (b - a) % width:
+                raise ValueError("tensor %d has no rows of %d elements" % (r.tensor, width))
+            size = deft.deft_embed_workspace_bytes(r.ids.numel(), (b - a) // width, width)
+            if size == 0:
+                raise deft.DeftError("deft_embed_workspace_bytes", deft.ERR_INVALID_ARG)
+            need = max(need, size)
+            parts.add((a, b))
+            todo.append((r, a, b, width))
+        if len(parts) > deft.MAX_PARTS:
+            raise ValueError("at most %d tensors may have their gradient by rows" % deft.MAX_PARTS)
+        if need and (self._ws_rows is None or self._ws_rows.numel() < need):
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                self._ws_rows = torch.empty(need, dtype=torch.uint8, device=self.device)
+        for r, a, b, width in todo:
+            deft.deft_embed_grad(r.grad_out, r.ids, resid[a:b].view(-1, width), self._ws_rows, accumulate=True,
+                                 skip_id=r.skip_id, scale=r.scale, p=r.p, seed=r.seed, offset=r.offset,
+                                 offset_d=r.offset_d, stream=stream)
+        return np.array(sorted(parts), dtype=np.int64).reshape(-1, 2)
 
     # -- step 1: accumulate + norms (device) ------------------------------------------------
-    def layer_norms(self, resid: torch.Tensor, grad: Optional[torch.Tensor]) -> np.ndarray:
-        deft.deft_layer_norms(resid, grad, self.layer_start_d, self.norms_d, self.ws)
+    def layer_norms(self, resid: torch.Tensor, grad: Optional[torch.Tensor], rows: Sequence[RowGradient] = ()) -> np.ndarray:
+        """acc = resid + grad in place, norms per layer.  `rows`: tensors whose gradient comes by rows; `grad` is not
+        read in their parts."""
+        if grad is not None and grad.numel() != self.n_g:
+            raise ValueError("grad: a tensor of n_g elements")
+        deft.deft_layer_norms_part(resid, grad, self.add_rows(resid, rows), self.layer_start_d, self.norms_d, self.ws)
         self.norms_h.copy_(self.norms_d, non_blocking=True)
         torch.cuda.current_stream().synchronize()
         return self.norms_h.numpy()
@@ -102,9 +158,10 @@ class DeftStep:
 
     # -- the whole step in ONE library call ---------------------------------------------------
     def step_fused(self, resid: torch.Tensor, grad: Optional[torch.Tensor], iteration: int = 0, rank: int = -1,
-                   events=None, stream=None) -> StepPlan:
+                   events=None, stream=None, rows: Sequence[RowGradient] = ()) -> StepPlan:
         """accumulate + norms -> host planning -> selection + residual update, one C call
-        (`deft_step`): all simulated workers in one launch (rank = -1) or one worker.
+        (`deft_step`): all simulated workers in one launch (rank = -1) or one worker.  `rows`: tensors whose
+        gradient comes by rows (added first, see `add_rows`); `grad` is not read in their parts.
         The pointers of the buffers this object owns are marshalled once and reused: the call is made
         every step and the device waits for the host between its two kernels."""
         import ctypes
@@ -141,13 +198,15 @@ class DeftStep:
                 flat.append(e.cuda_event)
             ev = (ctypes.c_void_p * 4)(*flat)
         st = torch.cuda.current_stream(self.device) if stream is None else stream
-        status = deft.lib().deft_step(
+        parts = self.add_rows(resid, rows, st) if rows else None
+        status = deft.lib().deft_step_part(
             ctypes.c_void_p(resid.data_ptr()), None if grad is None else ctypes.c_void_p(grad.data_ptr()), self.n_g,
+            None if parts is None else ctypes.c_void_p(parts.ctypes.data), 0 if parts is None else len(parts),
             f["ls_h"], f["ls_d"], self.L, self.N, int(self.k), int(self.mode), int(self.cost_model), int(iteration),
             int(rank), f["norms_d"], f["norms_h"], f["k_l"], f["sum_k"], f["bins"], f["load"], f["plan_h"],
             f["plan_cap"], f["plan_d"], f["val_d"], f["idx_d"], f["out_cap"], f["ws"], f["ws_bytes"], ev,
             ctypes.c_void_p(st.cuda_stream))
-        deft._check("deft_step", status, allow_warn=True)
+        deft._check("deft_step_part", status, allow_warn=True)
         n_layers, elems, rank_k, out_off = deft.deft_plan_rank_table(self.plan_h, self.N)
         off = np.empty(self.N + 1, dtype=np.int64)
         off[:-1] = out_off
@@ -157,10 +216,10 @@ class DeftStep:
 
     # -- the whole step for all simulated ranks ---------------------------------------------
     def step(self, resid: torch.Tensor, grad: Optional[torch.Tensor], iteration: int = 0, events=None,
-             per_rank: bool = False):
+             per_rank: bool = False, rows: Sequence[RowGradient] = ()):
         """accumulate + norms -> plan -> (selection, residual update) for every rank.  Returns the plan and,
         per rank, views of its selected (values, indices)."""
-        norms = self.layer_norms(resid, grad)
+        norms = self.layer_norms(resid, grad, rows)
         plan = self.plan(norms, iteration)
         self.select_and_update_all(resid, plan, events, per_rank)
         off = plan.rank_out_off

@@ -75,13 +75,14 @@ class MultiWorkerSim:
         return self.union[:int(self.count_d.item())]
 
     # -- Algorithm 1, lines 5-12, for all workers ---------------------------------------------
-    def step(self, grads: List[torch.Tensor]):
-        """grads[r]: worker r's gradient (already scaled by the learning rate).  Returns
+    def step(self, grads: List[torch.Tensor], rows=None):
+        """grads[r]: worker r's gradient (already scaled by the learning rate).  rows[r], when given: worker r's
+        `pipeline.RowGradient`s; its gradient is not read in their parts.  Returns
         (actual density, error after the update)."""
         ds, N, t = self.ds, self.N, self.iteration
         norms_all = []
         for r in range(N):                                         # line 5: acc_r = e_r + g_r (in place)
-            norms_all.append(ds.layer_norms(self.e[r], grads[r]).copy())
+            norms_all.append(ds.layer_norms(self.e[r], grads[r], rows[r] if rows else ()).copy())
         if self.kind == "deft":
             plan = ds.plan(norms_all[self.delegate], t)            # Algorithms 3 + 4 on the delegate, shared
             for r in range(N):                                     # line 6: worker r, its layers, its vector
