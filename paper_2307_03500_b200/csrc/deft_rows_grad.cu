@@ -2,8 +2,8 @@
 //
 // 1. k_group_tokens puts the token positions in order of their table rows (positions of one row ascending) and
 //    writes, per table row, where its positions start and how many there are.
-// 2. k_rows_sum adds up each row's tokens in fp32, in that order: the result does not depend on how the work
-//    was scheduled.
+// 2. k_rows_reduce adds up each row's tokens in fp32, in an order that does not depend on how the work was
+//    scheduled.
 #include "deft_rows.cuh"
 
 namespace deft {
@@ -23,6 +23,8 @@ struct GroupOut {
     uint2* sorted;      // [n] (table row, token position)
     uint2* row_tab;     // [rows] (first place in sorted, tokens)
     uint32_t* total;    // tokens in sorted: those whose id is a row of the table and not the one left out
+    uint32_t* arrived;  // the second kernel's counters, cleared here
+    size_t arrived_n;
 };
 
 inline size_t group_smem(int warps, int64_t per_cta) {
@@ -39,7 +41,9 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
     uint32_t* cnt = reinterpret_cast<uint32_t*>(smem + sizeof(uint2) * kListCap * warps);   // [warps][per_cta]
     uint32_t* start = cnt + (size_t)warps * per_cta;                                        // [per_cta]
     uint32_t* red = start + per_cta;                                                        // [2][32]
+    asm volatile("griddepcontrol.launch_dependents;");
     for (int i = threadIdx.x; i < warps * per_cta; i += blockDim.x) cnt[i] = 0u;
+    for (size_t i = (size_t)me * blockDim.x + threadIdx.x; i < out.arrived_n; i += (size_t)kOwners * blockDim.x) out.arrived[i] = 0u;
     __syncthreads();
     uint32_t* mine = cnt + (size_t)warp * per_cta;
     const uint32_t part = (n + warps - 1) / warps;
@@ -132,50 +136,200 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 }
 
 // ---- 2. the sums ----
-// One warp per table row and 256 columns.
-template <typename T, int kAlign>
-__global__ void __launch_bounds__(256) k_rows_sum(const EmbedGradArgs a, const uint2* __restrict__ sorted, const uint2* __restrict__ row_tab, int slices) {
-    const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t row = task / slices;
-    if (row >= a.rows) return;
-    const uint32_t group = (uint32_t)(task - row * slices) * 32 + lane;
-    const int64_t col = (int64_t)group * kGroup;
-    const uint2 tab = row_tab[row];
-    if (col >= a.width || (a.accumulate && tab.y == 0)) return;
-    const int count = a.width - col < kGroup ? (int)(a.width - col) : kGroup;
-    const uint64_t offset = drop_offset(a.drop);
-    float sum[kGroup] = {};
-    for (uint32_t i = 0; i < tab.y; ++i) {
-        const uint32_t pos = sorted[tab.x + i].y;
-        float v[kGroup];
-        load8<T, kAlign>(static_cast<const T*>(a.dy) + (int64_t)pos * a.ld_dy + col, count, v);
-        if (a.drop.threshold) drop8<false>(v, a.drop, offset, pos, group);
+// The grouped tokens are cut into units of kUnit consecutive ones, whatever rows they belong to: every unit is the
+// same work, and all its loads are known from the start (a warp per row would wait for one token's load after the
+// other, and a frequent token's row would keep one warp busy for the whole launch).  A warp takes one unit and 256
+// columns, eight per lane.  Runs of one row that lie inside a unit are finished there.  A run that crosses units
+// leaves a partial sum per unit; the warp that arrives last at the run's counter adds them in order (in two levels of
+// kJoin when there are more), so the bits do not depend on the order of arrival.
+constexpr int kReduceThreads = 256;
+constexpr int kJoin = 32;        // units whose partial sums one warp adds up
+constexpr int kDeep = 4;         // tokens whose loads a warp has in flight
+constexpr int kZeroRows = 8;     // rows a warp clears if they have no tokens
+
+struct ReduceArgs {
+    const uint2* sorted;
+    const uint2* row_tab;
+    const uint32_t* total;
+    float* partial;              // [2 * units][slices * 256]: a unit's first run (even) and last run (odd)
+    uint32_t* arrived;           // [2][2 * units * slices]: units of a group, groups of a run
+    int unit, units, slices;
+};
+
+__device__ __forceinline__ float4 load_cg(const float* p) { return __ldcg(reinterpret_cast<const float4*>(p)); }
+
+// Adds one row's 8 columns to the gradient (or writes them).
+template <int kGradAlign>
+__device__ __forceinline__ void emit8(float* dst, int count, const float (&sum)[kGroup], const float (&old)[kGroup], float factor, bool accumulate) {
+    float g[kGroup];
 #pragma unroll
-        for (int c = 0; c < kGroup; ++c) sum[c] += v[c];
+    for (int c = 0; c < kGroup; ++c) {
+        g[c] = __fmul_rn(sum[c], factor);
+        if (accumulate) g[c] = __fadd_rn(old[c], g[c]);
     }
-    float* dst = a.grad + row * a.width + col;
-#pragma unroll
-    for (int c = 0; c < kGroup; ++c)
-        if (c < count) {
-            const float g = tab.y ? __fmul_rn(sum[c], a.factor) : 0.0f;   // (+0 also where the factor is negative)
-            dst[c] = a.accumulate ? __fadd_rn(dst[c], g) : g;
-        }
+    store8<float, kGradAlign>(dst, count, g);
 }
 
-struct GradWs { size_t total, row_tab, sorted, bytes; };
-inline GradWs grad_ws(int64_t n, int64_t rows) {
+template <typename T, int kAlign, int kGradAlign>
+__global__ void __launch_bounds__(kReduceThreads) k_rows_reduce(const EmbedGradArgs a, const ReduceArgs r) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * (kReduceThreads / 32) + (threadIdx.x >> 5);
+    const int64_t reduce_tasks = (int64_t)r.units * r.slices;
+    if (task >= reduce_tasks) {
+        // rows without tokens, where the gradient is written
+        if (a.accumulate) return;
+        const int64_t row0 = (task - reduce_tasks) * kZeroRows;
+        const bool empty = lane < kZeroRows && row0 + lane < a.rows && r.row_tab[row0 + lane].y == 0;
+        for (uint32_t m = __ballot_sync(0xffffffffu, empty); m; m &= m - 1) {
+            float* dst = a.grad + (row0 + __ffs((int)m) - 1) * a.width;
+            const float zero[kGroup] = {};
+            for (int64_t col = lane * kGroup; col < a.width; col += 32 * kGroup)
+                store8<float, kGradAlign>(dst + col, a.width - col < kGroup ? (int)(a.width - col) : kGroup, zero);
+        }
+        return;
+    }
+    const int unit_id = (int)(task / r.slices), slice = (int)(task - (int64_t)unit_id * r.slices);
+    const uint32_t total = *r.total, first = (uint32_t)unit_id * (uint32_t)r.unit;
+    if (first >= total) return;
+    const int have = (int)min(total - first, (uint32_t)r.unit);
+    const uint2 item = lane < have ? r.sorted[first + lane] : make_uint2(0xffffffffu, 0u);
+    const uint32_t before = first > 0 ? r.sorted[first - 1].x : 0xffffffffu;
+    const uint32_t after = first + have < total ? r.sorted[first + have].x : 0xffffffffu;
+    const uint32_t next_row = __shfl_down_sync(0xffffffffu, item.x, 1);
+    const uint32_t ends = __ballot_sync(0xffffffffu, lane < have && (lane == have - 1 || next_row != item.x));
+    const bool open_front = before == __shfl_sync(0xffffffffu, item.x, 0);
+    const bool open_back = after == __shfl_sync(0xffffffffu, item.x, have - 1);
+    const int first_end = __ffs((int)ends) - 1;
+
+    const uint32_t group = (uint32_t)slice * 32 + lane;
+    const int64_t col = (int64_t)group * kGroup;
+    const int count = col >= a.width ? 0 : (a.width - col < kGroup ? (int)(a.width - col) : kGroup);
+    const uint64_t offset = drop_offset(a.drop);
+    const T* dy = static_cast<const T*>(a.dy) + col;
+    const size_t pitch = (size_t)r.slices * 256;
+    float sum[kGroup] = {};
+    for (int i0 = 0; i0 < have; i0 += kDeep) {
+        float v[kDeep][kGroup], old[kDeep][kGroup];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int i = i0 + k;
+            const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i & 31), row = __shfl_sync(0xffffffffu, item.x, i & 31);
+            if (i < have && count) {
+                load8<T, kAlign>(dy + (int64_t)pos * a.ld_dy, count, v[k]);
+                const bool closed = !(i == first_end && open_front) && !(i == have - 1 && open_back);
+                if (a.accumulate && (ends >> i & 1u) && closed) load8<float, kGradAlign>(a.grad + (int64_t)row * a.width + col, count, old[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int i = i0 + k;
+            if (i >= have) break;
+            const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i), row = __shfl_sync(0xffffffffu, item.x, i);
+            if (count) {
+                if (a.drop.threshold) drop8<false>(v[k], a.drop, offset, pos, group);
+#pragma unroll
+                for (int c = 0; c < kGroup; ++c) sum[c] += v[k][c];
+            }
+            if (!(ends >> i & 1u)) continue;
+            const bool front = i == first_end && open_front, back = i == have - 1 && open_back;
+            float* dst = a.grad + (int64_t)row * a.width + col;
+            if (!front && !back) {
+                if (count) emit8<kGradAlign>(dst, count, sum, old[k], a.factor, a.accumulate);
+            } else {
+                // the run's units are s .. t; this unit's partial sum goes to its odd place where the run starts here
+                const uint2 tab = r.row_tab[row];
+                const int s = (int)(tab.x / (uint32_t)r.unit), t = (int)((tab.x + tab.y - 1) / (uint32_t)r.unit);
+                auto place = [&](int u) { return (size_t)(2 * u + (u == s ? 1 : 0)); };
+                float* mine = r.partial + place(unit_id) * pitch + col;
+                *reinterpret_cast<float4*>(mine) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                *reinterpret_cast<float4*>(mine + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+                // true for the last of `expected` warps to arrive at a place
+                auto last_at = [&](size_t at, int level, int expected) {
+                    __threadfence();
+                    __syncwarp();
+                    uint32_t n = 0;
+                    if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + at) * r.slices + slice, 1u);
+                    n = __shfl_sync(0xffffffffu, n, 0);
+                    __threadfence();
+                    return n == (uint32_t)(expected - 1);
+                };
+                // the partial sums of the units u, u + step, ... below end, in order
+                auto add_up = [&](int u, int step, int end) {
+                    float total8[kGroup] = {};
+#pragma unroll 4
+                    for (; u < end; u = (u / step + 1) * step) {
+                        const float* p = r.partial + place(u) * pitch + col;
+                        const float4 x = load_cg(p), y = load_cg(p + 4);
+                        total8[0] += x.x; total8[1] += x.y; total8[2] += x.z; total8[3] += x.w;
+                        total8[4] += y.x; total8[5] += y.y; total8[6] += y.z; total8[7] += y.w;
+                    }
+#pragma unroll
+                    for (int c = 0; c < kGroup; ++c) sum[c] = total8[c];
+                };
+                const int u0 = max(s, unit_id / kJoin * kJoin), u1 = min(t + 1, (unit_id / kJoin + 1) * kJoin);
+                const int groups = t / kJoin - s / kJoin + 1;
+                bool done = false;
+                if (last_at(place(u0), 0, u1 - u0)) {
+                    add_up(u0, 1, u1);
+                    done = groups == 1;
+                    if (!done) {
+                        float* joined = r.partial + place(u0) * pitch + col;
+                        *reinterpret_cast<float4*>(joined) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                        *reinterpret_cast<float4*>(joined + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+                        if (last_at(place(s), 1, groups)) {
+                            add_up(s, kJoin, t + 1);
+                            done = true;
+                        }
+                    }
+                }
+                if (done && count) {
+                    float was[kGroup];
+                    if (a.accumulate) load8<float, kGradAlign>(dst, count, was);
+                    emit8<kGradAlign>(dst, count, sum, was, a.factor, a.accumulate);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kGroup; ++c) sum[c] = 0.0f;
+        }
+    }
+}
+
+// Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls.
+constexpr int64_t kMinTasks = 4096;
+inline int unit_of(int64_t n, int64_t slices) {
+    int unit = 32;
+    while (unit > 4 && (n + unit - 1) / unit * slices < kMinTasks) unit >>= 1;
+    return unit;
+}
+// Upper bound of units * slices over all calls of up to n tokens and up to `slices` slices (unit_of() gives fewer
+// tokens more units): what the workspace is sized by, so that it serves smaller calls too.
+inline size_t most_tasks(int64_t n, int64_t slices) {
+    const int64_t few = (n + 3) / 4 * slices, many = (n + 31) / 32 * slices;
+    const int64_t small = few < 2 * kMinTasks + slices ? few : 2 * kMinTasks + slices;
+    return (size_t)(small > many ? small : many);
+}
+
+struct GradWs { size_t total, row_tab, sorted, arrived, arrived_n, partial, bytes; int unit, units, slices; };
+inline GradWs grad_ws(int64_t n, int64_t rows, int64_t width) {
     GradWs w{};
+    w.slices = (int)((width + 255) / 256);
+    w.unit = unit_of(n, w.slices);
+    w.units = (int)((n + w.unit - 1) / w.unit);
+    w.arrived_n = 4 * (size_t)w.units * (size_t)w.slices;
     w.total = 0;
     w.row_tab = 256;
     w.sorted = w.row_tab + align_up(sizeof(uint2) * (size_t)rows, 256);
-    w.bytes = w.sorted + align_up(sizeof(uint2) * (size_t)n, 256);
+    w.arrived = w.sorted + align_up(sizeof(uint2) * (size_t)n, 256);
+    w.partial = w.arrived + align_up(sizeof(uint32_t) * w.arrived_n, 256);
+    const size_t most = most_tasks(n, w.slices);
+    w.bytes = w.arrived + align_up(sizeof(uint32_t) * 4 * most, 256) + sizeof(float) * 2 * most * 256;
     return w;
 }
 
 }  // namespace
 
-size_t embed_grad_ws_bytes(int64_t n, int64_t rows, int64_t width) { return grad_ws(n, rows).bytes; }
+size_t embed_grad_ws_bytes(int64_t n, int64_t rows, int64_t width) { return grad_ws(n, rows, width).bytes; }
 
 deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes, cudaStream_t stream) {
     const int per_cta = (int)((a.rows + kOwners - 1) / kOwners);
@@ -183,8 +337,12 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     while (warps > 1 && group_smem(warps, per_cta) > kGroupSmem) warps >>= 1;
     const size_t smem = group_smem(warps, per_cta);
     if (smem > kGroupSmem) return DEFT_ERR_TOO_LARGE;
-    const GradWs w = grad_ws(a.n, a.rows);
-    GroupOut out{reinterpret_cast<uint2*>(a.ws + w.sorted), reinterpret_cast<uint2*>(a.ws + w.row_tab), reinterpret_cast<uint32_t*>(a.ws + w.total)};
+    const GradWs w = grad_ws(a.n, a.rows, a.width);
+    const int64_t tasks = (int64_t)w.units * w.slices + (a.accumulate ? 0 : (a.rows + kZeroRows - 1) / kZeroRows);
+    const int64_t blocks = (tasks + kReduceThreads / 32 - 1) / (kReduceThreads / 32);
+    if (blocks > 0x7fffffff) return DEFT_ERR_TOO_LARGE;
+    GroupOut out{reinterpret_cast<uint2*>(a.ws + w.sorted), reinterpret_cast<uint2*>(a.ws + w.row_tab), reinterpret_cast<uint32_t*>(a.ws + w.total),
+                 reinterpret_cast<uint32_t*>(a.ws + w.arrived), w.arrived_n};
     auto group = [&](auto id) -> deft_status {
         using Id = decltype(id);
         DEFT_CUDA_TRY(cudaFuncSetAttribute(k_group_tokens<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGroupSmem));
@@ -194,14 +352,25 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     };
     const deft_status s = id_bytes == 8 ? group(int64_t{}) : group(int32_t{});
     if (s != DEFT_OK) return s;
-    const int slices = (int)((a.width + 255) / 256);
-    const int64_t blocks = (a.rows * slices + 7) / 8;
-    if (blocks > 0x7fffffff) return DEFT_ERR_TOO_LARGE;
+    const ReduceArgs r{out.sorted, out.row_tab, out.total, reinterpret_cast<float*>(a.ws + w.partial), out.arrived, w.unit, w.units, w.slices};
+    // The second kernel's CTAs take their places while the first still runs and wait there for its end.
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kReduceThreads);
+    cfg.stream = stream;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    auto reduce = [&](auto t, auto al, auto gal) -> deft_status {
+        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_rows_reduce<decltype(t), decltype(al)::value, decltype(gal)::value>, a, r));
+        return DEFT_OK;
+    };
+    const bool wide = row_align(a.grad, a.width, sizeof(float)) == 16;
     return with_type(dy_type, [&](auto t) {
         return with_align(row_align(a.dy, a.ld_dy, type_bytes(dy_type)), [&](auto al) -> deft_status {
-            k_rows_sum<decltype(t), decltype(al)::value><<<(unsigned)blocks, 256, 0, stream>>>(a, out.sorted, out.row_tab, slices);
-            DEFT_CUDA_TRY(cudaGetLastError());
-            return DEFT_OK;
+            return wide ? reduce(t, al, AlignTag<16>{}) : reduce(t, al, AlignTag<0>{});
         });
     });
 }
