@@ -1,66 +1,187 @@
 // Embedding lookup and dropout: rows of a matrix taken in groups of eight columns.
+//
+// A thread keeps its columns and takes every `stride`-th row (up to four rows' loads in flight), so that consecutive
+// threads read consecutive groups whatever the width, one division places it, and the parts of the generator's first
+// two rounds that depend on the column or the offset alone are computed once.  Rows that start on no 8-byte boundary are taken by warps in slices of
+// 256 columns instead, dealt out one by one.
 #include "deft_rows.cuh"
 
 namespace deft {
 namespace {
 
 constexpr int kRowThreads = 256;
+constexpr int kInFlight = 16;    // words a thread that takes several rows has in flight
+constexpr int kMostDeep = 4;     // rows it has in flight, when a row's group is four words
+constexpr int kMostEach = 16;    // rows it takes in all
+constexpr int kRounds = 8;       // rounds of CTAs a launch has at least before threads take several rows
+constexpr int kBlocksOne = 8;    // CTAs an SM holds where threads take one row (32 registers) ...
+constexpr int kBlocksDeep = 4;   // ... and where they take several (64)
 
-template <typename TW, typename TO, typename Id, int kAlign>
-__global__ void __launch_bounds__(kRowThreads) k_embed(const EmbedArgs a, uint32_t groups, int64_t total) {
+// Rows in flight of a thread that loads `words` words of each.
+__host__ __device__ constexpr int deep_of(int words) {
+    return kInFlight / words < 2 ? 2 : (kInFlight / words > kMostDeep ? kMostDeep : kInFlight / words);
+}
+
+// How the matrix is split: `units` (groups of a row, or slices of it) times `stride` rows are taken at a time.
+struct RowSplit {
+    FastDiv units;
+    uint32_t stride, rows;
+    bool same_pos;       // all rows of a thread have the same position row
+};
+
+// What one thread (kAlign != 0) or warp (kAlign == 0) works on.
+template <int kAlign>
+struct Place {
+    static constexpr int kSpan = kAlign ? kGroup : 256;
+    uint32_t row, unit;
+    int64_t col;      // first column of the group or slice
+    __device__ __forceinline__ explicit Place(const RowSplit& s) {
+        const uint32_t at = kAlign ? blockIdx.x * (uint32_t)kRowThreads + threadIdx.x
+                                   : blockIdx.x * (uint32_t)(kRowThreads / 32) + (threadIdx.x >> 5);
+        row = s.units.div(at);
+        unit = at - row * s.units.d;
+        col = (int64_t)unit * kSpan;
+    }
+};
+
+// kAlign != 0: eight columns of this thread; else this lane's share of the slice.  kFull: none of the group's (slice's)
+// columns lies beyond the row's end; left = columns from the first one to the end.
+template <bool kFull, typename T, int kAlign>
+__device__ __forceinline__ void fetch_share(const T* p, int left, Raw8<T, kAlign>& raw) {
+    if constexpr (kAlign != 0) fetch8<kFull>(p, left, raw);
+    else fetch_dealt<kFull>(p, left, raw);
+}
+template <bool kFull, typename T, int kAlign>
+__device__ __forceinline__ void store_share(T* p, int left, const float (&v)[kGroup]) {
+    if constexpr (kAlign != 0) store8<T, kAlign>(p, kFull ? kGroup : left, v);
+    else store_dealt<kFull>(p, left, v);
+}
+template <int kAlign>
+__device__ __forceinline__ void drop_share(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t unit) {
+    if constexpr (kAlign != 0) drop8<true>(v, d, offset, row, unit);
+    else drop8_dealt<true>(v, d, offset, row, unit);
+}
+
+template <bool kFull, int kDeep, bool kPos, typename TW, typename TO, typename Id, int kAlign>
+__device__ __forceinline__ void embed_rows(const EmbedArgs& a, const RowSplit& split, const FastDiv& pos_rows, const Place<kAlign>& at, int left) {
     const uint64_t offset = drop_offset(a.drop);
-    for (int64_t g = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; g < total; g += (int64_t)gridDim.x * kRowThreads) {
-        const int64_t t = g / groups;
-        const uint32_t group = (uint32_t)(g - t * groups);
-        const int64_t col = (int64_t)group * kGroup;
-        const int count = a.width - col < kGroup ? (int)(a.width - col) : kGroup;
-        const int64_t id = (int64_t)static_cast<const Id*>(a.ids)[t];
-        float v[kGroup] = {};
-        if (id >= 0 && id < a.rows) load8<TW, kAlign>(static_cast<const TW*>(a.table) + id * a.ld_table + col, count, v);
+    const TW* table = static_cast<const TW*>(a.table) + at.col;
+    const TW* pos = static_cast<const TW*>(a.pos) + at.col;
+    TO* out = static_cast<TO*>(a.out) + at.col;
+    const Id* ids = static_cast<const Id*>(a.ids);
+    Raw8<TW, kAlign> q;
+    if (kPos) fetch_share<kFull>(pos + (int64_t)(at.row - pos_rows.div(at.row) * pos_rows.d) * a.ld_pos, left, q);
+    for (uint32_t t0 = at.row; t0 < split.rows; t0 += kDeep * split.stride) {
+        Raw8<TW, kAlign> w[kDeep];
+        int64_t id[kDeep];
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) v[i] = __fmul_rn(v[i], a.scale);
-        if (a.pos) {
-            float q[kGroup];
-            load8<TW, kAlign>(static_cast<const TW*>(a.pos) + (t % a.pos_rows) * a.ld_pos + col, count, q);
-#pragma unroll
-            for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], q[i]);
+        for (int k = 0; k < kDeep; ++k) {
+            const uint32_t t = t0 + k * split.stride;
+            id[k] = t < split.rows ? (int64_t)__ldg(ids + t) : -1;
         }
-        if (a.drop.threshold) drop8<true>(v, a.drop, offset, (uint32_t)t, group);
-        store8<TO, kAlign>(static_cast<TO*>(a.out) + t * a.ld_out + col, count, v);
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k)
+            if (id[k] >= 0 && id[k] < a.rows) fetch_share<kFull>(table + id[k] * a.ld_table, left, w[k]);
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const uint32_t t = t0 + k * split.stride;
+            if (t >= split.rows) break;
+            float v[kGroup];
+            w[k].unpack(v);
+            if (id[k] < 0 || id[k] >= a.rows) {      // a row outside the table
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) v[i] = 0.0f;
+            }
+            if (a.scale != 1.0f) {
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) v[i] = __fmul_rn(v[i], a.scale);
+            }
+            if (kPos) {
+                float x[kGroup];
+                if (!split.same_pos) fetch_share<kFull>(pos + (int64_t)(t - pos_rows.div(t) * pos_rows.d) * a.ld_pos, left, q);
+                q.unpack(x);
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], x[i]);
+            }
+            if (a.drop.threshold) drop_share<kAlign>(v, a.drop, offset, t, at.unit);
+            store_share<kFull, TO, kAlign>(out + (int64_t)t * a.ld_out, left, v);
+        }
     }
 }
 
-template <typename TX, typename TY, int kAlign>
-__global__ void __launch_bounds__(kRowThreads) k_dropout(const DropoutArgs a, uint32_t groups, int64_t total) {
+template <int kDeep, bool kPos, typename TW, typename TO, typename Id, int kAlign>
+__global__ void __launch_bounds__(kRowThreads, kDeep == 1 ? kBlocksOne : kBlocksDeep) k_embed(const __grid_constant__ EmbedArgs a, const RowSplit split, const FastDiv pos_rows) {
+    const Place<kAlign> at(split);
+    if (at.row >= split.stride) return;
+    const int64_t left = a.width - at.col;
+    if (left >= at.kSpan) embed_rows<true, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, at.kSpan);
+    else embed_rows<false, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, (int)left);
+}
+
+template <bool kFull, int kDeep, bool kAdd, typename TX, typename TY, int kAlign>
+__device__ __forceinline__ void dropout_rows(const DropoutArgs& a, const RowSplit& split, const Place<kAlign>& at, int left) {
     const uint64_t offset = drop_offset(a.drop);
-    for (int64_t g = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; g < total; g += (int64_t)gridDim.x * kRowThreads) {
-        const int64_t r = g / groups;
-        const uint32_t group = (uint32_t)(g - r * groups);
-        const int64_t col = (int64_t)group * kGroup;
-        const int count = a.cols - col < kGroup ? (int)(a.cols - col) : kGroup;
-        float v[kGroup];
-        load8<TX, kAlign>(static_cast<const TX*>(a.x) + r * a.ld_x + col, count, v);
-        if (a.drop.threshold) drop8<true>(v, a.drop, offset, (uint32_t)r, group);
-        if (a.add) {
-            float q[kGroup];
-            load8<TY, kAlign>(static_cast<const TY*>(a.add) + r * a.ld_add + col, count, q);
+    const TX* x = static_cast<const TX*>(a.x) + at.col;
+    const TY* add = static_cast<const TY*>(a.add) + at.col;
+    TY* y = static_cast<TY*>(a.y) + at.col;
+    for (uint32_t r0 = at.row; r0 < split.rows; r0 += kDeep * split.stride) {
+        Raw8<TX, kAlign> w[kDeep];
+        Raw8<TY, kAlign> q[kDeep];
 #pragma unroll
-            for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], q[i]);
+        for (int k = 0; k < kDeep; ++k) {
+            const uint32_t r = r0 + k * split.stride;
+            if (r < split.rows) {
+                fetch_share<kFull>(x + (int64_t)r * a.ld_x, left, w[k]);
+                if (kAdd) fetch_share<kFull>(add + (int64_t)r * a.ld_add, left, q[k]);
+            }
         }
-        store8<TY, kAlign>(static_cast<TY*>(a.y) + r * a.ld_y + col, count, v);
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const uint32_t r = r0 + k * split.stride;
+            if (r >= split.rows) break;
+            float v[kGroup];
+            w[k].unpack(v);
+            if (a.drop.threshold) drop_share<kAlign>(v, a.drop, offset, r, at.unit);
+            if (kAdd) {
+                float z[kGroup];
+                q[k].unpack(z);
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], z[i]);
+            }
+            store_share<kFull, TY, kAlign>(y + (int64_t)r * a.ld_y, left, v);
+        }
     }
 }
 
-inline unsigned grid_of(int64_t total) {
-    const int64_t want = (total + kRowThreads - 1) / kRowThreads;
-    return (unsigned)(want < 0x7fffffff ? want : 0x7fffffff);
+template <int kDeep, bool kAdd, typename TX, typename TY, int kAlign>
+__global__ void __launch_bounds__(kRowThreads, kDeep == 1 ? kBlocksOne : kBlocksDeep) k_dropout(const __grid_constant__ DropoutArgs a, const RowSplit split) {
+    const Place<kAlign> at(split);
+    if (at.row >= split.stride) return;
+    const int64_t left = a.cols - at.col;
+    if (left >= at.kSpan) dropout_rows<true, kDeep, kAdd, TX, TY, kAlign>(a, split, at, at.kSpan);
+    else dropout_rows<false, kDeep, kAdd, TX, TY, kAlign>(a, split, at, (int)left);
+}
+
+// Threads take up to kMostEach rows each, as many as leave every SM several rounds of CTAs (the last round is rarely
+// full).  pos_rows != 0: `stride` becomes a multiple of it where that is possible, so that a thread reads its position
+// row once for all its tokens.
+inline RowSplit row_split(int64_t rows, int64_t cols, int align, int64_t pos_rows, unsigned* blocks) {
+    const int64_t units = align ? (cols + kGroup - 1) / kGroup : (cols + 255) / 256;
+    const int64_t per_block = align ? kRowThreads : kRowThreads / 32;
+    int64_t each = rows * units / ((int64_t)sm_count() * kBlocksDeep * per_block * kRounds);
+    each = each < 1 ? 1 : (each > kMostEach ? kMostEach : each);
+    int64_t stride = (rows + each - 1) / each;
+    if (pos_rows && each > 1 && pos_rows < rows) stride = (stride + pos_rows - 1) / pos_rows * pos_rows;
+    const int64_t most = (0x7fffffff - 255) / units;   // places are 31-bit; a larger matrix takes more turns of the loop
+    if (stride > most) stride = most;
+    if (stride > rows) stride = rows;
+    *blocks = (unsigned)((stride * units + per_block - 1) / per_block);
+    return RowSplit{fast_div((uint32_t)units), (uint32_t)stride, (uint32_t)rows, pos_rows && (stride % pos_rows == 0 || stride == rows)};
 }
 
 }  // namespace
 
 deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int id_bytes, cudaStream_t stream) {
-    const uint32_t groups = (uint32_t)((a.width + kGroup - 1) / kGroup);
-    const int64_t total = a.n * groups;
     int align = row_align(a.table, a.ld_table, type_bytes(table_type));
     const int ao = row_align(a.out, a.ld_out, type_bytes(out_type));
     if (ao < align) align = ao;
@@ -68,14 +189,24 @@ deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int i
         const int ap = row_align(a.pos, a.ld_pos, type_bytes(table_type));
         if (ap < align) align = ap;
     }
+    unsigned blocks;
+    const RowSplit split = row_split(a.n, a.width, align, a.pos ? a.pos_rows : 0, &blocks);
+    // a token's number is below 2^31: more position rows than that are never wrapped around
+    const FastDiv pos_rows = fast_div((uint32_t)(a.pos_rows < 0x7fffffff ? a.pos_rows : 0x7fffffff));
     return with_type(table_type, [&](auto w) {
         return with_type(out_type, [&](auto o) {
             return with_align(align, [&](auto al) -> deft_status {
                 using TW = decltype(w);
                 using TO = decltype(o);
                 constexpr int kAlign = decltype(al)::value;
-                if (id_bytes == 8) k_embed<TW, TO, int64_t, kAlign><<<grid_of(total), kRowThreads, 0, stream>>>(a, groups, total);
-                else k_embed<TW, TO, int32_t, kAlign><<<grid_of(total), kRowThreads, 0, stream>>>(a, groups, total);
+                auto run = [&](auto kernel) { kernel<<<blocks, kRowThreads, 0, stream>>>(a, split, pos_rows); };
+                auto with_id = [&](auto id) {
+                    using Id = decltype(id);
+                    constexpr int kDeep = deep_of((int)sizeof(TW) * 2);
+                    if (split.stride == split.rows) a.pos ? run(k_embed<1, true, TW, TO, Id, kAlign>) : run(k_embed<1, false, TW, TO, Id, kAlign>);
+                    else a.pos ? run(k_embed<kDeep, true, TW, TO, Id, kAlign>) : run(k_embed<kDeep, false, TW, TO, Id, kAlign>);
+                };
+                id_bytes == 8 ? with_id(int64_t{}) : with_id(int32_t{});
                 DEFT_CUDA_TRY(cudaGetLastError());
                 return DEFT_OK;
             });
@@ -84,8 +215,6 @@ deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int i
 }
 
 deft_status launch_dropout(const DropoutArgs& a, int x_type, int y_type, cudaStream_t stream) {
-    const uint32_t groups = (uint32_t)((a.cols + kGroup - 1) / kGroup);
-    const int64_t total = a.rows * groups;
     int align = row_align(a.x, a.ld_x, type_bytes(x_type));
     const int ay = row_align(a.y, a.ld_y, type_bytes(y_type));
     if (ay < align) align = ay;
@@ -93,10 +222,18 @@ deft_status launch_dropout(const DropoutArgs& a, int x_type, int y_type, cudaStr
         const int aa = row_align(a.add, a.ld_add, type_bytes(y_type));
         if (aa < align) align = aa;
     }
+    unsigned blocks;
+    const RowSplit split = row_split(a.rows, a.cols, align, 0, &blocks);
     return with_type(x_type, [&](auto x) {
         return with_type(y_type, [&](auto y) {
             return with_align(align, [&](auto al) -> deft_status {
-                k_dropout<decltype(x), decltype(y), decltype(al)::value><<<grid_of(total), kRowThreads, 0, stream>>>(a, groups, total);
+                auto run = [&](auto kernel) { kernel<<<blocks, kRowThreads, 0, stream>>>(a, split); };
+                using TX = decltype(x);
+                using TY = decltype(y);
+                constexpr int kAlign = decltype(al)::value;
+                constexpr int kPlain = deep_of((int)sizeof(TX) * 2), kBoth = deep_of((int)sizeof(TX) * 2 + (int)sizeof(TY) * 2);
+                if (split.stride == split.rows) a.add ? run(k_dropout<1, true, TX, TY, kAlign>) : run(k_dropout<1, false, TX, TY, kAlign>);
+                else a.add ? run(k_dropout<kBoth, true, TX, TY, kAlign>) : run(k_dropout<kPlain, false, TX, TY, kAlign>);
                 DEFT_CUDA_TRY(cudaGetLastError());
                 return DEFT_OK;
             });

@@ -13,7 +13,7 @@ constexpr int kGroup = 8;   // columns a thread takes at a time: one call of the
 // What dropout needs to know.  threshold = t << 16, where an element is kept when its 16-bit number is at
 // least t = round(65536 p); 0 means no dropout.  gain = 65536 / (65536 - t), rounded once to fp32.
 struct DropArgs {
-    uint32_t key0, key1;
+    uint32_t keys[20];          // the ten rounds' two key words
     uint64_t offset;
     const uint64_t* offset_d;   // added to offset when not NULL (device memory: a replayed graph draws new masks)
     uint32_t threshold;
@@ -21,32 +21,63 @@ struct DropArgs {
 };
 
 // Philox4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3",
-// SC 2011): counter (c.x, c.y, c.z, c.w), key (k0, k1).
-__device__ __forceinline__ uint4 philox10(uint4 c, uint32_t k0, uint32_t k1) {
+// SC 2011).  The rounds' keys come from the host, as operands from the constant bank: a round is two wide products and
+// two three-way exclusive ors.
+__device__ __forceinline__ uint4 philox10(uint4 c, const uint32_t (&keys)[20]) {
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
-        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ keys[2 * r], (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ keys[2 * r + 1], (uint32_t)a);
     }
     return c;
+}
+inline void philox_keys(uint64_t seed, uint32_t (&keys)[20]) {
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+    for (int r = 0; r < 10; ++r, k0 += 0x9E3779B9u, k1 += 0xBB67AE85u) {
+        keys[2 * r] = k0;
+        keys[2 * r + 1] = k1;
+    }
 }
 
 __device__ __forceinline__ uint64_t drop_offset(const DropArgs& d) {
     return d.threshold && d.offset_d ? d.offset + *d.offset_d : d.offset;
 }
 
-// Applies the mask of (row, columns 8 * group .. + 7) to v: dropped elements become +0 whatever they were.
+// The random words of (row, columns 8 * group .. + 7).
+__device__ __forceinline__ uint4 drop_words(const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
+    return philox10(make_uint4(group, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.keys);
+}
+
+// Applies a group's mask to v: dropped elements become +0 whatever they were.  The even column goes by a word's low
+// half, the odd one by its high half.
 template <bool kScale>
 __device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
-    const uint4 w = philox10(make_uint4(group, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.key0, d.key1);
+    const uint4 w = drop_words(d, offset, row, group);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // the even column goes by a word's low half, the odd one by its high half
+    for (int i = 0; i < 4; ++i) {
         const float a = kScale ? v[2 * i] * d.gain : v[2 * i], b = kScale ? v[2 * i + 1] * d.gain : v[2 * i + 1];
         v[2 * i] = (u[i] << 16) >= d.threshold ? a : 0.0f;
         v[2 * i + 1] = u[i] >= d.threshold ? b : 0.0f;
+    }
+}
+
+// The same where a warp's 256 columns are dealt out one by one (lane l has the columns 32 k + l): every lane draws the
+// eight bits of its own group and fetches those of its columns from the lanes that have them.
+template <bool kScale>
+__device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
+    const int lane = threadIdx.x & 31;
+    const uint4 w = drop_words(d, offset, row, slice * 32 + lane);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        bits |= ((u[i] << 16) >= d.threshold ? 1u << (2 * i) : 0u) | (u[i] >= d.threshold ? 2u << (2 * i) : 0u);
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) {
+        const uint32_t there = __shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3));
+        const float x = kScale ? v[k] * d.gain : v[k];
+        v[k] = there >> (lane & 7) & 1u ? x : 0.0f;
     }
 }
 
@@ -61,27 +92,46 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return
 template <int kBytes> struct Piece;
 template <> struct Piece<16> { using type = uint4; };
 template <> struct Piece<8> { using type = uint2; };
+template <> struct Piece<4> { using type = uint32_t; };
+template <> struct Piece<2> { using type = uint16_t; };
+
+// Eight elements as they lie in memory.  Loading and converting are apart so that a thread can have several groups'
+// loads in flight before it waits for the first.
+template <typename T, int kAlign>
+struct Raw8 {
+    static constexpr int kPiece = kAlign ? kAlign : (int)sizeof(T);
+    using P = typename Piece<kPiece>::type;
+    static constexpr int kPieces = kGroup * (int)sizeof(T) / kPiece;
+    P piece[kPieces];
+    __device__ __forceinline__ void unpack(float (&v)[kGroup]) const {
+        const T* e = reinterpret_cast<const T*>(piece);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) v[i] = to_f32(e[i]);
+    }
+};
 
 // A group of up to eight consecutive elements.  kAlign: 16 or 8 when every group of the matrix starts on such
 // a boundary (base and row pitch are multiples of it), 0 when only single elements are aligned.
-// count < 8 in the last group of a row: nothing beyond the row is touched.  Plain loads: what is read may be
-// what the same thread writes afterwards (dropout in place, rows added to).
+// kFull: all eight are there; else the first `count` (the last group of a row: nothing beyond it is touched).  Plain
+// loads: what is read may be what the same thread writes afterwards (dropout in place, rows added to).
+template <bool kFull, typename T, int kAlign>
+__device__ __forceinline__ void fetch8(const T* p, int count, Raw8<T, kAlign>& raw) {
+    using P = typename Raw8<T, kAlign>::P;
+    if constexpr (kFull) {
+#pragma unroll
+        for (int i = 0; i < Raw8<T, kAlign>::kPieces; ++i) raw.piece[i] = reinterpret_cast<const P*>(p)[i];
+    } else {
+        T* e = reinterpret_cast<T*>(raw.piece);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) e[i] = i < count ? p[i] : from_f32<T>(0.0f);
+    }
+}
 template <typename T, int kAlign>
 __device__ __forceinline__ void load8(const T* p, int count, float (&v)[kGroup]) {
-    if constexpr (kAlign != 0) {
-        if (count == kGroup) {
-            using P = typename Piece<kAlign>::type;
-            constexpr int per = kAlign / (int)sizeof(T), pieces = kGroup / per;
-            P raw[pieces];
-#pragma unroll
-            for (int i = 0; i < pieces; ++i) raw[i] = reinterpret_cast<const P*>(p)[i];
-#pragma unroll
-            for (int i = 0; i < kGroup; ++i) v[i] = to_f32(reinterpret_cast<const T*>(raw)[i]);
-            return;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) v[i] = i < count ? to_f32(p[i]) : 0.0f;
+    Raw8<T, kAlign> raw;
+    if (kAlign != 0 && count == kGroup) fetch8<true>(p, count, raw);
+    else fetch8<false>(p, count, raw);
+    raw.unpack(v);
 }
 
 template <typename T, int kAlign>
@@ -101,6 +151,37 @@ __device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]
 #pragma unroll
     for (int i = 0; i < kGroup; ++i)
         if (i < count) p[i] = from_f32<T>(v[i]);
+}
+
+// A slice of 256 columns dealt out one by one: lane l has the columns 32 k + l, so that loads and stores of a matrix whose
+// rows start on no vector boundary are whole sectors all the same (eight consecutive elements per lane would touch 32
+// sectors with every load).  kFull: the slice has all
+// 256; else `left` (from its first column to the row's end).
+template <bool kFull, typename T>
+__device__ __forceinline__ void fetch_dealt(const T* p, int left, Raw8<T, 0>& raw) {
+    const int lane = threadIdx.x & 31;
+    T* e = reinterpret_cast<T*>(raw.piece);
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) e[k] = kFull || k * 32 + lane < left ? p[k * 32 + lane] : from_f32<T>(0.0f);
+}
+template <bool kFull, typename T>
+__device__ __forceinline__ void store_dealt(T* p, int left, const float (&v)[kGroup]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k)
+        if (kFull || k * 32 + lane < left) p[k * 32 + lane] = from_f32<T>(v[k]);
+}
+
+// n / d for n < 2^31 by a product (d >= 1): m = ceil(2^p / d) with p = 31 + ceil(log2 d) is exact in that range.
+struct FastDiv {
+    uint32_t d, m, shift;
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> shift; }
+};
+inline FastDiv fast_div(uint32_t d) {
+    uint32_t log = 0;
+    while ((1ull << log) < d) ++log;
+    const uint32_t p = 31 + log;
+    return FastDiv{d, (uint32_t)(((1ull << p) + d - 1) / d), p - 32};
 }
 
 // ---- launchers ----

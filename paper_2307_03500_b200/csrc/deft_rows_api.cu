@@ -23,8 +23,7 @@ bool drop_args(double p, uint64_t seed, uint64_t offset, const uint64_t* offset_
     uint32_t t = (uint32_t)std::floor(p * 65536.0 + 0.5);
     if (t > 65535u) t = 65535u;
     *gain = 65536.0 / (double)(65536u - t);
-    d->key0 = (uint32_t)seed;
-    d->key1 = (uint32_t)(seed >> 32);
+    philox_keys(seed, d->keys);
     d->offset = offset;
     d->offset_d = offset_d;
     d->threshold = t << 16;

@@ -16,8 +16,8 @@ namespace {
 // order of the positions; a table of counts per (warp, row) turns into places by a prefix over the warps and one
 // over the rows.
 constexpr int kOwners = 128;                 // CTAs (a power of two below the 148 SMs)
-constexpr int kListCap = 128;                // own tokens a warp remembers; one that has more reads the ids again
 constexpr size_t kGroupSmem = 220 * 1024;
+constexpr int kListMost = 1024;              // own tokens a warp remembers at most; one that has more reads the ids again
 
 struct GroupOut {
     uint2* sorted;      // [n] (table row, token position)
@@ -27,18 +27,28 @@ struct GroupOut {
     size_t arrived_n;
 };
 
-inline size_t group_smem(int warps, int64_t per_cta) {
-    return sizeof(uint32_t) * (size_t)(warps + 1) * (size_t)per_cta + sizeof(uint2) * (size_t)kListCap * (size_t)warps + 256 + sizeof(uint32_t) * 64;
+// Shared memory: [warps][list_cap] (row of the CTA, token) | [warps][per_cta] counts | [per_cta] first places | sums.
+inline size_t group_smem(int warps, int64_t per_cta, int list_cap) {
+    return sizeof(uint2) * (size_t)list_cap * (size_t)warps + sizeof(uint32_t) * ((size_t)(warps + 1) * (size_t)per_cta + 64);
+}
+
+// An id as a row of the table, or kNoRow.
+constexpr uint32_t kNoRow = 0xffffffffu;
+__device__ __forceinline__ uint32_t row_of(int32_t id, uint32_t rows, uint32_t skip) {
+    return (uint32_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
+}
+__device__ __forceinline__ uint32_t row_of(int64_t id, uint32_t rows, uint32_t skip) {
+    return (uint64_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
 }
 
 template <typename Id>
-__global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ ids, uint32_t n, int64_t rows, int64_t skip_id,
-                                                        int per_cta, const GroupOut out) {
+__global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ ids, uint32_t n, uint32_t rows, uint32_t skip,
+                                                        int per_cta, int list_cap, const GroupOut out) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t me = blockIdx.x, lt = (1u << lane) - 1u;
-    uint2* list = reinterpret_cast<uint2*>(smem) + warp * kListCap;
-    uint32_t* cnt = reinterpret_cast<uint32_t*>(smem + sizeof(uint2) * kListCap * warps);   // [warps][per_cta]
+    uint2* list = reinterpret_cast<uint2*>(smem) + warp * list_cap;
+    uint32_t* cnt = reinterpret_cast<uint32_t*>(smem + sizeof(uint2) * list_cap * warps);   // [warps][per_cta]
     uint32_t* start = cnt + (size_t)warps * per_cta;                                        // [per_cta]
     uint32_t* red = start + per_cta;                                                        // [2][32]
     asm volatile("griddepcontrol.launch_dependents;");
@@ -49,25 +59,24 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
     const uint32_t part = (n + warps - 1) / warps;
     const uint32_t lo = min((uint32_t)warp * part, n), hi = min(lo + part, n);
     uint32_t below = 0, have = 0;   // valid tokens of lower CTAs (per lane); own tokens of this warp
-    for (uint32_t p = lo; p < hi; p += 256) {
-        Id v[8];
+    constexpr int kAhead = 16;
+    for (uint32_t p = lo; p < hi; p += 32 * kAhead) {
+        uint32_t row[kAhead];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kAhead; ++j) {
             const uint32_t pos = p + j * 32 + lane;
-            v[j] = pos < hi ? __ldg(ids + pos) : (Id)-1;
+            row[j] = pos < hi ? row_of(__ldg(ids + pos), rows, skip) : kNoRow;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t id = (int64_t)v[j];
-            const bool ok = id >= 0 && id < rows && id != skip_id;
-            const uint32_t owner = (uint32_t)id & (kOwners - 1);
-            below += ok && owner < me;
-            const bool own = ok && owner == me;
+        for (int j = 0; j < kAhead; ++j) {
+            const uint32_t owner = row[j] % kOwners;
+            below += row[j] != kNoRow && owner < me;
+            const bool own = row[j] != kNoRow && owner == me;
             const uint32_t mask = __ballot_sync(0xffffffffu, own);
             if (own) {
-                const uint32_t r = (uint32_t)(id / kOwners), at = have + __popc(mask & lt);
+                const uint32_t r = row[j] / kOwners, at = have + __popc(mask & lt);
                 atomicAdd(mine + r, 1u);
-                if (at < kListCap) list[at] = make_uint2(r, p + j * 32 + lane);
+                if (at < (uint32_t)list_cap) list[at] = make_uint2(r, p + j * 32 + lane);
             }
             have += __popc(mask);
         }
@@ -105,32 +114,32 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
     for (int r = r0; r < r1; ++r) {
         const uint32_t c = start[r];
         start[r] = at;
-        const int64_t row = (int64_t)r * kOwners + me;
+        const uint32_t row = (uint32_t)r * kOwners + me;
         if (row < rows) out.row_tab[row] = make_uint2(at, c);
         at += c;
     }
     if (me == kOwners - 1 && threadIdx.x == blockDim.x - 1) *out.total = at;
     __syncthreads();
     // each warp puts its tokens in place, 32 at a time in order of position
-    const bool again = have > kListCap;
+    const bool again = have > (uint32_t)list_cap;
     const uint32_t steps = again ? hi - lo : have;
     for (uint32_t i0 = 0; i0 < steps; i0 += 32) {
         const uint32_t i = i0 + lane;
-        uint32_t r = 0xffffffffu, pos = 0;
+        uint32_t r = kNoRow, pos = 0;
         if (!again) {
             if (i < have) { r = list[i].x; pos = list[i].y; }
         } else if (i < steps) {
             pos = lo + i;
-            const int64_t id = (int64_t)__ldg(ids + pos);
-            if (id >= 0 && id < rows && id != skip_id && ((uint32_t)id & (kOwners - 1)) == me) r = (uint32_t)(id / kOwners);
+            const uint32_t row = row_of(__ldg(ids + pos), rows, skip);
+            if (row != kNoRow && row % kOwners == me) r = row / kOwners;
         }
         const uint32_t same = __match_any_sync(0xffffffffu, r);
-        if (r != 0xffffffffu) {
+        if (r != kNoRow) {
             const uint32_t place = start[r] + mine[r] + __popc(same & lt);
             out.sorted[place] = make_uint2(r * kOwners + me, pos);
         }
         __syncwarp();
-        if (r != 0xffffffffu && (same & lt) == 0) mine[r] += __popc(same);
+        if (r != kNoRow && (same & lt) == 0) mine[r] += __popc(same);
         __syncwarp();
     }
 }
@@ -143,6 +152,7 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 // leaves a partial sum per unit; the warp that arrives last at the run's counter adds them in order (in two levels of
 // kJoin when there are more), so the bits do not depend on the order of arrival.
 constexpr int kReduceThreads = 256;
+constexpr int kReduceBlocks = 3; // CTAs an SM holds
 constexpr int kJoin = 32;        // units whose partial sums one warp adds up
 constexpr int kDeep = 4;         // tokens whose loads a warp has in flight
 constexpr int kZeroRows = 8;     // rows a warp clears if they have no tokens
@@ -156,36 +166,109 @@ struct ReduceArgs {
     int unit, units, slices;
 };
 
-__device__ __forceinline__ float4 load_cg(const float* p) { return __ldcg(reinterpret_cast<const float4*>(p)); }
+// A warp's share of 256 columns of a row: eight per lane side by side (kAlign != 0; both matrices' rows start on such a
+// boundary), or dealt out one by one (kAlign == 0).  left: columns from the slice's first one to the row's end.
+template <typename T, int kAlign>
+__device__ __forceinline__ void fetch_slice(const T* p, int left, Raw8<T, kAlign>& raw) {
+    if constexpr (kAlign != 0) {
+        const int mine = left - (int)(threadIdx.x & 31) * kGroup;
+        p += (threadIdx.x & 31) * kGroup;
+        if (mine >= kGroup) fetch8<true>(p, mine, raw);
+        else if (mine > 0) fetch8<false>(p, mine, raw);
+    } else {
+        fetch_dealt<false>(p, left, raw);
+    }
+}
+template <int kAlign>
+__device__ __forceinline__ void store_slice(float* p, int left, const float (&v)[kGroup]) {
+    if constexpr (kAlign != 0) {
+        const int mine = left - (int)(threadIdx.x & 31) * kGroup;
+        p += (threadIdx.x & 31) * kGroup;
+        if (mine > 0) store8<float, 16>(p, mine < kGroup ? mine : kGroup, v);
+    } else {
+        store_dealt<false>(p, left, v);
+    }
+}
+// The gradient's rows start on 16-byte boundaries wherever kAlign != 0.
+template <int kAlign> constexpr int kGradAlign = kAlign ? 16 : 0;
 
-// Adds one row's 8 columns to the gradient (or writes them).
-template <int kGradAlign>
-__device__ __forceinline__ void emit8(float* dst, int count, const float (&sum)[kGroup], const float (&old)[kGroup], float factor, bool accumulate) {
-    float g[kGroup];
+// One row's columns: its tokens' sum times the factor, written or added to what was there.
+template <bool kAdd, int kAlign>
+__device__ __forceinline__ void emit(float* dst, int left, const float (&sum)[kGroup], const Raw8<float, kGradAlign<kAlign>>& old, float factor) {
+    float g[kGroup], was[kGroup];
+    if (kAdd) old.unpack(was);
 #pragma unroll
     for (int c = 0; c < kGroup; ++c) {
         g[c] = __fmul_rn(sum[c], factor);
-        if (accumulate) g[c] = __fadd_rn(old[c], g[c]);
+        if (kAdd) g[c] = __fadd_rn(was[c], g[c]);
     }
-    store8<float, kGradAlign>(dst, count, g);
+    store_slice<kAlign>(dst, left, g);
 }
 
-template <typename T, int kAlign, int kGradAlign>
-__global__ void __launch_bounds__(kReduceThreads) k_rows_reduce(const EmbedGradArgs a, const ReduceArgs r) {
+// A run of one row that crosses units: leaves this unit's partial sum; the last warp to arrive adds them all up.  The
+// run's units are s .. t; a unit's partial sum lies at its odd place where the run starts in it, else at its even one.
+template <bool kAdd, int kAlign>
+__device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r, uint32_t row, int unit_id, int slice, int left,
+                                  float4 lo, float4 hi) {
+    const int lane = threadIdx.x & 31;
+    const uint2 tab = r.row_tab[row];
+    const int s = (int)(tab.x / (uint32_t)r.unit), t = (int)((tab.x + tab.y - 1) / (uint32_t)r.unit);
+    const size_t pitch = (size_t)r.slices * 256;
+    auto place = [&](int u) { return (size_t)(2 * u + (u == s ? 1 : 0)); };
+    auto at = [&](int u) { return reinterpret_cast<float4*>(r.partial + place(u) * pitch + (size_t)slice * 256 + lane * kGroup); };
+    auto leave = [&](int u) { at(u)[0] = lo; at(u)[1] = hi; };
+    // true for the last of `expected` warps to arrive at a unit's place
+    auto last_at = [&](int u, int level, int expected) {
+        __threadfence();
+        __syncwarp();
+        uint32_t n = 0;
+        if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + place(u)) * r.slices + slice, 1u);
+        n = __shfl_sync(0xffffffffu, n, 0);
+        __threadfence();
+        return n == (uint32_t)(expected - 1);
+    };
+    // the partial sums of the units u, the next multiple of step, ... below end, in order
+    auto add_up = [&](int u, int step, int end) {
+        lo = hi = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+        for (; u < end; u = (u / step + 1) * step) {
+            const float4 x = __ldcg(at(u)), y = __ldcg(at(u) + 1);
+            lo.x += x.x; lo.y += x.y; lo.z += x.z; lo.w += x.w;
+            hi.x += y.x; hi.y += y.y; hi.z += y.z; hi.w += y.w;
+        }
+    };
+    leave(unit_id);
+    const int u0 = max(s, unit_id / kJoin * kJoin), u1 = min(t + 1, (unit_id / kJoin + 1) * kJoin);
+    const int groups = t / kJoin - s / kJoin + 1;
+    if (!last_at(u0, 0, u1 - u0)) return;
+    add_up(u0, 1, u1);
+    if (groups > 1) {
+        leave(u0);
+        if (!last_at(s, 1, groups)) return;
+        add_up(s, kJoin, t + 1);
+    }
+    float* dst = a.grad + (int64_t)row * a.width + (int64_t)slice * 256;
+    Raw8<float, kGradAlign<kAlign>> old;
+    if (kAdd) fetch_slice(dst, left, old);
+    const float sum[kGroup] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    emit<kAdd, kAlign>(dst, left, sum, old, a.factor);
+}
+
+template <bool kAdd, typename T, int kAlign>
+__global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(const __grid_constant__ EmbedGradArgs a, const __grid_constant__ ReduceArgs r) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * (kReduceThreads / 32) + (threadIdx.x >> 5);
     const int64_t reduce_tasks = (int64_t)r.units * r.slices;
     if (task >= reduce_tasks) {
         // rows without tokens, where the gradient is written
-        if (a.accumulate) return;
+        if (kAdd) return;
         const int64_t row0 = (task - reduce_tasks) * kZeroRows;
         const bool empty = lane < kZeroRows && row0 + lane < a.rows && r.row_tab[row0 + lane].y == 0;
+        const float zero[kGroup] = {};
         for (uint32_t m = __ballot_sync(0xffffffffu, empty); m; m &= m - 1) {
             float* dst = a.grad + (row0 + __ffs((int)m) - 1) * a.width;
-            const float zero[kGroup] = {};
-            for (int64_t col = lane * kGroup; col < a.width; col += 32 * kGroup)
-                store8<float, kGradAlign>(dst + col, a.width - col < kGroup ? (int)(a.width - col) : kGroup, zero);
+            for (int64_t col = 0; col < a.width; col += 256) store_slice<kAlign>(dst + col, (int)min(a.width - col, (int64_t)256), zero);
         }
         return;
     }
@@ -193,105 +276,63 @@ __global__ void __launch_bounds__(kReduceThreads) k_rows_reduce(const EmbedGradA
     const uint32_t total = *r.total, first = (uint32_t)unit_id * (uint32_t)r.unit;
     if (first >= total) return;
     const int have = (int)min(total - first, (uint32_t)r.unit);
-    const uint2 item = lane < have ? r.sorted[first + lane] : make_uint2(0xffffffffu, 0u);
-    const uint32_t before = first > 0 ? r.sorted[first - 1].x : 0xffffffffu;
-    const uint32_t after = first + have < total ? r.sorted[first + have].x : 0xffffffffu;
+    const uint2 item = lane < have ? r.sorted[first + lane] : make_uint2(kNoRow, 0u);
+    const uint32_t before = first > 0 ? r.sorted[first - 1].x : kNoRow;
+    const uint32_t after = first + have < total ? r.sorted[first + have].x : kNoRow;
     const uint32_t next_row = __shfl_down_sync(0xffffffffu, item.x, 1);
+    // where runs end, and which of them lie inside the unit
     const uint32_t ends = __ballot_sync(0xffffffffu, lane < have && (lane == have - 1 || next_row != item.x));
-    const bool open_front = before == __shfl_sync(0xffffffffu, item.x, 0);
-    const bool open_back = after == __shfl_sync(0xffffffffu, item.x, have - 1);
-    const int first_end = __ffs((int)ends) - 1;
+    uint32_t closed = ends;
+    if (before == __shfl_sync(0xffffffffu, item.x, 0)) closed &= closed - 1;
+    if (after == __shfl_sync(0xffffffffu, item.x, have - 1)) closed &= ~(1u << (have - 1));
 
-    const uint32_t group = (uint32_t)slice * 32 + lane;
-    const int64_t col = (int64_t)group * kGroup;
-    const int count = col >= a.width ? 0 : (a.width - col < kGroup ? (int)(a.width - col) : kGroup);
+    const int64_t col = (int64_t)slice * 256;
+    const int left = (int)min(a.width - col, (int64_t)256);
     const uint64_t offset = drop_offset(a.drop);
     const T* dy = static_cast<const T*>(a.dy) + col;
-    const size_t pitch = (size_t)r.slices * 256;
-    float sum[kGroup] = {};
+    float* grad = a.grad + col;
+    float sum[kGroup] = {}, front[kGroup];
     for (int i0 = 0; i0 < have; i0 += kDeep) {
-        float v[kDeep][kGroup], old[kDeep][kGroup];
+        Raw8<T, kAlign> v[kDeep];
+        Raw8<float, kGradAlign<kAlign>> old[kDeep];
+        uint32_t pos[kDeep], row[kDeep];
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
-            const int i = i0 + k;
-            const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i & 31), row = __shfl_sync(0xffffffffu, item.x, i & 31);
-            if (i < have && count) {
-                load8<T, kAlign>(dy + (int64_t)pos * a.ld_dy, count, v[k]);
-                const bool closed = !(i == first_end && open_front) && !(i == have - 1 && open_back);
-                if (a.accumulate && (ends >> i & 1u) && closed) load8<float, kGradAlign>(a.grad + (int64_t)row * a.width + col, count, old[k]);
-            }
+            pos[k] = __shfl_sync(0xffffffffu, item.y, (i0 + k) & 31);
+            row[k] = __shfl_sync(0xffffffffu, item.x, (i0 + k) & 31);
+            if (i0 + k < have) fetch_slice(dy + (int64_t)pos[k] * a.ld_dy, left, v[k]);
+            if (kAdd && (closed >> (i0 + k) & 1u)) fetch_slice(grad + (int64_t)row[k] * a.width, left, old[k]);
         }
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
             const int i = i0 + k;
             if (i >= have) break;
-            const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i), row = __shfl_sync(0xffffffffu, item.x, i);
-            if (count) {
-                if (a.drop.threshold) drop8<false>(v[k], a.drop, offset, pos, group);
-#pragma unroll
-                for (int c = 0; c < kGroup; ++c) sum[c] += v[k][c];
+            float x[kGroup];
+            v[k].unpack(x);
+            if (a.drop.threshold) {
+                if constexpr (kAlign != 0) drop8<false>(x, a.drop, offset, pos[k], (uint32_t)slice * 32 + lane);
+                else drop8_dealt<false>(x, a.drop, offset, pos[k], (uint32_t)slice);
             }
+#pragma unroll
+            for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
             if (!(ends >> i & 1u)) continue;
-            const bool front = i == first_end && open_front, back = i == have - 1 && open_back;
-            float* dst = a.grad + (int64_t)row * a.width + col;
-            if (!front && !back) {
-                if (count) emit8<kGradAlign>(dst, count, sum, old[k], a.factor, a.accumulate);
-            } else {
-                // the run's units are s .. t; this unit's partial sum goes to its odd place where the run starts here
-                const uint2 tab = r.row_tab[row];
-                const int s = (int)(tab.x / (uint32_t)r.unit), t = (int)((tab.x + tab.y - 1) / (uint32_t)r.unit);
-                auto place = [&](int u) { return (size_t)(2 * u + (u == s ? 1 : 0)); };
-                float* mine = r.partial + place(unit_id) * pitch + col;
-                *reinterpret_cast<float4*>(mine) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-                *reinterpret_cast<float4*>(mine + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
-                // true for the last of `expected` warps to arrive at a place
-                auto last_at = [&](size_t at, int level, int expected) {
-                    __threadfence();
-                    __syncwarp();
-                    uint32_t n = 0;
-                    if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + at) * r.slices + slice, 1u);
-                    n = __shfl_sync(0xffffffffu, n, 0);
-                    __threadfence();
-                    return n == (uint32_t)(expected - 1);
-                };
-                // the partial sums of the units u, u + step, ... below end, in order
-                auto add_up = [&](int u, int step, int end) {
-                    float total8[kGroup] = {};
-#pragma unroll 4
-                    for (; u < end; u = (u / step + 1) * step) {
-                        const float* p = r.partial + place(u) * pitch + col;
-                        const float4 x = load_cg(p), y = load_cg(p + 4);
-                        total8[0] += x.x; total8[1] += x.y; total8[2] += x.z; total8[3] += x.w;
-                        total8[4] += y.x; total8[5] += y.y; total8[6] += y.z; total8[7] += y.w;
-                    }
+            if (closed >> i & 1u) emit<kAdd, kAlign>(grad + (int64_t)row[k] * a.width, left, sum, old[k], a.factor);
+            else if (i == have - 1) break;      // (the last run: its sum stays)
 #pragma unroll
-                    for (int c = 0; c < kGroup; ++c) sum[c] = total8[c];
-                };
-                const int u0 = max(s, unit_id / kJoin * kJoin), u1 = min(t + 1, (unit_id / kJoin + 1) * kJoin);
-                const int groups = t / kJoin - s / kJoin + 1;
-                bool done = false;
-                if (last_at(place(u0), 0, u1 - u0)) {
-                    add_up(u0, 1, u1);
-                    done = groups == 1;
-                    if (!done) {
-                        float* joined = r.partial + place(u0) * pitch + col;
-                        *reinterpret_cast<float4*>(joined) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-                        *reinterpret_cast<float4*>(joined + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
-                        if (last_at(place(s), 1, groups)) {
-                            add_up(s, kJoin, t + 1);
-                            done = true;
-                        }
-                    }
-                }
-                if (done && count) {
-                    float was[kGroup];
-                    if (a.accumulate) load8<float, kGradAlign>(dst, count, was);
-                    emit8<kGradAlign>(dst, count, sum, was, a.factor, a.accumulate);
-                }
+            for (int c = 0; c < kGroup; ++c) {
+                if (!(closed >> i & 1u)) front[c] = sum[c];
+                sum[c] = 0.0f;
             }
-#pragma unroll
-            for (int c = 0; c < kGroup; ++c) sum[c] = 0.0f;
         }
+    }
+    // at most two runs cross the unit's ends: its first and its last (or one that is both)
+    for (uint32_t open = ends & ~closed; open; open &= open - 1) {
+        const int i = __ffs((int)open) - 1;
+        float y[kGroup];
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) y[c] = i == have - 1 ? sum[c] : front[c];
+        join<kAdd, kAlign>(a, r, __shfl_sync(0xffffffffu, item.x, i), unit_id, slice, left, make_float4(y[0], y[1], y[2], y[3]),
+                           make_float4(y[4], y[5], y[6], y[7]));
     }
 }
 
@@ -334,9 +375,15 @@ size_t embed_grad_ws_bytes(int64_t n, int64_t rows, int64_t width) { return grad
 deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes, cudaStream_t stream) {
     const int per_cta = (int)((a.rows + kOwners - 1) / kOwners);
     int warps = 32;
-    while (warps > 1 && group_smem(warps, per_cta) > kGroupSmem) warps >>= 1;
-    const size_t smem = group_smem(warps, per_cta);
-    if (smem > kGroupSmem) return DEFT_ERR_TOO_LARGE;
+    while (warps > 1 && group_smem(warps, per_cta, 128) > kGroupSmem) warps >>= 1;
+    if (group_smem(warps, per_cta, 1) > kGroupSmem) return DEFT_ERR_TOO_LARGE;
+    int list_cap = (int)((kGroupSmem - group_smem(warps, per_cta, 0)) / (sizeof(uint2) * (size_t)warps));
+    const int part = (int)((a.n + warps - 1) / warps);      // more than a warp can have
+    if (list_cap > kListMost) list_cap = kListMost;
+    if (list_cap > part) list_cap = part > 1 ? part : 1;
+    const size_t smem = group_smem(warps, per_cta, list_cap);
+    // -1, and any other number that is no row, leaves nothing out
+    const uint32_t skip = a.skip_id >= 0 && a.skip_id < a.rows ? (uint32_t)a.skip_id : kNoRow;
     const GradWs w = grad_ws(a.n, a.rows, a.width);
     const int64_t tasks = (int64_t)w.units * w.slices + (a.accumulate ? 0 : (a.rows + kZeroRows - 1) / kZeroRows);
     const int64_t blocks = (tasks + kReduceThreads / 32 - 1) / (kReduceThreads / 32);
@@ -346,7 +393,7 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     auto group = [&](auto id) -> deft_status {
         using Id = decltype(id);
         DEFT_CUDA_TRY(cudaFuncSetAttribute(k_group_tokens<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGroupSmem));
-        k_group_tokens<Id><<<kOwners, warps * 32, smem, stream>>>(static_cast<const Id*>(a.ids), (uint32_t)a.n, a.rows, a.skip_id, per_cta, out);
+        k_group_tokens<Id><<<kOwners, warps * 32, smem, stream>>>(static_cast<const Id*>(a.ids), (uint32_t)a.n, (uint32_t)a.rows, skip, per_cta, list_cap, out);
         DEFT_CUDA_TRY(cudaGetLastError());
         return DEFT_OK;
     };
@@ -363,14 +410,14 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     cfg.stream = stream;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    auto reduce = [&](auto t, auto al, auto gal) -> deft_status {
-        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_rows_reduce<decltype(t), decltype(al)::value, decltype(gal)::value>, a, r));
-        return DEFT_OK;
-    };
-    const bool wide = row_align(a.grad, a.width, sizeof(float)) == 16;
+    const int align = row_align(a.grad, a.width, sizeof(float)) == 16 && a.n ? row_align(a.dy, a.ld_dy, type_bytes(dy_type)) : 0;
     return with_type(dy_type, [&](auto t) {
-        return with_align(row_align(a.dy, a.ld_dy, type_bytes(dy_type)), [&](auto al) -> deft_status {
-            return wide ? reduce(t, al, AlignTag<16>{}) : reduce(t, al, AlignTag<0>{});
+        return with_align(align, [&](auto al) -> deft_status {
+            using T = decltype(t);
+            constexpr int kAlign = decltype(al)::value;
+            DEFT_CUDA_TRY(a.accumulate ? cudaLaunchKernelEx(&cfg, k_rows_reduce<true, T, kAlign>, a, r)
+                                       : cudaLaunchKernelEx(&cfg, k_rows_reduce<false, T, kAlign>, a, r));
+            return DEFT_OK;
         });
     });
 }
