@@ -110,32 +110,21 @@ struct Raw8 {
     }
 };
 
-// A group of up to eight consecutive elements.  kAlign: 16 or 8 when every group of the matrix starts on such
-// a boundary (base and row pitch are multiples of it), 0 when only single elements are aligned.
-// kFull: all eight are there; else the first `count` (the last group of a row: nothing beyond it is touched).  Plain
-// loads: what is read may be what the same thread writes afterwards (dropout in place, rows added to).
+// A group of eight consecutive elements of which the first `left` (or more) belong to the row.  kAlign: 16 or 8 when
+// every group of the matrix starts on such a boundary (base and row pitch are multiples of it).  A piece that starts
+// inside the row is read whole (what lies behind the row's end in it is not used); pieces behind the end are not
+// touched.  Plain loads: what is read may be what the same thread writes afterwards (dropout in place, rows added to).
 template <bool kFull, typename T, int kAlign>
-__device__ __forceinline__ void fetch8(const T* p, int count, Raw8<T, kAlign>& raw) {
+__device__ __forceinline__ void fetch8(const T* p, int left, Raw8<T, kAlign>& raw) {
     using P = typename Raw8<T, kAlign>::P;
-    if constexpr (kFull) {
+    constexpr int per = kAlign / (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < Raw8<T, kAlign>::kPieces; ++i) raw.piece[i] = reinterpret_cast<const P*>(p)[i];
-    } else {
-        T* e = reinterpret_cast<T*>(raw.piece);
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) e[i] = i < count ? p[i] : from_f32<T>(0.0f);
-    }
-}
-template <typename T, int kAlign>
-__device__ __forceinline__ void load8(const T* p, int count, float (&v)[kGroup]) {
-    Raw8<T, kAlign> raw;
-    if (kAlign != 0 && count == kGroup) fetch8<true>(p, count, raw);
-    else fetch8<false>(p, count, raw);
-    raw.unpack(v);
+    for (int i = 0; i < Raw8<T, kAlign>::kPieces; ++i)
+        if (kFull || i * per < left) raw.piece[i] = reinterpret_cast<const P*>(p)[i];
 }
 
 template <typename T, int kAlign>
-__device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]) {
+__device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]) {   // the first `count` of them
     if constexpr (kAlign != 0) {
         if (count == kGroup) {
             using P = typename Piece<kAlign>::type;

@@ -51,7 +51,6 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
     uint32_t* cnt = reinterpret_cast<uint32_t*>(smem + sizeof(uint2) * list_cap * warps);   // [warps][per_cta]
     uint32_t* start = cnt + (size_t)warps * per_cta;                                        // [per_cta]
     uint32_t* red = start + per_cta;                                                        // [2][32]
-    asm volatile("griddepcontrol.launch_dependents;");
     for (int i = threadIdx.x; i < warps * per_cta; i += blockDim.x) cnt[i] = 0u;
     for (size_t i = (size_t)me * blockDim.x + threadIdx.x; i < out.arrived_n; i += (size_t)kOwners * blockDim.x) out.arrived[i] = 0u;
     __syncthreads();
@@ -152,10 +151,10 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 // leaves a partial sum per unit; the warp that arrives last at the run's counter adds them in order (in two levels of
 // kJoin when there are more), so the bits do not depend on the order of arrival.
 constexpr int kReduceThreads = 256;
-constexpr int kReduceBlocks = 3; // CTAs an SM holds
+constexpr int kReduceBlocks = 4; // CTAs an SM holds (64 registers a thread)
 constexpr int kJoin = 32;        // units whose partial sums one warp adds up
-constexpr int kDeep = 4;         // tokens whose loads a warp has in flight
 constexpr int kZeroRows = 8;     // rows a warp clears if they have no tokens
+constexpr int kRing = 6144;      // bytes of shared memory a warp's copies go to: 192 KB on an SM
 
 struct ReduceArgs {
     const uint2* sorted;
@@ -164,50 +163,82 @@ struct ReduceArgs {
     float* partial;              // [2 * units][slices * 256]: a unit's first run (even) and last run (odd)
     uint32_t* arrived;           // [2][2 * units * slices]: units of a group, groups of a run
     int unit, units, slices;
+    int64_t clear_blocks;        // CTAs that clear rows (0 where the gradient is added)
 };
 
-// A warp's share of 256 columns of a row: eight per lane side by side (kAlign != 0; both matrices' rows start on such a
-// boundary), or dealt out one by one (kAlign == 0).  left: columns from the slice's first one to the row's end.
-template <typename T, int kAlign>
-__device__ __forceinline__ void fetch_slice(const T* p, int left, Raw8<T, kAlign>& raw) {
-    if constexpr (kAlign != 0) {
-        const int mine = left - (int)(threadIdx.x & 31) * kGroup;
-        p += (threadIdx.x & 31) * kGroup;
-        if (mine >= kGroup) fetch8<true>(p, mine, raw);
-        else if (mine > 0) fetch8<false>(p, mine, raw);
-    } else {
-        fetch_dealt<false>(p, left, raw);
-    }
-}
-template <int kAlign>
+// How a warp shares out the 256 columns of its slice.  kWide (rows of both matrices start on 16-byte boundaries): eight
+// per lane side by side, and a lane copies and reads its own bytes only.  Else they are dealt out one by one (lane l has
+// the columns 32 k + l), the warp copies the 16-byte granules that the slice lies in, and the lanes read at its offset.
+// left: columns from the lane's first one (kWide) or the slice's first one (else) to the row's end, 256 at most.
+template <bool kWide>
+__device__ __forceinline__ int lane_first() { return kWide ? (int)(threadIdx.x & 31) * kGroup : 0; }
+
+template <bool kWide>
 __device__ __forceinline__ void store_slice(float* p, int left, const float (&v)[kGroup]) {
-    if constexpr (kAlign != 0) {
-        const int mine = left - (int)(threadIdx.x & 31) * kGroup;
-        p += (threadIdx.x & 31) * kGroup;
-        if (mine > 0) store8<float, 16>(p, mine < kGroup ? mine : kGroup, v);
+    if constexpr (kWide) {   // the width is a multiple of four
+        if (left > 0) reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        if (left > 4) reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
         store_dealt<false>(p, left, v);
     }
 }
-// The gradient's rows start on 16-byte boundaries wherever kAlign != 0.
-template <int kAlign> constexpr int kGradAlign = kAlign ? 16 : 0;
+
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
+// Room for one slice of a row, and the copy into it and the reading of it.
+template <typename T, bool kWide>
+struct Slot {
+    static constexpr int kBytes = 256 * (int)sizeof(T) + (kWide ? 0 : 16);
+    static __device__ __forceinline__ void copy(char* slot, const T* p, int left) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (kWide) {
+            constexpr int per = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < kGroup / per; ++i)
+                if (i * per < left) copy16(slot + lane * kGroup * (int)sizeof(T) + i * 16, p + i * per);
+        } else {
+            const char* from = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+            const int bytes = (int)(reinterpret_cast<const char*>(p) - from) + left * (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < (kBytes + 511) / 512; ++i)
+                if ((i * 32 + lane) * 16 < bytes) copy16(slot + (i * 32 + lane) * 16, from + (i * 32 + lane) * 16);
+        }
+    }
+    static __device__ __forceinline__ void read(const char* slot, const T* p, int left, float (&v)[kGroup]) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (kWide) {
+            Raw8<T, 16> raw;
+#pragma unroll
+            for (int i = 0; i < Raw8<T, 16>::kPieces; ++i) raw.piece[i] = reinterpret_cast<const uint4*>(slot + lane * kGroup * (int)sizeof(T))[i];
+            raw.unpack(v);
+        } else {
+            const T* e = reinterpret_cast<const T*>(slot + (reinterpret_cast<uintptr_t>(p) & 15)) + lane;
+#pragma unroll
+            for (int k = 0; k < kGroup; ++k) v[k] = k * 32 + lane < left ? to_f32(e[k * 32]) : 0.0f;
+        }
+    }
+};
 
 // One row's columns: its tokens' sum times the factor, written or added to what was there.
-template <bool kAdd, int kAlign>
-__device__ __forceinline__ void emit(float* dst, int left, const float (&sum)[kGroup], const Raw8<float, kGradAlign<kAlign>>& old, float factor) {
-    float g[kGroup], was[kGroup];
-    if (kAdd) old.unpack(was);
+template <bool kAdd, bool kWide>
+__device__ __forceinline__ void emit(float* dst, int left, const float (&sum)[kGroup], const float (&was)[kGroup], float factor) {
+    float g[kGroup];
 #pragma unroll
     for (int c = 0; c < kGroup; ++c) {
         g[c] = __fmul_rn(sum[c], factor);
         if (kAdd) g[c] = __fadd_rn(was[c], g[c]);
     }
-    store_slice<kAlign>(dst, left, g);
+    store_slice<kWide>(dst, left, g);
 }
 
 // A run of one row that crosses units: leaves this unit's partial sum; the last warp to arrive adds them all up.  The
 // run's units are s .. t; a unit's partial sum lies at its odd place where the run starts in it, else at its even one.
-template <bool kAdd, int kAlign>
+template <bool kAdd, bool kWide>
 __device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r, uint32_t row, int unit_id, int slice, int left,
                                   float4 lo, float4 hi) {
     const int lane = threadIdx.x & 31;
@@ -230,7 +261,7 @@ __device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r
     // the partial sums of the units u, the next multiple of step, ... below end, in order
     auto add_up = [&](int u, int step, int end) {
         lo = hi = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
+#pragma unroll 4
         for (; u < end; u = (u / step + 1) * step) {
             const float4 x = __ldcg(at(u)), y = __ldcg(at(u) + 1);
             lo.x += x.x; lo.y += x.y; lo.z += x.z; lo.w += x.w;
@@ -247,31 +278,52 @@ __device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r
         if (!last_at(s, 1, groups)) return;
         add_up(s, kJoin, t + 1);
     }
-    float* dst = a.grad + (int64_t)row * a.width + (int64_t)slice * 256;
-    Raw8<float, kGradAlign<kAlign>> old;
-    if (kAdd) fetch_slice(dst, left, old);
+    float* dst = a.grad + (int64_t)row * a.width + (int64_t)slice * 256 + lane_first<kWide>();
+    float was[kGroup];
+    if (kAdd) {
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) {
+            const int i = kWide ? c : c * 32 + lane;
+            was[c] = i < left ? dst[i] : 0.0f;
+        }
+    }
     const float sum[kGroup] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    emit<kAdd, kAlign>(dst, left, sum, old, a.factor);
+    emit<kAdd, kWide>(dst, left, sum, was, a.factor);
 }
 
-template <bool kAdd, typename T, int kAlign>
+// Rows without tokens, where the gradient is written: one warp for kZeroRows of them.
+template <bool kWide>
+__device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const ReduceArgs& r, int64_t row0) {
+    const int lane = threadIdx.x & 31;
+    const bool empty = lane < kZeroRows && row0 + lane < a.rows && r.row_tab[row0 + lane].y == 0;
+    const float zero[kGroup] = {};
+    for (uint32_t m = __ballot_sync(0xffffffffu, empty); m; m &= m - 1) {
+        float* dst = a.grad + (row0 + __ffs((int)m) - 1) * a.width;
+        for (int64_t col = lane_first<kWide>(); col < a.width; col += 256) store_slice<kWide>(dst + col, (int)min(a.width - col, (int64_t)256), zero);
+    }
+}
+
+template <bool kAdd, typename T, bool kWide>
 __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(const __grid_constant__ EmbedGradArgs a, const __grid_constant__ ReduceArgs r) {
+    // a warp's ring of slots: a token's slice and, where the gradient is added, the row's own
+    constexpr int kSlot = Slot<T, kWide>::kBytes + (kAdd ? Slot<float, kWide>::kBytes : 0);
+    constexpr int kSlots = kRing / kSlot > 8 ? 8 : kRing / kSlot;
+    static_assert(kSlots >= 2, "a slot in use and one on its way");
+    __shared__ __align__(16) char ring_all[kReduceThreads / 32][kSlots * kSlot];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * (kReduceThreads / 32) + (threadIdx.x >> 5);
-    const int64_t reduce_tasks = (int64_t)r.units * r.slices;
-    if (task >= reduce_tasks) {
-        // rows without tokens, where the gradient is written
-        if (kAdd) return;
-        const int64_t row0 = (task - reduce_tasks) * kZeroRows;
-        const bool empty = lane < kZeroRows && row0 + lane < a.rows && r.row_tab[row0 + lane].y == 0;
-        const float zero[kGroup] = {};
-        for (uint32_t m = __ballot_sync(0xffffffffu, empty); m; m &= m - 1) {
-            float* dst = a.grad + (row0 + __ffs((int)m) - 1) * a.width;
-            for (int64_t col = 0; col < a.width; col += 256) store_slice<kAlign>(dst + col, (int)min(a.width - col, (int64_t)256), zero);
+    int64_t block = blockIdx.x;
+    if (!kAdd) {
+        // clearing CTAs are spread evenly among the others: the ones write while the others wait for what they read
+        const int64_t cleared = block * r.clear_blocks / gridDim.x;
+        if ((block + 1) * r.clear_blocks / gridDim.x > cleared) {
+            clear_rows<kWide>(a, r, (cleared * (kReduceThreads / 32) + (threadIdx.x >> 5)) * kZeroRows);
+            return;
         }
-        return;
+        block -= cleared;
     }
+    const int64_t task = block * (kReduceThreads / 32) + (threadIdx.x >> 5);
+    if (task >= (int64_t)r.units * r.slices) return;
     const int unit_id = (int)(task / r.slices), slice = (int)(task - (int64_t)unit_id * r.slices);
     const uint32_t total = *r.total, first = (uint32_t)unit_id * (uint32_t)r.unit;
     if (first >= total) return;
@@ -286,53 +338,61 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
     if (before == __shfl_sync(0xffffffffu, item.x, 0)) closed &= closed - 1;
     if (after == __shfl_sync(0xffffffffu, item.x, have - 1)) closed &= ~(1u << (have - 1));
 
-    const int64_t col = (int64_t)slice * 256;
-    const int left = (int)min(a.width - col, (int64_t)256);
+    const int64_t col = (int64_t)slice * 256 + lane_first<kWide>();
+    const int left = (int)max(min(a.width - col, (int64_t)256), (int64_t)0);
     const uint64_t offset = drop_offset(a.drop);
     const T* dy = static_cast<const T*>(a.dy) + col;
     float* grad = a.grad + col;
-    float sum[kGroup] = {}, front[kGroup];
-    for (int i0 = 0; i0 < have; i0 += kDeep) {
-        Raw8<T, kAlign> v[kDeep];
-        Raw8<float, kGradAlign<kAlign>> old[kDeep];
-        uint32_t pos[kDeep], row[kDeep];
-#pragma unroll
-        for (int k = 0; k < kDeep; ++k) {
-            pos[k] = __shfl_sync(0xffffffffu, item.y, (i0 + k) & 31);
-            row[k] = __shfl_sync(0xffffffffu, item.x, (i0 + k) & 31);
-            if (i0 + k < have) fetch_slice(dy + (int64_t)pos[k] * a.ld_dy, left, v[k]);
-            if (kAdd && (closed >> (i0 + k) & 1u)) fetch_slice(grad + (int64_t)row[k] * a.width, left, old[k]);
+    char* ring = ring_all[threadIdx.x >> 5];
+    auto token = [&](int i) { return dy + (int64_t)__shfl_sync(0xffffffffu, item.y, i) * a.ld_dy; };
+    auto target = [&](int i) { return grad + (int64_t)__shfl_sync(0xffffffffu, item.x, i) * a.width; };
+    auto start = [&](int i, int slot) {      // everything token i needs, as one group of copies (an empty one behind the last)
+        if (i < have) {
+            Slot<T, kWide>::copy(ring + slot * kSlot, token(i), left);
+            if (kAdd && (closed >> i & 1u)) Slot<float, kWide>::copy(ring + slot * kSlot + Slot<T, kWide>::kBytes, target(i), left);
+        }
+        copies_end();
+    };
+    for (int i = 0; i < kSlots; ++i) start(i, i);
+    float sum[kGroup] = {}, front[kGroup] = {};
+    for (int i = 0, slot = 0; i < have; ++i, slot = slot + 1 < kSlots ? slot + 1 : 0) {
+        copies_wait<kSlots - 1>();
+        if (!kWide) __syncwarp();            // other lanes' copies are read
+        float x[kGroup];
+        Slot<T, kWide>::read(ring + slot * kSlot, token(i), left, x);
+        if (a.drop.threshold) {
+            const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i);
+            if constexpr (kWide) drop8<false>(x, a.drop, offset, pos, (uint32_t)slice * 32 + lane);
+            else drop8_dealt<false>(x, a.drop, offset, pos, (uint32_t)slice);
         }
 #pragma unroll
-        for (int k = 0; k < kDeep; ++k) {
-            const int i = i0 + k;
-            if (i >= have) break;
-            float x[kGroup];
-            v[k].unpack(x);
-            if (a.drop.threshold) {
-                if constexpr (kAlign != 0) drop8<false>(x, a.drop, offset, pos[k], (uint32_t)slice * 32 + lane);
-                else drop8_dealt<false>(x, a.drop, offset, pos[k], (uint32_t)slice);
+        for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
+        if (ends >> i & 1u) {
+            if (closed >> i & 1u) {
+                float* dst = target(i);
+                float was[kGroup];
+                if (kAdd) Slot<float, kWide>::read(ring + slot * kSlot + Slot<T, kWide>::kBytes, dst, left, was);
+                emit<kAdd, kWide>(dst, left, sum, was, a.factor);
+            } else if (i == have - 1) {
+                break;                       // the last run goes on in the next unit: its sum stays
+            } else {
+#pragma unroll
+                for (int c = 0; c < kGroup; ++c) front[c] = sum[c];
             }
 #pragma unroll
-            for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
-            if (!(ends >> i & 1u)) continue;
-            if (closed >> i & 1u) emit<kAdd, kAlign>(grad + (int64_t)row[k] * a.width, left, sum, old[k], a.factor);
-            else if (i == have - 1) break;      // (the last run: its sum stays)
-#pragma unroll
-            for (int c = 0; c < kGroup; ++c) {
-                if (!(closed >> i & 1u)) front[c] = sum[c];
-                sum[c] = 0.0f;
-            }
+            for (int c = 0; c < kGroup; ++c) sum[c] = 0.0f;
         }
+        if (!kWide) __syncwarp();            // the slot has been read by all
+        start(i + kSlots, slot);
     }
+    copies_wait<0>();
     // at most two runs cross the unit's ends: its first and its last (or one that is both)
     for (uint32_t open = ends & ~closed; open; open &= open - 1) {
         const int i = __ffs((int)open) - 1;
-        float y[kGroup];
-#pragma unroll
-        for (int c = 0; c < kGroup; ++c) y[c] = i == have - 1 ? sum[c] : front[c];
-        join<kAdd, kAlign>(a, r, __shfl_sync(0xffffffffu, item.x, i), unit_id, slice, left, make_float4(y[0], y[1], y[2], y[3]),
-                           make_float4(y[4], y[5], y[6], y[7]));
+        const bool back = i == have - 1;
+        join<kAdd, kWide>(a, r, __shfl_sync(0xffffffffu, item.x, i), unit_id, slice, left,
+                          back ? make_float4(sum[0], sum[1], sum[2], sum[3]) : make_float4(front[0], front[1], front[2], front[3]),
+                          back ? make_float4(sum[4], sum[5], sum[6], sum[7]) : make_float4(front[4], front[5], front[6], front[7]));
     }
 }
 
@@ -385,8 +445,9 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     // -1, and any other number that is no row, leaves nothing out
     const uint32_t skip = a.skip_id >= 0 && a.skip_id < a.rows ? (uint32_t)a.skip_id : kNoRow;
     const GradWs w = grad_ws(a.n, a.rows, a.width);
-    const int64_t tasks = (int64_t)w.units * w.slices + (a.accumulate ? 0 : (a.rows + kZeroRows - 1) / kZeroRows);
-    const int64_t blocks = (tasks + kReduceThreads / 32 - 1) / (kReduceThreads / 32);
+    constexpr int64_t kWarps = kReduceThreads / 32;
+    const int64_t clear_blocks = a.accumulate ? 0 : (a.rows + kZeroRows * kWarps - 1) / (kZeroRows * kWarps);
+    const int64_t blocks = ((int64_t)w.units * w.slices + kWarps - 1) / kWarps + clear_blocks;
     if (blocks > 0x7fffffff) return DEFT_ERR_TOO_LARGE;
     GroupOut out{reinterpret_cast<uint2*>(a.ws + w.sorted), reinterpret_cast<uint2*>(a.ws + w.row_tab), reinterpret_cast<uint32_t*>(a.ws + w.total),
                  reinterpret_cast<uint32_t*>(a.ws + w.arrived), w.arrived_n};
@@ -399,7 +460,7 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     };
     const deft_status s = id_bytes == 8 ? group(int64_t{}) : group(int32_t{});
     if (s != DEFT_OK) return s;
-    const ReduceArgs r{out.sorted, out.row_tab, out.total, reinterpret_cast<float*>(a.ws + w.partial), out.arrived, w.unit, w.units, w.slices};
+    const ReduceArgs r{out.sorted, out.row_tab, out.total, reinterpret_cast<float*>(a.ws + w.partial), out.arrived, w.unit, w.units, w.slices, clear_blocks};
     // The second kernel's CTAs take their places while the first still runs and wait there for its end.
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -410,15 +471,13 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     cfg.stream = stream;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    const int align = row_align(a.grad, a.width, sizeof(float)) == 16 && a.n ? row_align(a.dy, a.ld_dy, type_bytes(dy_type)) : 0;
-    return with_type(dy_type, [&](auto t) {
-        return with_align(align, [&](auto al) -> deft_status {
-            using T = decltype(t);
-            constexpr int kAlign = decltype(al)::value;
-            DEFT_CUDA_TRY(a.accumulate ? cudaLaunchKernelEx(&cfg, k_rows_reduce<true, T, kAlign>, a, r)
-                                       : cudaLaunchKernelEx(&cfg, k_rows_reduce<false, T, kAlign>, a, r));
-            return DEFT_OK;
-        });
+    const bool wide = row_align(a.grad, a.width, sizeof(float)) == 16 && (a.n == 0 || row_align(a.dy, a.ld_dy, type_bytes(dy_type)) == 16);
+    return with_type(dy_type, [&](auto t) -> deft_status {
+        using T = decltype(t);
+        auto run = [&](auto kernel) { return cudaLaunchKernelEx(&cfg, kernel, a, r); };
+        if (wide) DEFT_CUDA_TRY(a.accumulate ? run(k_rows_reduce<true, T, true>) : run(k_rows_reduce<false, T, true>));
+        else DEFT_CUDA_TRY(a.accumulate ? run(k_rows_reduce<true, T, false>) : run(k_rows_reduce<false, T, false>));
+        return DEFT_OK;
     });
 }
 
