@@ -189,15 +189,33 @@ k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
                     slot = ss->layer[0] == l ? 0 : (ss->layer[1] == l ? 1 : -1);
                     if (slot >= 0) cut = ss->cut[slot];
                 }
-                for (int64_t i = ps + threadIdx.x; i < pe; i += kNormThreads) {
-                    float x = e[i];
-                    if (kHasGrad && (!kParts || in_parts(ap, i, i + 1) == 0)) {
-                        x = __fadd_rn(x, __ldg(g + i));
-                        e[i] = x;
+                // Several loads of each vector are on their way before the first is used (these tiles decide how long a
+                // small vector takes); the squares are added in the order of the elements.  Not where the pass stages:
+                // it has 40 registers, and its vectors are large.
+                constexpr int kAhead = kStage ? 1 : 8;
+                const int piece_part = kParts && part ? in_parts(ap, ps, pe) : 0;
+                auto added = [&](int64_t i) { return kParts && (piece_part == 1 || (piece_part == 2 && in_parts(ap, i, i + 1))); };
+                for (int64_t i0 = ps + threadIdx.x; i0 < pe; i0 += kAhead * kNormThreads) {
+                    float xs[kAhead], gs[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int64_t i = i0 + u * kNormThreads;
+                        xs[u] = i < pe ? e[i] : 0.0f;
+                        if (kHasGrad) gs[u] = i < pe && !added(i) ? __ldg(g + i) : 0.0f;
                     }
-                    if (kStage && cut != 0xffffffffu && key_of(__float_as_uint(x)) >= cut)
-                        stage_append(ss, slot, lo, i, __float_as_uint(x));
-                    acc += (double)x * (double)x;
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int64_t i = i0 + u * kNormThreads;
+                        if (i >= pe) break;
+                        float x = xs[u];
+                        if (kHasGrad && !added(i)) {
+                            x = __fadd_rn(x, gs[u]);
+                            e[i] = x;
+                        }
+                        if (kStage && cut != 0xffffffffu && key_of(__float_as_uint(x)) >= cut)
+                            stage_append(ss, slot, lo, i, __float_as_uint(x));
+                        acc += (double)x * (double)x;
+                    }
                 }
                 const double tot = block_sum(acc, sh);
                 if (threadIdx.x == 0 && pe > ps) partial[t + l] = tot;
@@ -293,7 +311,13 @@ k_norm_finalize(const int64_t* __restrict__ ls, int L, const double* __restrict_
     double acc = 0.0;
     if (e > s) {
         const int64_t t0 = s / kTileA, t1 = (e - 1) / kTileA;
-        for (int64_t t = t0 + threadIdx.x; t <= t1; t += kNormThreads) acc += partial[t + l];
+        for (int64_t t = t0 + threadIdx.x; t <= t1; t += 8 * kNormThreads) {   // (eight loads ahead of the additions)
+            double x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = t + u * kNormThreads <= t1 ? partial[t + u * kNormThreads + l] : 0.0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) acc += x[u];
+        }
     }
     const double tot = block_sum(acc, sh);
     if (threadIdx.x == 0) {

@@ -13,7 +13,8 @@ constexpr int kRowThreads = 256;
 constexpr int kInFlight = 16;    // words a thread that takes several rows has in flight
 constexpr int kMostDeep = 4;     // rows it has in flight, when a row's group is four words
 constexpr int kMostEach = 16;    // rows it takes in all
-constexpr int kRounds = 8;       // rounds of CTAs a launch has at least before threads take several rows
+constexpr int kRounds = 8;       // rounds of CTAs a launch has at least before threads take several rows ...
+constexpr int kEmbedRounds = 3;  // ... fewer where a thread waits for an id before it can load a row
 constexpr int kBlocksOne = 8;    // CTAs an SM holds where threads take one row (32 registers) ...
 constexpr int kBlocksDeep = 4;   // ... and where they take several (64)
 
@@ -165,10 +166,10 @@ __global__ void __launch_bounds__(kRowThreads, kDeep == 1 ? kBlocksOne : kBlocks
 // Threads take up to kMostEach rows each, as many as leave every SM several rounds of CTAs (the last round is rarely
 // full).  pos_rows != 0: `stride` becomes a multiple of it where that is possible, so that a thread reads its position
 // row once for all its tokens.
-inline RowSplit row_split(int64_t rows, int64_t cols, int align, int64_t pos_rows, unsigned* blocks) {
+inline RowSplit row_split(int64_t rows, int64_t cols, int align, int rounds, int64_t pos_rows, unsigned* blocks) {
     const int64_t units = align ? (cols + kGroup - 1) / kGroup : (cols + 255) / 256;
     const int64_t per_block = align ? kRowThreads : kRowThreads / 32;
-    int64_t each = rows * units / ((int64_t)sm_count() * kBlocksDeep * per_block * kRounds);
+    int64_t each = rows * units / ((int64_t)sm_count() * kBlocksDeep * per_block * rounds);
     each = each < 1 ? 1 : (each > kMostEach ? kMostEach : each);
     int64_t stride = (rows + each - 1) / each;
     if (pos_rows && each > 1 && pos_rows < rows) stride = (stride + pos_rows - 1) / pos_rows * pos_rows;
@@ -190,7 +191,7 @@ deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int i
         if (ap < align) align = ap;
     }
     unsigned blocks;
-    const RowSplit split = row_split(a.n, a.width, align, a.pos ? a.pos_rows : 0, &blocks);
+    const RowSplit split = row_split(a.n, a.width, align, kEmbedRounds, a.pos ? a.pos_rows : 0, &blocks);
     // a token's number is below 2^31: more position rows than that are never wrapped around
     const FastDiv pos_rows = fast_div((uint32_t)(a.pos_rows < 0x7fffffff ? a.pos_rows : 0x7fffffff));
     return with_type(table_type, [&](auto w) {
@@ -223,7 +224,7 @@ deft_status launch_dropout(const DropoutArgs& a, int x_type, int y_type, cudaStr
         if (aa < align) align = aa;
     }
     unsigned blocks;
-    const RowSplit split = row_split(a.rows, a.cols, align, 0, &blocks);
+    const RowSplit split = row_split(a.rows, a.cols, align, kRounds, 0, &blocks);
     return with_type(x_type, [&](auto x) {
         return with_type(y_type, [&](auto y) {
             return with_align(align, [&](auto al) -> deft_status {

@@ -48,8 +48,14 @@ __device__ __forceinline__ uint4 drop_words(const DropArgs& d, uint64_t offset, 
     return philox10(make_uint4(group, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.keys);
 }
 
-// Applies a group's mask to v: dropped elements become +0 whatever they were.  The even column goes by a word's low
-// half, the odd one by its high half.
+// Whether the even (low half) and the odd column (high half) of a word are kept: what lies below a half does not change
+// how it compares with the threshold.
+__device__ __forceinline__ void kept2(uint32_t word, uint32_t threshold, bool& even, bool& odd) {
+    even = (word << 16) >= threshold;
+    odd = word >= threshold;
+}
+
+// Applies a group's mask to v: dropped elements become +0 whatever they were.
 template <bool kScale>
 __device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
     const uint4 w = drop_words(d, offset, row, group);
@@ -57,8 +63,10 @@ __device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uin
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float a = kScale ? v[2 * i] * d.gain : v[2 * i], b = kScale ? v[2 * i + 1] * d.gain : v[2 * i + 1];
-        v[2 * i] = (u[i] << 16) >= d.threshold ? a : 0.0f;
-        v[2 * i + 1] = u[i] >= d.threshold ? b : 0.0f;
+        bool even, odd;
+        kept2(u[i], d.threshold, even, odd);
+        v[2 * i] = even ? a : 0.0f;
+        v[2 * i + 1] = odd ? b : 0.0f;
     }
 }
 
@@ -71,8 +79,11 @@ __device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& 
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
     uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        bits |= ((u[i] << 16) >= d.threshold ? 1u << (2 * i) : 0u) | (u[i] >= d.threshold ? 2u << (2 * i) : 0u);
+    for (int i = 0; i < 4; ++i) {
+        bool even, odd;
+        kept2(u[i], d.threshold, even, odd);
+        bits |= (even ? 1u << (2 * i) : 0u) | (odd ? 2u << (2 * i) : 0u);
+    }
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) {
         const uint32_t there = __shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3));
@@ -140,6 +151,12 @@ __device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]
 #pragma unroll
     for (int i = 0; i < kGroup; ++i)
         if (i < count) p[i] = from_f32<T>(v[i]);
+}
+
+// Eight fp32 values to a 32-byte boundary.
+__device__ __forceinline__ void store32(float* p, const float (&v)[kGroup]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+                 "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
 // A slice of 256 columns dealt out one by one: lane l has the columns 32 k + l, so that loads and stores of a matrix whose

@@ -181,10 +181,12 @@ def _dp(t, dtype=None):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+def _stream(stream, device: Optional[int] = None) -> ctypes.c_void_p:
+    """The handle of `stream`, or of the current stream of the device (the current one by default)."""
+    if stream is None:   # (the handle alone: building a Stream object costs more than the call it is for)
+        import torch
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device))
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 # ------------------------------------------------------------------------------------------
@@ -296,8 +298,12 @@ def deft_layer_norms(resid_acc, grad, layer_start_d, norms_d, ws, stream=None) -
                                   _dp(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
-def _parts(parts) -> np.ndarray:
-    return _np(parts, np.int64).reshape(-1, 2) if len(parts) else np.empty((0, 2), dtype=np.int64)
+def _parts(parts):
+    """(begin, end) pairs as a host array for the library, and their number."""
+    flat = [int(x) for part in parts for x in part]
+    if len(flat) != 2 * len(parts):
+        raise ValueError("parts: (begin, end) pairs")
+    return (ctypes.c_int64 * max(1, len(flat)))(*flat), len(parts)
 
 
 def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, stream=None) -> None:
@@ -309,9 +315,9 @@ def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, st
         raise ValueError("grad and resid_acc differ in length")
     if norms_d.numel() < L:
         raise ValueError("norms_d too small")
-    pt = _parts(parts)
+    pt, n_parts = _parts(parts)
     _check("deft_layer_norms_part",
-           lib().deft_layer_norms_part(_dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g, _hp(pt), len(pt),
+           lib().deft_layer_norms_part(_dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g, pt, n_parts,
                                        _dp(layer_start_d, torch.int64), L, _dp(norms_d, torch.float64),
                                        _dp(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
@@ -642,7 +648,7 @@ def _matrix(t, name: str) -> Tuple[int, int, int]:
     """(rows, columns, pitch) of a tensor whose last dimension is the row and whose others are one list of rows."""
     if t.dim() == 0:
         raise ValueError("%s: at least one dimension expected" % name)
-    cols = t.shape[-1]
+    cols = t.size(-1)
     if t.is_contiguous():
         return (t.numel() // cols if cols else 0), cols, cols
     lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
@@ -654,24 +660,26 @@ def _matrix(t, name: str) -> Tuple[int, int, int]:
     return t.numel() // cols, cols, pitch
 
 
-class _OnDevice:
-    """Makes `device` current for a call whose tensors are not on the current one; checks that they share a device."""
+def _device(*tensors) -> int:
+    """The one CUDA device that the tensors (None: not given) lie on."""
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != index or index < 0):
+            raise ValueError("expected CUDA tensors on one device")
+    return index
 
-    def __init__(self, *tensors):
-        import torch
-        self.index = tensors[0].device.index
-        for t in tensors:
-            if t is not None and (not t.is_cuda or t.device.index != self.index):
-                raise ValueError("expected CUDA tensors on one device")
-        self.guard = None if torch.cuda.current_device() == self.index else torch.cuda.device(self.index)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(name: str, device: int, *args) -> None:
+    """Calls the library with `device` current."""
+    import torch
+    fn = getattr(_lib or lib(), name)
+    if torch._C._cuda_getDevice() == device:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args)
+    if status:
+        _check(name, status)
 
 
 def _ids(ids) -> int:
@@ -704,11 +712,10 @@ def deft_embed(table, ids, out, scale: float = 1.0, pos=None, p: float = 0.0, se
         pos_rows, w, ld_pos = _matrix(pos, "pos")
         if w != width or pos.dtype != table.dtype:
             raise ValueError("pos: rows like the table's expected")
-    with _OnDevice(out, table, ids, pos, offset_d):
-        _check("deft_embed",
-               lib().deft_embed(table.data_ptr(), _type(table), rows, width, ld_table, ids.data_ptr(), _ids(ids), n, scale,
-                                None if pos is None else pos.data_ptr(), pos_rows, ld_pos, p, seed & _U64, offset & _U64,
-                                _offset(offset_d), out.data_ptr(), _type(out), ld_out, _stream(stream)))
+    dev = _device(out, table, ids, pos, offset_d)
+    _call("deft_embed", dev, table.data_ptr(), _type(table), rows, width, ld_table, ids.data_ptr(), _ids(ids), n, scale,
+          None if pos is None else pos.data_ptr(), pos_rows, ld_pos, p, seed & _U64, offset & _U64, _offset(offset_d), out.data_ptr(),
+          _type(out), ld_out, _stream(stream, dev))
 
 
 def deft_embed_workspace_bytes(n: int, rows: int, width: int) -> int:
@@ -737,11 +744,10 @@ def deft_embed_grad(grad_out, ids, grad, ws, accumulate: bool = False, skip_id: 
         n, w, ld = 0, width, width
     if w != width or ids.numel() != n:
         raise ValueError("grad_out, ids and grad disagree")
-    with _OnDevice(grad, grad_out, ids, ws, offset_d):
-        _check("deft_embed_grad",
-               lib().deft_embed_grad(grad_out.data_ptr(), _type(grad_out), ld, ids.data_ptr(), _ids(ids), n, rows, width, skip_id,
-                                     scale, p, seed & _U64, offset & _U64, _offset(offset_d), grad.data_ptr(), 1 if accumulate else 0,
-                                     ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+    dev = _device(grad, grad_out, ids, ws, offset_d)
+    _call("deft_embed_grad", dev, grad_out.data_ptr(), _type(grad_out), ld, ids.data_ptr(), _ids(ids), n, rows, width, skip_id, scale, p,
+          seed & _U64, offset & _U64, _offset(offset_d), grad.data_ptr(), 1 if accumulate else 0, ws.data_ptr(),
+          ws.numel() * ws.element_size(), _stream(stream, dev))
 
 
 def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0, offset_d=None, stream=None) -> None:
@@ -752,7 +758,6 @@ def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0,
         raise ValueError("x, y and add disagree")
     ld_y = _matrix(y, "y")[2]
     ld_add = 0 if add is None else _matrix(add, "add")[2]
-    with _OnDevice(y, x, add, offset_d):
-        _check("deft_dropout",
-               lib().deft_dropout(x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(),
-                                  _type(y), ld_y, rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d), _stream(stream)))
+    dev = _device(y, x, add, offset_d)
+    _call("deft_dropout", dev, x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(), _type(y), ld_y,
+          rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d), _stream(stream, dev))

@@ -137,4 +137,4 @@ def test_matrix_shapes_of_the_binding():
     with pytest.raises(ValueError):
         deft._offset(torch.zeros(1))
     with pytest.raises(ValueError):
-        deft._OnDevice(torch.zeros(1))
+        deft._device(torch.zeros(1))
