@@ -72,8 +72,8 @@ __device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uin
 
 // The same where a warp's 256 columns are dealt out one by one (lane l has the columns 32 k + l): every lane draws the
 // eight bits of its own group and fetches those of its columns from the lanes that have them.
-template <bool kScale>
-__device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
+template <typename F>
+__device__ __forceinline__ void for_kept_dealt(const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice, F&& f) {
     const int lane = threadIdx.x & 31;
     const uint4 w = drop_words(d, offset, row, slice * 32 + lane);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -85,11 +85,27 @@ __device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& 
         bits |= (even ? 1u << (2 * i) : 0u) | (odd ? 2u << (2 * i) : 0u);
     }
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
-        const uint32_t there = __shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3));
-        const float x = kScale ? v[k] * d.gain : v[k];
-        v[k] = there >> (lane & 7) & 1u ? x : 0.0f;
+    for (int k = 0; k < kGroup; ++k) f(k, (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7) & 1u) != 0);
+}
+template <bool kScale>
+__device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
+    for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { v[k] = kept ? (kScale ? v[k] * d.gain : v[k]) : 0.0f; });
+}
+
+// Adds what the mask keeps of v to sum.
+__device__ __forceinline__ void add_kept8(float (&sum)[kGroup], const float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
+    const uint4 w = drop_words(d, offset, row, group);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bool even, odd;
+        kept2(u[i], d.threshold, even, odd);
+        if (even) sum[2 * i] += v[2 * i];
+        if (odd) sum[2 * i + 1] += v[2 * i + 1];
     }
+}
+__device__ __forceinline__ void add_kept8_dealt(float (&sum)[kGroup], const float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
+    for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { if (kept) sum[k] += v[k]; });
 }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }

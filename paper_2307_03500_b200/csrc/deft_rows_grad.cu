@@ -339,45 +339,53 @@ __device__ __forceinline__ void emit(float* dst, int left, const float (&sum)[kG
     store_slice<kWide>(dst, left, g);
 }
 
-// A run of one row that crosses units: leaves this unit's partial sum; the last warp to arrive adds them all up.  The
-// run's units are s .. t; a unit's partial sum lies at its odd place where the run starts in it, else at its even one.
+// A run that crosses units leaves a partial sum in each: at the unit's odd place where the run starts in it, else at its
+// even one.
+__device__ __forceinline__ float4* partial_at(const ReduceArgs& r, int unit, bool starts, int slice) {
+    return reinterpret_cast<float4*>(r.partial + (size_t)(2 * unit + (starts ? 1 : 0)) * (size_t)r.slices * 256 + (size_t)slice * 256 +
+                                     (threadIdx.x & 31) * kGroup);
+}
+__device__ __forceinline__ void leave(float4* at, const float (&sum)[kGroup]) {
+    at[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    at[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+}
+
+// The warp has left its unit's partial sum of a run: the last one to arrive adds them all up.
 template <bool kAdd, bool kWide>
-__device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r, uint32_t row, int unit_id, int slice, int left,
-                                  float4 lo, float4 hi) {
+__device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r, uint32_t row, int unit_id, int slice, int left) {
     const int lane = threadIdx.x & 31;
     const uint2 tab = r.row_tab[row];
-    const int s = (int)(tab.x / (uint32_t)r.unit), t = (int)((tab.x + tab.y - 1) / (uint32_t)r.unit);
-    const size_t pitch = (size_t)r.slices * 256;
-    auto place = [&](int u) { return (size_t)(2 * u + (u == s ? 1 : 0)); };
-    auto at = [&](int u) { return reinterpret_cast<float4*>(r.partial + place(u) * pitch + (size_t)slice * 256 + lane * kGroup); };
-    auto leave = [&](int u) { at(u)[0] = lo; at(u)[1] = hi; };
+    const int s = (int)(tab.x / (uint32_t)r.unit), t = (int)((tab.x + tab.y - 1) / (uint32_t)r.unit);   // the run's units
+    float sum[kGroup];
     // true for the last of `expected` warps to arrive at a unit's place
     auto last_at = [&](int u, int level, int expected) {
         __threadfence();
         __syncwarp();
         uint32_t n = 0;
-        if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + place(u)) * r.slices + slice, 1u);
+        if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + 2 * u + (u == s ? 1 : 0)) * r.slices + slice, 1u);
         n = __shfl_sync(0xffffffffu, n, 0);
         __threadfence();
         return n == (uint32_t)(expected - 1);
     };
     // the partial sums of the units u, the next multiple of step, ... below end, in order
     auto add_up = [&](int u, int step, int end) {
-        lo = hi = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
 #pragma unroll 4
         for (; u < end; u = (u / step + 1) * step) {
-            const float4 x = __ldcg(at(u)), y = __ldcg(at(u) + 1);
+            const float4* at = partial_at(r, u, u == s, slice);
+            const float4 x = __ldcg(at), y = __ldcg(at + 1);
             lo.x += x.x; lo.y += x.y; lo.z += x.z; lo.w += x.w;
             hi.x += y.x; hi.y += y.y; hi.z += y.z; hi.w += y.w;
         }
+        sum[0] = lo.x; sum[1] = lo.y; sum[2] = lo.z; sum[3] = lo.w;
+        sum[4] = hi.x; sum[5] = hi.y; sum[6] = hi.z; sum[7] = hi.w;
     };
-    leave(unit_id);
     const int u0 = max(s, unit_id / kJoin * kJoin), u1 = min(t + 1, (unit_id / kJoin + 1) * kJoin);
     const int groups = t / kJoin - s / kJoin + 1;
     if (!last_at(u0, 0, u1 - u0)) return;
     add_up(u0, 1, u1);
     if (groups > 1) {
-        leave(u0);
+        leave(partial_at(r, u0, u0 == s, slice), sum);
         if (!last_at(s, 1, groups)) return;
         add_up(s, kJoin, t + 1);
     }
@@ -390,7 +398,6 @@ __device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r
             was[c] = i < left ? dst[i] : 0.0f;
         }
     }
-    const float sum[kGroup] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     emit<kAdd, kWide>(dst, left, sum, was, a.factor);
 }
 
@@ -440,7 +447,8 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
     // where runs end, and which of them lie inside the unit
     const uint32_t ends = __ballot_sync(0xffffffffu, lane < have && (lane == have - 1 || next_row != item.x));
     uint32_t closed = ends;
-    if (before == __shfl_sync(0xffffffffu, item.x, 0)) closed &= closed - 1;
+    const bool from_before = before == __shfl_sync(0xffffffffu, item.x, 0);
+    if (from_before) closed &= closed - 1;
     if (after == __shfl_sync(0xffffffffu, item.x, have - 1)) closed &= ~(1u << (have - 1));
 
     const int64_t col = (int64_t)slice * 256 + lane_first<kWide>();
@@ -459,7 +467,7 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
         copies_end();
     };
     for (int i = 0; i < kSlots; ++i) start(i, i);
-    float sum[kGroup] = {}, front[kGroup] = {};
+    float sum[kGroup] = {};
     for (int i = 0, slot = 0; i < have; ++i, slot = slot + 1 < kSlots ? slot + 1 : 0) {
         copies_wait<kSlots - 1>();
         if (!kWide) __syncwarp();            // other lanes' copies are read
@@ -467,22 +475,20 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
         const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i);
         Slot<T, kWide>::read(ring + slot * kSlot, (uint32_t)reinterpret_cast<uintptr_t>(dy) + pos * (uint32_t)a.ld_dy * (uint32_t)sizeof(T), left, x);
         if (a.drop.threshold) {
-            if constexpr (kWide) drop8<false>(x, a.drop, offset, pos, (uint32_t)slice * 32 + lane);
-            else drop8_dealt<false>(x, a.drop, offset, pos, (uint32_t)slice);
-        }
+            if constexpr (kWide) add_kept8(sum, x, a.drop, offset, pos, (uint32_t)slice * 32 + lane);
+            else add_kept8_dealt(sum, x, a.drop, offset, pos, (uint32_t)slice);
+        } else {
 #pragma unroll
-        for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
+            for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
+        }
         if (ends >> i & 1u) {
             if (closed >> i & 1u) {
                 float* dst = target(i);
                 float was[kGroup];
                 if (kAdd) Slot<float, kWide>::read(ring + slot * kSlot + Slot<T, kWide>::kBytes, (uint32_t)reinterpret_cast<uintptr_t>(dst), left, was);
                 emit<kAdd, kWide>(dst, left, sum, was, a.factor);
-            } else if (i == have - 1) {
-                break;                       // the last run goes on in the next unit: its sum stays
-            } else {
-#pragma unroll
-                for (int c = 0; c < kGroup; ++c) front[c] = sum[c];
+            } else {                         // goes on in the next unit (and starts here unless it is the first, too), or began before
+                leave(partial_at(r, unit_id, i == have - 1 && !((ends & ((1u << i) - 1u)) == 0 && from_before), slice), sum);
             }
 #pragma unroll
             for (int c = 0; c < kGroup; ++c) sum[c] = 0.0f;
@@ -492,13 +498,8 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
     }
     copies_wait<0>();
     // at most two runs cross the unit's ends: its first and its last (or one that is both)
-    for (uint32_t open = ends & ~closed; open; open &= open - 1) {
-        const int i = __ffs((int)open) - 1;
-        const bool back = i == have - 1;
-        join<kAdd, kWide>(a, r, __shfl_sync(0xffffffffu, item.x, i), unit_id, slice, left,
-                          back ? make_float4(sum[0], sum[1], sum[2], sum[3]) : make_float4(front[0], front[1], front[2], front[3]),
-                          back ? make_float4(sum[4], sum[5], sum[6], sum[7]) : make_float4(front[4], front[5], front[6], front[7]));
-    }
+    for (uint32_t open = ends & ~closed; open; open &= open - 1)
+        join<kAdd, kWide>(a, r, __shfl_sync(0xffffffffu, item.x, __ffs((int)open) - 1), unit_id, slice, left);
 }
 
 // Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls.
