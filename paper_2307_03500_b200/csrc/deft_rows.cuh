@@ -92,22 +92,6 @@ __device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& 
     for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { v[k] = kept ? (kScale ? v[k] * d.gain : v[k]) : 0.0f; });
 }
 
-// Adds what the mask keeps of v to sum.
-__device__ __forceinline__ void add_kept8(float (&sum)[kGroup], const float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
-    const uint4 w = drop_words(d, offset, row, group);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bool even, odd;
-        kept2(u[i], d.threshold, even, odd);
-        if (even) sum[2 * i] += v[2 * i];
-        if (odd) sum[2 * i + 1] += v[2 * i + 1];
-    }
-}
-__device__ __forceinline__ void add_kept8_dealt(float (&sum)[kGroup], const float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
-    for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { if (kept) sum[k] += v[k]; });
-}
-
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
@@ -115,6 +99,17 @@ template <typename T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+// sum + x, x converted exactly: one instruction, without unpacking the 16-bit type first.
+__device__ __forceinline__ float add_elem(float sum, float x) { return sum + x; }
+__device__ __forceinline__ float add_elem(float sum, __nv_bfloat16 x) {
+    asm("add.f32.bf16 %0, %1, %0;" : "+f"(sum) : "h"(__bfloat16_as_ushort(x)));
+    return sum;
+}
+__device__ __forceinline__ float add_elem(float sum, __half x) {
+    asm("add.f32.f16 %0, %1, %0;" : "+f"(sum) : "h"(__half_as_ushort(x)));
+    return sum;
+}
 
 template <int kBytes> struct Piece;
 template <> struct Piece<16> { using type = uint4; };

@@ -312,17 +312,18 @@ struct Slot {
                 if ((i * 32 + lane) * 16 < bytes) copy16(slot + (i * 32 + lane) * 16, from + (i * 32 + lane) * 16);
         }
     }
-    static __device__ __forceinline__ void read(const char* slot, uint32_t at, int left, float (&v)[kGroup]) {   // at: the slice's address
+    static __device__ __forceinline__ void read(const char* slot, uint32_t at, int left, T (&v)[kGroup]) {   // at: the slice's address
         const int lane = threadIdx.x & 31;
         if constexpr (kWide) {
             Raw8<T, 16> raw;
 #pragma unroll
             for (int i = 0; i < Raw8<T, 16>::kPieces; ++i) raw.piece[i] = *reinterpret_cast<const uint4*>(slot + (i * 32 + lane) * 16);
-            raw.unpack(v);
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) v[i] = reinterpret_cast<const T*>(raw.piece)[i];
         } else {
             const T* e = reinterpret_cast<const T*>(slot + (at & 15u)) + lane;
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k) v[k] = k * 32 + lane < left ? to_f32(e[k * 32]) : 0.0f;
+            for (int k = 0; k < kGroup; ++k) v[k] = k * 32 + lane < left ? e[k * 32] : from_f32<T>(0.0f);
         }
     }
 };
@@ -473,15 +474,26 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
     for (int i = 0, slot = 0; i < have; ++i, slot = slot + 1 < kSlots ? slot + 1 : 0) {
         copies_wait<kSlots - 1>();
         if (!kWide) __syncwarp();            // other lanes' copies are read
-        float x[kGroup];
+        T x[kGroup];
         const uint32_t pos = __shfl_sync(0xffffffffu, item.y, i);
         Slot<T, kWide>::read(ring + slot * kSlot, (uint32_t)reinterpret_cast<uintptr_t>(dy) + pos * (uint32_t)a.ld_dy * (uint32_t)sizeof(T), left, x);
         if (a.drop.threshold) {
-            if constexpr (kWide) add_kept8(sum, x, a.drop, offset, pos, (uint32_t)slice * 32 + lane);
-            else add_kept8_dealt(sum, x, a.drop, offset, pos, (uint32_t)slice);
+            if constexpr (kWide) {
+                const uint4 w = drop_words(a.drop, offset, pos, (uint32_t)slice * 32 + lane);
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    bool even, odd;
+                    kept2(u[c], a.drop.threshold, even, odd);
+                    if (even) sum[2 * c] = add_elem(sum[2 * c], x[2 * c]);
+                    if (odd) sum[2 * c + 1] = add_elem(sum[2 * c + 1], x[2 * c + 1]);
+                }
+            } else {
+                for_kept_dealt(a.drop, offset, pos, (uint32_t)slice, [&](int c, bool kept) { if (kept) sum[c] = add_elem(sum[c], x[c]); });
+            }
         } else {
 #pragma unroll
-            for (int c = 0; c < kGroup; ++c) sum[c] += x[c];
+            for (int c = 0; c < kGroup; ++c) sum[c] = add_elem(sum[c], x[c]);
         }
         if (ends >> i & 1u) {
             if (closed >> i & 1u) {
