@@ -45,6 +45,9 @@ struct Place {
     }
 };
 
+// What an id outside the table is looked up in: a share of a row at most.
+__device__ __align__(16) const char g_zeros[256 * sizeof(float)] = {};
+
 // kAlign != 0: eight columns of this thread; else this lane's share of the slice.  kFull: none of the group's (slice's)
 // columns lies beyond the row's end; left = columns from the first one to the end.
 template <bool kFull, typename T, int kAlign>
@@ -72,37 +75,34 @@ __device__ __forceinline__ void embed_rows(const EmbedArgs& a, const RowSplit& s
     const Id* ids = static_cast<const Id*>(a.ids);
     Raw8<TW, kAlign> q;
     if (kPos) fetch_share<kFull>(pos + (int64_t)(at.row - pos_rows.div(at.row) * pos_rows.d) * a.ld_pos, left, q);
-    for (uint32_t t0 = at.row; t0 < split.rows; t0 += kDeep * split.stride) {
-        Raw8<TW, kAlign> w[kDeep];
-        int64_t id[kDeep];
+    uint32_t next[kDeep];                // the table rows of the next turn's tokens
+    auto look = [&](uint32_t t0) {
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
             const uint32_t t = t0 + k * split.stride;
-            id[k] = t < split.rows ? (int64_t)__ldg(ids + t) : -1;
+            next[k] = t < split.rows ? row_of(__ldg(ids + t), (uint32_t)a.rows, kNoRow) : kNoRow;
         }
+    };
+    look(at.row);
+    for (uint32_t t0 = at.row; t0 < split.rows; t0 += kDeep * split.stride) {
+        Raw8<TW, kAlign> w[kDeep];
 #pragma unroll
         for (int k = 0; k < kDeep; ++k)
-            if (id[k] >= 0 && id[k] < a.rows) fetch_share<kFull>(table + id[k] * a.ld_table, left, w[k]);
+            fetch_share<kFull>(next[k] != kNoRow ? table + next[k] * a.ld_table : reinterpret_cast<const TW*>(g_zeros), left, w[k]);
+        if (kDeep > 1) look(t0 + kDeep * split.stride);
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
             const uint32_t t = t0 + k * split.stride;
             if (t >= split.rows) break;
             float v[kGroup];
             w[k].unpack(v);
-            if (id[k] < 0 || id[k] >= a.rows) {      // a row outside the table
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i) v[i] = 0.0f;
-            }
             if (a.scale != 1.0f) {
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) v[i] = __fmul_rn(v[i], a.scale);
             }
             if (kPos) {
-                float x[kGroup];
                 if (!split.same_pos) fetch_share<kFull>(pos + (int64_t)(t - pos_rows.div(t) * pos_rows.d) * a.ld_pos, left, q);
-                q.unpack(x);
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], x[i]);
+                q.add_to(v);
             }
             if (a.drop.threshold) drop_share<kAlign>(v, a.drop, offset, t, at.unit);
             store_share<kFull, TO, kAlign>(out + (int64_t)t * a.ld_out, left, v);
@@ -143,12 +143,7 @@ __device__ __forceinline__ void dropout_rows(const DropoutArgs& a, const RowSpli
             float v[kGroup];
             w[k].unpack(v);
             if (a.drop.threshold) drop_share<kAlign>(v, a.drop, offset, r, at.unit);
-            if (kAdd) {
-                float z[kGroup];
-                q[k].unpack(z);
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i) v[i] = __fadd_rn(v[i], z[i]);
-            }
+            if (kAdd) q[k].add_to(v);
             store_share<kFull, TY, kAlign>(y + (int64_t)r * a.ld_y, left, v);
         }
     }

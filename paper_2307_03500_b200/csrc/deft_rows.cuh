@@ -130,6 +130,11 @@ struct Raw8 {
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) v[i] = to_f32(e[i]);
     }
+    __device__ __forceinline__ void add_to(float (&v)[kGroup]) const {
+        const T* e = reinterpret_cast<const T*>(piece);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) v[i] = add_elem(v[i], e[i]);
+    }
 };
 
 // A group of eight consecutive elements of which the first `left` (or more) belong to the row.  kAlign: 16 or 8 when
@@ -199,6 +204,15 @@ inline FastDiv fast_div(uint32_t d) {
     while ((1ull << log) < d) ++log;
     const uint32_t p = 31 + log;
     return FastDiv{d, (uint32_t)(((1ull << p) + d - 1) / d), p - 32};
+}
+
+// An id as a row of the table, or kNoRow (no table has that many).
+constexpr uint32_t kNoRow = 0xffffffffu;
+__device__ __forceinline__ uint32_t row_of(int32_t id, uint32_t rows, uint32_t skip) {
+    return (uint32_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
+}
+__device__ __forceinline__ uint32_t row_of(int64_t id, uint32_t rows, uint32_t skip) {
+    return (uint64_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
 }
 
 // ---- launchers ----

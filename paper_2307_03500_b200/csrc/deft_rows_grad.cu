@@ -36,15 +36,6 @@ inline size_t group_smem(int warps, int64_t per_cta, int list_cap) {
     return sizeof(uint2) * (size_t)list_cap * (size_t)warps + sizeof(uint32_t) * ((size_t)(warps + 1) * (size_t)per_cta + 64);
 }
 
-// An id as a row of the table, or kNoRow.
-constexpr uint32_t kNoRow = 0xffffffffu;
-__device__ __forceinline__ uint32_t row_of(int32_t id, uint32_t rows, uint32_t skip) {
-    return (uint32_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
-}
-__device__ __forceinline__ uint32_t row_of(int64_t id, uint32_t rows, uint32_t skip) {
-    return (uint64_t)id < rows && (uint32_t)id != skip ? (uint32_t)id : kNoRow;
-}
-
 // Puts a tile's tokens in order of their CTAs (tokens of one CTA in order of position) and writes where each CTA's begin.
 template <typename Id>
 __global__ void __launch_bounds__(256) k_split_tokens(const Id* __restrict__ ids, uint32_t n, uint32_t rows, uint32_t skip, uint2* entries, uint16_t* first) {
@@ -518,16 +509,17 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
 
 // Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls.
 constexpr int64_t kMinTasks = 4096;
-constexpr int kLeast = 8;
+constexpr int kLeastUnit = 8, kMostUnit = 32;
+static_assert(kMostUnit <= 32 && kMostUnit % kLeastUnit == 0, "a lane for every token of a unit");
 inline int unit_of(int64_t n, int64_t slices) {
-    int unit = 32;
-    while (unit > kLeast && (n + unit - 1) / unit * slices < kMinTasks) unit >>= 1;
+    int unit = kMostUnit;
+    while (unit > kLeastUnit && (n + unit - 1) / unit * slices < kMinTasks) unit >>= 1;
     return unit;
 }
 // Upper bound of units * slices over all calls of up to n tokens and up to `slices` slices (unit_of() gives fewer
 // tokens more units): what the workspace is sized by, so that it serves smaller calls too.
 inline size_t most_tasks(int64_t n, int64_t slices) {
-    const int64_t few = (n + kLeast - 1) / kLeast * slices, many = (n + 31) / 32 * slices;
+    const int64_t few = (n + kLeastUnit - 1) / kLeastUnit * slices, many = (n + kMostUnit - 1) / kMostUnit * slices;
     const int64_t small = few < 2 * kMinTasks + slices ? few : 2 * kMinTasks + slices;
     return (size_t)(small > many ? small : many);
 }
