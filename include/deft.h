@@ -474,8 +474,10 @@ DEFT_API deft_status deft_step_part(float* resid_acc_d, const float* grad_d, int
 /* ------------------------------------------------------------------------------------------
  * Row operators: the row-sparse front end of a language model (no counterpart in the paper, whose
  * language model's embedding gradient they produce).  Matrices are row-major with a pitch (ld, in
- * elements, >= the row length); pointers need the alignment of their elements only.  Arithmetic is
- * fp32 whatever the types, with one rounding at the end.
+ * elements, >= the row length); pointers need the alignment of their elements only (rows that start on
+ * 16-byte boundaries are fastest).  Reads are of whole 16-byte granules: the bytes beside a row that share
+ * one with its elements are read too (and not used), which any CUDA allocation allows.  Writes touch the
+ * elements alone.  Arithmetic is fp32 whatever the types, with one rounding at the end.
  *
  * Dropout.  The mask is a function of (seed, offset, row, column) and is never stored:
  * Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011) with the counter (column / 8, row, low and
@@ -519,8 +521,8 @@ DEFT_API deft_status deft_embed(const void* table_d, int32_t table_type, int64_t
  *   ws_d        deft_embed_workspace_bytes(n, rows, width), 256-byte aligned; holds nothing between
  *               calls.  Calls that share a workspace must not overlap on the GPU.
  * The position rows' gradient is the same call with ids[t] = t % pos_rows and scale 1.
- * Errors: INVALID_ARG, CAPACITY (workspace), TOO_LARGE (n or width beyond 2^31 - 1, rows beyond
- * DEFT_EMBED_MAX_ROWS), CUDA.
+ * Errors: INVALID_ARG, CAPACITY (workspace), TOO_LARGE (n beyond 2^31 - 1, width or ld_grad_out
+ * beyond 2^30 - 1, rows beyond DEFT_EMBED_MAX_ROWS), CUDA.
  */
 DEFT_API size_t deft_embed_workspace_bytes(int64_t n, int64_t rows, int64_t width);
 DEFT_API deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_type, int64_t ld_grad_out,

@@ -7,6 +7,7 @@ namespace deft {
 namespace {
 
 constexpr int64_t kMaxTokens = 2147483647LL;   // token positions, rows and columns are 32-bit
+constexpr int64_t kMaxWidth = (1LL << 30) - 1;   // of the gradient's matrices: a row's bytes are a 32-bit number
 
 bool type_ok(int32_t t) { return t == DEFT_F32 || t == DEFT_BF16 || t == DEFT_F16; }
 bool elem_aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -70,7 +71,7 @@ deft_status deft_embed(const void* table_d, int32_t table_type, int64_t rows, in
 }
 
 size_t deft_embed_workspace_bytes(int64_t n, int64_t rows, int64_t width) {
-    if (n < 0 || n > kMaxTokens || rows < 1 || rows > DEFT_EMBED_MAX_ROWS || width < 1 || width > kMaxTokens) return 0;
+    if (n < 0 || n > kMaxTokens || rows < 1 || rows > DEFT_EMBED_MAX_ROWS || width < 1 || width > kMaxWidth) return 0;
     return embed_grad_ws_bytes(n, rows, width);
 }
 
@@ -84,7 +85,7 @@ deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_type, int64
     EmbedGradArgs a{};
     double gain;
     if (!drop_args(p, seed, offset, offset_d, &a.drop, &gain)) return DEFT_ERR_INVALID_ARG;
-    if (n > kMaxTokens || width > kMaxTokens || rows > DEFT_EMBED_MAX_ROWS) return DEFT_ERR_TOO_LARGE;
+    if (n > kMaxTokens || width > kMaxWidth || rows > DEFT_EMBED_MAX_ROWS || (n > 0 && ld_grad_out > kMaxWidth)) return DEFT_ERR_TOO_LARGE;
     if (n > 0 && (!matrix_ok(grad_out_d, grad_out_type, n, width, ld_grad_out) || !ids_d || !elem_aligned(ids_d, (size_t)id_bytes)))
         return DEFT_ERR_INVALID_ARG;
     if (embed_grad_ws_bytes(n, rows, width) > ws_bytes) return DEFT_ERR_CAPACITY;

@@ -181,11 +181,11 @@ def _dp(t, dtype=None):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream, device: Optional[int] = None) -> ctypes.c_void_p:
-    """The handle of `stream`, or of the current stream of the device (the current one by default)."""
-    if stream is None:   # (the handle alone: building a Stream object costs more than the call it is for)
+def _stream(stream) -> ctypes.c_void_p:
+    """The handle of `stream`, or of the current stream."""
+    if stream is None:   # (the handle alone: a Stream object takes 3 us to build, as long as a launch)
         import torch
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -660,24 +660,27 @@ def _matrix(t, name: str) -> Tuple[int, int, int]:
     return t.numel() // cols, cols, pitch
 
 
-def _device(*tensors) -> int:
+def _device(first, *others) -> int:
     """The one CUDA device that the tensors (None: not given) lie on."""
-    index = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and (t.get_device() != index or index < 0):
+    index = first.get_device()
+    if index < 0:
+        raise ValueError("expected CUDA tensors on one device")
+    for t in others:
+        if t is not None and t.get_device() != index:
             raise ValueError("expected CUDA tensors on one device")
     return index
 
 
-def _call(name: str, device: int, *args) -> None:
-    """Calls the library with `device` current."""
+def _call(name: str, device: int, stream, *args) -> None:
+    """Calls the library with `device` current, on `stream` or that device's current one."""
     import torch
     fn = getattr(_lib or lib(), name)
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
     if torch._C._cuda_getDevice() == device:
-        status = fn(*args)
+        status = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            status = fn(*args)
+            status = fn(*args, handle)
     if status:
         _check(name, status)
 
@@ -692,7 +695,8 @@ def _ids(ids) -> int:
 def _offset(offset_d) -> Optional[int]:
     if offset_d is None:
         return None
-    if offset_d.numel() != 1 or offset_d.element_size() != 8 or offset_d.is_floating_point():
+    import torch
+    if offset_d.numel() != 1 or offset_d.dtype not in (torch.int64, torch.uint64):
         raise ValueError("offset_d: one 64-bit integer")
     return offset_d.data_ptr()
 
@@ -713,9 +717,9 @@ def deft_embed(table, ids, out, scale: float = 1.0, pos=None, p: float = 0.0, se
         if w != width or pos.dtype != table.dtype:
             raise ValueError("pos: rows like the table's expected")
     dev = _device(out, table, ids, pos, offset_d)
-    _call("deft_embed", dev, table.data_ptr(), _type(table), rows, width, ld_table, ids.data_ptr(), _ids(ids), n, scale,
+    _call("deft_embed", dev, stream, table.data_ptr(), _type(table), rows, width, ld_table, ids.data_ptr(), _ids(ids), n, scale,
           None if pos is None else pos.data_ptr(), pos_rows, ld_pos, p, seed & _U64, offset & _U64, _offset(offset_d), out.data_ptr(),
-          _type(out), ld_out, _stream(stream, dev))
+          _type(out), ld_out)
 
 
 def deft_embed_workspace_bytes(n: int, rows: int, width: int) -> int:
@@ -744,10 +748,12 @@ def deft_embed_grad(grad_out, ids, grad, ws, accumulate: bool = False, skip_id: 
         n, w, ld = 0, width, width
     if w != width or ids.numel() != n:
         raise ValueError("grad_out, ids and grad disagree")
+    if not ws.is_contiguous():
+        raise ValueError("ws: a contiguous tensor")
     dev = _device(grad, grad_out, ids, ws, offset_d)
-    _call("deft_embed_grad", dev, grad_out.data_ptr(), _type(grad_out), ld, ids.data_ptr(), _ids(ids), n, rows, width, skip_id, scale, p,
+    _call("deft_embed_grad", dev, stream, grad_out.data_ptr(), _type(grad_out), ld, ids.data_ptr(), _ids(ids), n, rows, width, skip_id, scale, p,
           seed & _U64, offset & _U64, _offset(offset_d), grad.data_ptr(), 1 if accumulate else 0, ws.data_ptr(),
-          ws.numel() * ws.element_size(), _stream(stream, dev))
+          ws.numel() * ws.element_size())
 
 
 def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0, offset_d=None, stream=None) -> None:
@@ -759,5 +765,5 @@ def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0,
     ld_y = _matrix(y, "y")[2]
     ld_add = 0 if add is None else _matrix(add, "add")[2]
     dev = _device(y, x, add, offset_d)
-    _call("deft_dropout", dev, x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(), _type(y), ld_y,
-          rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d), _stream(stream, dev))
+    _call("deft_dropout", dev, stream, x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(), _type(y), ld_y,
+          rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d))

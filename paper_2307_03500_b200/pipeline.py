@@ -84,15 +84,21 @@ class DeftStep:
         if not rows:
             return np.empty((0, 2), dtype=np.int64)
         todo, parts, need = [], set(), 0
-        if resid.dim() != 1 or resid.numel() != self.n_g:
-            raise ValueError("resid: a flat tensor of n_g elements")
+        if resid.dim() != 1 or resid.numel() != self.n_g or resid.dtype != torch.float32 or not resid.is_contiguous():
+            raise ValueError("resid: a flat float32 tensor of n_g elements")
         for r in rows:                      # everything is checked before anything is added
             if not 0 <= r.tensor < len(self.tensor_start) - 1:
                 raise ValueError("no tensor %d" % r.tensor)
             a, b = int(self.tensor_start[r.tensor]), int(self.tensor_start[r.tensor + 1])
-            width = int(r.grad_out.shape[-1])
+            n, width, _ = deft._matrix(r.grad_out, "grad_out")
+            deft._type(r.grad_out), deft._ids(r.ids), deft._offset(r.offset_d)
+            deft._device(resid, r.grad_out, r.ids, r.offset_d)
             if width < 1 or (b - a) % width:
                 raise ValueError("tensor %d has no rows of %d elements" % (r.tensor, width))
+            if r.ids.numel() != n:
+                raise ValueError("one id for every row of grad_out expected")
+            if not (0.0 <= r.p < 1.0 and math.isfinite(r.scale)):
+                raise ValueError("p in [0, 1) and a finite scale expected")
             size = deft.deft_embed_workspace_bytes(r.ids.numel(), (b - a) // width, width)
             if size == 0:
                 raise deft.DeftError("deft_embed_workspace_bytes", deft.ERR_INVALID_ARG)

@@ -164,12 +164,91 @@ def test_embed_grad_long_rows_and_large_tables(deft, n, rows, width, how, accumu
     check_grad(deft, rng, n, rows, width, "bf16", ids_of(rng, n, rows, how), accumulate=accumulate, p=0.1)
 
 
+@pytest.mark.parametrize("n", [32767, 32768, 32769, 33792, 40000])
+@pytest.mark.parametrize("how", ["outside", "zipf", "one"])
+def test_embed_grad_where_tokens_are_split_first(deft, n, how):
+    """Both sides of the size from which tokens are ordered by CTA first, whole and broken tiles of them."""
+    rng = np.random.default_rng(n)
+    check_grad(deft, rng, n, 1000, 8, "f32", ids_of(rng, n, 1000, how), skip_id=500 if how != "one" else 3)
+    check_grad(deft, rng, n, 129, 20, "bf16", ids_of(rng, n, 129, how), wide=False, accumulate=True, p=0.5)
+
+
+@pytest.mark.parametrize("n,rows", [(3000, 400000), (70000, 400000), (5000, 1500000), (40000, 3000000)])
+def test_embed_grad_lists_longer_than_their_room(deft, n, rows):
+    """Tables whose counters leave little room for a warp's list of tokens, and one token in all places: the ids (or the
+    split tiles) are read again."""
+    rng = np.random.default_rng(rows)
+    check_rows(deft, rng, n, rows, np.where(rng.random(n) < 0.9, rows - 1, rng.integers(0, rows, n)))
+    check_rows(deft, rng, n, rows, np.full(n, rows - 2))
+
+
+def check_rows(deft, rng, n, rows, ids):
+    """check_grad for tables too large for a dense reference: the rows with tokens, and that no others were written."""
+    width = 8
+    dy = randn(rng, (n, width), "f32")
+    g = torch.full((rows, width), float("nan"), device="cuda")
+    uniq, inv = np.unique(ids, return_inverse=True)
+    at = torch.from_numpy(uniq).cuda()
+    g[at] = 0.0
+    deft.deft_embed_grad(dy, torch.from_numpy(ids).cuda(), g, deft.alloc_embed_workspace(n, rows, width), accumulate=True)
+    want, size, tokens = P.embed_grad(host(dy), inv, uniq.size)
+    assert np.all(np.abs(host(g[at]) - want) <= (tokens[:, None] + 3) * U * size)
+    assert int(torch.isnan(g).any(1).sum()) == rows - uniq.size
+
+
 @pytest.mark.parametrize("n", [0, 5])
 def test_embed_grad_without_contributing_tokens(deft, n):
     rng = np.random.default_rng(1)
     for accumulate in (False, True):
         check_grad(deft, rng, n, 6, 16, "bf16", np.full(n, 4, dtype=np.int64), accumulate=accumulate, skip_id=4)
         check_grad(deft, rng, n, 6, 16, "f32", np.full(n, 600, dtype=np.int64), accumulate=accumulate)
+
+
+@pytest.mark.parametrize("pos_rows", [0, 64, 100, 16384, 20000])
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f32", "f16")])
+def test_embed_where_threads_take_several_rows(deft, pos_rows, kind, out):
+    """Enough tokens for several rows a thread, with position rows that repeat inside them, do not divide them, or never repeat."""
+    rng = np.random.default_rng(pos_rows)
+    n, rows, width = 16384 + 37, 300, 1032
+    w, pos = randn(rng, (rows, width), kind), randn(rng, (pos_rows, width), kind) if pos_rows else None
+    ids = ids_of(rng, n, rows, "outside")
+    ids[-1] = rows - 1
+    y = torch.full((n + 1, width), 9.0, dtype=TYPES[out], device="cuda")
+    deft.deft_embed(w, torch.from_numpy(ids).cuda(), y[:n], scale=0.5, pos=pos, p=0.25, seed=11)
+    kw = dict(scale=0.5, p=0.25, seed=11)
+    want = P.embed(host(w), ids, pos=None if pos is None else host(pos), **kw)
+    size = P.embed(np.abs(host(w)), ids, pos=None if pos is None else np.abs(host(pos)), **kw)
+    assert np.all(np.abs(host(y[:n]) - want) <= 5 * U * size + HALF[out] * np.abs(want) + TINY[out])
+    assert torch.all(y[n] == 9.0)
+
+
+@pytest.mark.parametrize("x_kind,y_kind", [("bf16", "bf16"), ("f32", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("with_add", [False, True])
+@pytest.mark.parametrize("cols", [1024, 1500, 1021])
+def test_dropout_where_threads_take_several_rows(deft, x_kind, y_kind, with_add, cols):
+    rng = np.random.default_rng(cols)
+    rows = 40003
+    x = torch.empty((rows, cols), dtype=TYPES[x_kind], device="cuda").normal_()
+    add = torch.empty((rows, cols), dtype=TYPES[y_kind], device="cuda").normal_() if with_add else None
+    y = torch.full((rows + 1, cols), 9.0, dtype=TYPES[y_kind], device="cuda")
+    deft.deft_dropout(x, y[:rows], add=add, p=0.1, seed=2, offset=8)
+    assert torch.all(y[rows] == 9.0)
+    pick = np.concatenate([np.arange(0, rows, 997), [rows - 1]])
+    sel = torch.from_numpy(pick).cuda()
+    c0, c1 = np.meshgrid(np.arange(-(-cols // 8), dtype=np.uint64), pick.astype(np.uint64))
+    words = np.stack(P.philox([c0, c1, np.full_like(c0, 8), 0 * c0], (2, 0)), -1)
+    k = np.stack([words & np.uint64(0xFFFF), words >> np.uint64(16)], -1).reshape(pick.size, -1)[:, :cols] >= P.threshold(0.1)
+    xs = host(x[sel])
+    want = np.where(k, xs * P.gain(0.1), 0.0) + (host(add[sel]) if with_add else 0.0)
+    size = np.abs(xs) * P.gain(0.1) + (np.abs(host(add[sel])) if with_add else 0.0)
+    assert np.all(np.abs(host(y[sel]) - want) <= 5 * U * size + HALF[y_kind] * np.abs(want) + TINY[y_kind])
+    again = torch.empty_like(y[:rows])                      # every row, against the same call on single rows' worth of work
+    half = rows // 2
+    deft.deft_dropout(x, again, add=add, p=0.1, seed=2, offset=8)
+    assert torch.equal(again, y[:rows])
+    small = torch.empty_like(x[:half], dtype=TYPES[y_kind])
+    deft.deft_dropout(x[:half], small, add=None if add is None else add[:half], p=0.1, seed=2, offset=8)
+    assert torch.equal(small, y[:half])                     # a row's mask does not depend on how many rows there are
 
 
 def test_largest_table_and_offsets_beyond_32_bits(deft):
@@ -377,7 +456,8 @@ def test_refusals_of_the_binding(deft):
                  lambda: deft.deft_embed_grad(f(4, 8), ids, f(6, 8).half(), ws), lambda: deft.deft_embed_grad(f(4, 9), ids, f(6, 8), ws),
                  lambda: deft.deft_embed_grad(f(4, 8), ids, f(6, 16)[:, :8], ws), lambda: deft.deft_embed_grad(f(1, 8).expand(4, 8), ids, f(6, 8), ws),
                  lambda: deft.deft_dropout(f(4, 8), f(4, 9)), lambda: deft.deft_dropout(f(4, 8), f(4, 8), add=f(4, 8).half()),
-                 lambda: deft.deft_dropout(f(8, 4).t(), f(4, 8))):
+                 lambda: deft.deft_dropout(f(8, 4).t(), f(4, 8)), lambda: deft.deft_embed_grad(f(4, 8), ids, f(6, 8), ws[::2]),
+                 lambda: deft.deft_dropout(f(4, 8), f(4, 8), offset_d=f(1, dtype=torch.complex64))):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: deft.deft_dropout(f(4, 8), f(4, 8), p=1.0), lambda: deft.deft_embed(f(6, 8), ids, f(4, 8), scale=float("inf")),
@@ -500,11 +580,32 @@ def test_step_rows_refusals(deft):
     ds, row, grad, _ = _rows_case(deft, rng, 90, 8, 50, [200, 100], 2, 0.05)
     e = randn(rng, (ds.n_g,), "f32")
     before = e.clone()
-    for bad in (replace(row, tensor=-1), replace(row, tensor=9), replace(row, tensor=0), replace(row, grad_out=row.grad_out[:, :7])):
+    for bad in (replace(row, tensor=-1), replace(row, tensor=9), replace(row, tensor=0), replace(row, grad_out=row.grad_out[:, :7]),
+                replace(row, ids=row.ids[:-1]), replace(row, ids=row.ids.short()), replace(row, ids=row.ids.cpu()), replace(row, p=1.0),
+                replace(row, scale=float("nan")), replace(row, grad_out=row.grad_out.double()), replace(row, offset_d=torch.zeros(1, device="cuda"))):
         for call in (ds.step, ds.step_fused):
             with pytest.raises(ValueError):
                 call(e, grad, 0, rows=[row, bad])
     assert torch.equal(e, before)                          # refused before anything was added
+
+
+def test_two_row_gradients_of_one_table(deft):
+    """A table that is looked up twice (encoder and decoder): its part takes both, in order."""
+    from paper_2307_03500_b200.pipeline import DeftStep, RowGradient
+    rng = np.random.default_rng(37)
+    vocab, width = 200, 24
+    ds = DeftStep([vocab * width, 1000], 2, 0.05)
+    rows = [RowGradient(0, torch.from_numpy(ids_of(rng, n, vocab, "zipf")).cuda(), randn(rng, (n, width), "f32")) for n in (300, 41)]
+    e, grad = randn(rng, (ds.n_g,), "f32"), randn(rng, (ds.n_g,), "f32")
+    want = e.clone()
+    table = want[:vocab * width].view(vocab, width)
+    for r in rows:
+        deft.deft_embed_grad(r.grad_out, r.ids, table, deft.alloc_embed_workspace(300, vocab, width), accumulate=True)
+    want[vocab * width:] += grad[vocab * width:]
+    norms = ds.layer_norms(e, grad, rows)
+    assert torch.equal(e, want)
+    ref = np.array([np.linalg.norm(host(want)[a:b]) for a, b in zip(ds.layer_start[:-1], ds.layer_start[1:])])
+    assert np.all(np.abs(norms - ref) <= 1e-5 * ref)
 
 
 def test_multi_worker_simulation_with_rows(deft):

@@ -138,3 +138,21 @@ def test_matrix_shapes_of_the_binding():
         deft._offset(torch.zeros(1))
     with pytest.raises(ValueError):
         deft._device(torch.zeros(1))
+
+
+def test_workspace_serves_smaller_calls():
+    """deft_embed_workspace_bytes does not fall with any of its arguments (small calls are split finer than large ones)."""
+    rng = np.random.default_rng(0)
+    for _ in range(3000):
+        n, rows, width = (int(np.exp(rng.uniform(0, hi))) for hi in (14, 14.9, 9))
+        most = deft.deft_embed_workspace_bytes(n, rows, width)
+        less = [int(rng.integers(1, x + 1)) for x in (n, rows, width)]
+        assert 0 < deft.deft_embed_workspace_bytes(*less) <= most
+        assert deft.deft_embed_workspace_bytes(0, rows, width) <= most
+
+
+def test_pitches_beyond_a_call():
+    big = 2 ** 30
+    assert _grad(ld=big) == _grad(width=big, ld=big) == deft.ERR_TOO_LARGE
+    assert deft.deft_embed_workspace_bytes(5, 5, big) == 0
+    assert _embed(ld_table=2 ** 60) == _embed(ld_out=2 ** 60) == _dropout(ld_x=2 ** 60) == deft.ERR_INVALID_ARG
