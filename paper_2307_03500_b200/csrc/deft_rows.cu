@@ -2,7 +2,14 @@
 //
 // A thread keeps its columns and takes every `stride`-th row (up to four rows' loads in flight), so that consecutive
 // threads read consecutive groups whatever the width, one division places it, and the parts of the generator's first
-// two rounds that depend on the column or the offset alone are computed once.  Rows that start on no 8-byte boundary are taken by warps in slices of
+// two rounds that depend on the column or the offset alone are computed once.  Loads of several rows are in flight before
+// the first is converted (converting each as it came made the kernel wait for every load: 0.44 instead of 0.17 ms).
+//
+// What bounds them: dropout of 65536 x 4096 bf16 the memory (172 us, 0.97 of the measured copy rate; 0.54 of the integer
+// pipes' time is the generator), of 16384 x 1024 with a residual added 18.5 us (0.84).  Lookup of 131072 x 1024 fp32 -> bf16
+// with positions and dropout 104 us (0.55 of the copy rate over the bytes it cannot do without; 0.81 GB move between
+// L2 and the SMs, because a table row is read again for each of its tokens): the wait for a table row behind its id,
+// with two rows in flight per thread.  Calls of up to a few hundred thousand elements: the launch (3 to 4 us).  Rows that start on no 8-byte boundary are taken by warps in slices of
 // 256 columns instead, dealt out one by one.
 #include "deft_rows.cuh"
 
@@ -167,7 +174,12 @@ inline RowSplit row_split(int64_t rows, int64_t cols, int align, int rounds, int
     int64_t each = rows * units / ((int64_t)sm_count() * kBlocksDeep * per_block * rounds);
     each = each < 1 ? 1 : (each > kMostEach ? kMostEach : each);
     int64_t stride = (rows + each - 1) / each;
-    if (pos_rows && each > 1 && pos_rows < rows) stride = (stride + pos_rows - 1) / pos_rows * pos_rows;
+    // a turn that goes past the last row counts up to eight strides further, in 32 bits: no rounding that would not fit
+    // (without it the stride is a sixteenth of the rows wherever they are many)
+    if (pos_rows && each > 1 && pos_rows < rows) {
+        const int64_t rounded = (stride + pos_rows - 1) / pos_rows * pos_rows;
+        if (rows + 8 * rounded <= 0xffffffffLL) stride = rounded;
+    }
     const int64_t most = (0x7fffffff - 255) / units;   // places are 31-bit; a larger matrix takes more turns of the loop
     if (stride > most) stride = most;
     if (stride > rows) stride = rows;

@@ -10,6 +10,8 @@ namespace deft {
 namespace {
 
 // ---- 1. grouping ----
+// What bounds it: latency.  4.3 us for 700 tokens, 8.6 us for 16384 (one read of the ids, two prefixes, five barriers),
+// 4.2 + 10.6 us for 131072 with the splitting pass before it (33.7 without; at 16384 the two forms are level).
 // Table row v belongs to CTA v % kOwners.  Every CTA reads all ids (they stay in L2) and keeps its own: no CTA
 // needs anything from another, so there is no barrier over the grid and no pass over global counters.  With many
 // tokens that reading is most of the work (34 us for 131072), and k_split_tokens orders tiles of them by CTA first.
@@ -19,7 +21,7 @@ namespace {
 constexpr int kOwners = 128;                 // CTAs (a power of two below the 148 SMs)
 constexpr size_t kGroupSmem = 220 * 1024;
 constexpr int kTokenTile = 1024;             // tokens per tile of the splitting pass
-constexpr int64_t kSplitFrom = 32768;        // calls of more tokens split first
+constexpr int64_t kSplitFrom = 32768;        // calls of more tokens split first (16384: 3.9 + 6.2 against 8.7 us, 131072: 14.8 against 33.7)
 constexpr int kSplitPitch = kOwners + 2;     // a tile's first entry of every CTA, and their number
 constexpr int kListMost = 1024;              // own tokens a warp remembers at most; one that has more reads the ids again
 
@@ -234,14 +236,22 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 }
 
 // ---- 2. the sums ----
-// The grouped tokens are cut into units of kUnit consecutive ones, whatever rows they belong to: every unit is the
-// same work, and all its loads are known from the start (a warp per row would wait for one token's load after the
-// other, and a frequent token's row would keep one warp busy for the whole launch).  A warp takes one unit and 256
-// columns, eight per lane.  Runs of one row that lie inside a unit are finished there.  A run that crosses units
-// leaves a partial sum per unit; the warp that arrives last at the run's counter adds them in order (in two levels of
-// kJoin when there are more), so the bits do not depend on the order of arrival.
+// G[v] = factor * sum of the kept elements of v's tokens.  The grouped tokens are cut into units of consecutive ones,
+// whatever rows they belong to: every unit is the same work, and all its loads are known from the start (a warp per row
+// waits for one token's load after the other, and a frequent token's row keeps one warp busy for the whole launch:
+// 4.9 ms instead of 0.12 at 131072 x 1024).  A warp takes one unit and 256 columns, eight per lane.  Its tokens' slices,
+// and where the gradient is added the target rows', come through a ring of asynchronous copies in shared memory: the
+// loads in flight do not cost registers (with them in registers the kernel spilled, or ran on half the warps: 0.15 to
+// 0.33 ms).  Runs of one row that lie inside a unit are finished there.  A run that crosses units leaves a partial sum per
+// unit; the warp that arrives last at the run's counter adds them in order (in two levels of kJoin when there are
+// more), so the bits do not depend on the order of arrival.
+//
+// What bounds it, 131072 x 1024 bf16 added with dropout: 103 us for 464 MB, 0.70 of the measured copy rate; the
+// schedulers issue in 68 % of the cycles (137 instructions per token and 256 columns, 34 of them the generator's
+// products and exclusive ors): the integer pipes and the memory are both near what they give together.  Without
+// dropout it is the memory.  Small calls are bound by latency: 9 us for 700 x 1500, of which a third is the joins.
 constexpr int kReduceThreads = 128;
-constexpr int kReduceBlocks = 8; // CTAs an SM holds (64 registers a thread)
+constexpr int kReduceBlocks = 8; // CTAs an SM holds (64 registers a thread; with 48 it spills)
 constexpr int kJoin = 32;        // units whose partial sums one warp adds up
 constexpr int kClearing = 2;     // clearing CTAs per SM
 constexpr int kRing = 6144;      // bytes of shared memory a warp's copies go to: 192 KB on an SM
@@ -507,7 +517,8 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
         join<kAdd, kWide>(a, r, __shfl_sync(0xffffffffu, item.x, __ffs((int)open) - 1), unit_id, slice, left);
 }
 
-// Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls.
+// Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls, but not fewer than eight: the
+// more units, the more partial sums are joined (700 x 1500: 17.2, 13.9, 11.4, 10.9 us with units of 1, 2, 4, 8).
 constexpr int64_t kMinTasks = 4096;
 constexpr int kLeastUnit = 8, kMostUnit = 32;
 static_assert(kMostUnit <= 32 && kMostUnit % kLeastUnit == 0, "a lane for every token of a unit");
