@@ -599,7 +599,7 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
             DEFT_CUDA_TRY(cudaGetLastError());
         }
         auto kernel = split ? k_group_tokens<Id, true> : k_group_tokens<Id, false>;
-        DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGroupSmem));
+        if (smem > 48 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGroupSmem));
         cfg.gridDim = dim3(kOwners);
         cfg.blockDim = dim3((unsigned)warps * 32);
         cfg.dynamicSmemBytes = smem;

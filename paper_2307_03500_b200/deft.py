@@ -300,10 +300,10 @@ def deft_layer_norms(resid_acc, grad, layer_start_d, norms_d, ws, stream=None) -
 
 def _parts(parts):
     """(begin, end) pairs as a host array for the library, and their number."""
-    flat = [int(x) for part in parts for x in part]
-    if len(flat) != 2 * len(parts):
+    n = len(parts)
+    if any(len(part) != 2 for part in parts):
         raise ValueError("parts: (begin, end) pairs")
-    return (ctypes.c_int64 * max(1, len(flat)))(*flat), len(parts)
+    return (ctypes.c_int64 * max(1, 2 * n))(*[int(x) for part in parts for x in part]), n
 
 
 def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, stream=None) -> None:
