@@ -21,7 +21,7 @@ namespace {
 constexpr int kOwners = 128;                 // CTAs (a power of two below the 148 SMs)
 constexpr size_t kGroupSmem = 220 * 1024;
 constexpr int kTokenTile = 1024;             // tokens per tile of the splitting pass
-constexpr int64_t kSplitFrom = 32768;        // calls of more tokens split first (16384: 3.9 + 6.2 against 8.7 us, 131072: 14.8 against 33.7)
+constexpr int64_t kSplitFrom = 16384;        // calls of more tokens split first (16384: 3.9 + 6.9 against 9.2 us, 20000: 11.2 against 12.3, 131072: 14.8 against 33.7)
 constexpr int kSplitPitch = kOwners + 2;     // a tile's first entry of every CTA, and their number
 constexpr int kListMost = 1024;              // own tokens a warp remembers at most; one that has more reads the ids again
 
