@@ -365,9 +365,9 @@ __device__ __forceinline__ void join(const EmbedGradArgs& a, const ReduceArgs& r
         __syncwarp();
         uint32_t n = 0;
         if (lane == 0) n = atomicAdd(r.arrived + ((size_t)level * 2 * r.units + 2 * u + (u == s ? 1 : 0)) * r.slices + slice, 1u);
-        n = __shfl_sync(0xffffffffu, n, 0);
+        if (__shfl_sync(0xffffffffu, n, 0) != (uint32_t)(expected - 1)) return false;
         __threadfence();
-        return n == (uint32_t)(expected - 1);
+        return true;
     };
     // the partial sums of the units u, the next multiple of step, ... below end, in order
     auto add_up = [&](int u, int step, int end) {
@@ -517,21 +517,22 @@ __global__ void __launch_bounds__(kReduceThreads, kReduceBlocks) k_rows_reduce(c
         join<kAdd, kWide>(a, r, __shfl_sync(0xffffffffu, item.x, __ffs((int)open) - 1), unit_id, slice, left);
 }
 
-// Tokens per unit: 32 where there are enough for every SM's warps, fewer for small calls, but not fewer than eight: the
-// more units, the more partial sums are joined (700 x 1500: 17.2, 13.9, 11.4, 10.9 us with units of 1, 2, 4, 8).
-constexpr int64_t kMinTasks = 4096;
+// Tokens per unit: as few as make one round of warps (a second, broken one costs as much as the first: 16384 x 1024
+// written in units of 16 took 14 us longer for the tenth of the CTAs that had to wait), but eight at least: the more
+// units, the more partial sums are joined (700 x 1500: 17.2, 13.9, 11.4, 10.9 us with units of 1, 2, 4, 8), and 32 at
+// most (a lane for each).  The numbers of SMs and CTAs are constants: a call's bits do not depend on the device.
 constexpr int kLeastUnit = 8, kMostUnit = 32;
-static_assert(kMostUnit <= 32 && kMostUnit % kLeastUnit == 0, "a lane for every token of a unit");
+constexpr int64_t kRound = 148 * (kReduceBlocks - kClearing) * (kReduceThreads / 32);
 inline int unit_of(int64_t n, int64_t slices) {
-    int unit = kMostUnit;
-    while (unit > kLeastUnit && (n + unit - 1) / unit * slices < kMinTasks) unit >>= 1;
-    return unit;
+    const int64_t units = kRound / slices;      // of one round
+    const int64_t unit = units > 0 ? (n + units - 1) / units : kMostUnit;
+    return (int)(unit < kLeastUnit ? kLeastUnit : (unit > kMostUnit ? kMostUnit : unit));
 }
-// Upper bound of units * slices over all calls of up to n tokens and up to `slices` slices (unit_of() gives fewer
-// tokens more units): what the workspace is sized by, so that it serves smaller calls too.
+// Upper bound of units * slices over all calls of up to n tokens and up to `slices` slices (fewer tokens can make more
+// units): what the workspace is sized by, so that it serves smaller calls too.
 inline size_t most_tasks(int64_t n, int64_t slices) {
     const int64_t few = (n + kLeastUnit - 1) / kLeastUnit * slices, many = (n + kMostUnit - 1) / kMostUnit * slices;
-    const int64_t small = few < 2 * kMinTasks + slices ? few : 2 * kMinTasks + slices;
+    const int64_t round = kRound + slices, small = few < round ? few : round;
     return (size_t)(small > many ? small : many);
 }
 
