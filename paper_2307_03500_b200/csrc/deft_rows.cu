@@ -7,7 +7,7 @@
 //
 // What bounds them: dropout of 65536 x 4096 bf16 the memory (172 us, 0.97 of the measured copy rate; 0.54 of the integer
 // pipes' time is the generator), of 16384 x 1024 with a residual added 18.5 us (0.84).  Lookup of 131072 x 1024 fp32 -> bf16
-// with positions and dropout 104 us (0.55 of the copy rate over the bytes it cannot do without; 0.81 GB move between
+// with positions and dropout 104 us (0.55 of the copy rate over the bytes it cannot do without; 0.84 GB move between
 // L2 and the SMs, because a table row is read again for each of its tokens): the wait for a table row behind its id,
 // with two rows in flight per thread.  Calls of up to a few hundred thousand elements: the launch (3 to 4 us).  Rows that start on no 8-byte boundary are taken by warps in slices of
 // 256 columns instead, dealt out one by one.
