@@ -676,3 +676,67 @@ def test_language_model_front_end_step(deft):
         assert (acc - full).norm() <= 2e-3 * full.norm()   # the two products in torch run in TF32 at worst (2^-11 per term)
         sel = torch.cat([i for _, i in outs])
         assert sel.numel() == ds.k and torch.all(e[sel] == 0)
+
+
+def test_subnormals_are_kept(deft):
+    """Neither the mixed-precision additions nor the products flush: single tokens come back exactly."""
+    for kind, tiny in (("bf16", 2.0 ** -133), ("f16", 2.0 ** -24), ("f32", 2.0 ** -149)):
+        for width in (8, 41):
+            x = (torch.arange(1, 4 * width + 1, device="cuda", dtype=torch.float64).view(4, width) * tiny).to(TYPES[kind])
+            x[1] = -x[1]
+            ids = torch.tensor([2, 0, 3, 1], device="cuda")
+            g = torch.empty((4, width), device="cuda")
+            ws = deft.alloc_embed_workspace(4, 4, width)
+            deft.deft_embed_grad(x, ids, g, ws)
+            assert torch.equal(g[ids].double(), x.double())
+            y, z = torch.empty_like(x), torch.empty((4, width), device="cuda")
+            deft.deft_embed(x, ids, y)
+            assert torch.equal(y, x[ids])
+            deft.deft_dropout(x, z, add=torch.zeros_like(z), p=0.0)
+            assert torch.equal(z.double(), x.double())
+
+
+def test_captured_large_calls(deft):
+    """The split pass and a launch with most of the shared memory, captured and replayed with other ids."""
+    rng = np.random.default_rng(41)
+    n, rows, width = 20000, 150000, 40
+    dy = randn(rng, (n, width), "bf16")
+    ids = torch.from_numpy(ids_of(rng, n, rows, "zipf")).cuda()
+    g, ws = torch.zeros((rows, width), device="cuda"), deft.alloc_embed_workspace(n, rows, width)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        deft.deft_embed_grad(dy, ids, g, ws, p=0.1, seed=2)
+    for how in ("zipf", "uniform", "one"):
+        ids.copy_(torch.from_numpy(ids_of(rng, n, rows, how)))
+        graph.replay()
+        want = torch.empty_like(g)
+        torch.cuda.synchronize()
+        deft.deft_embed_grad(dy, ids, want, deft.alloc_embed_workspace(n, rows, width), p=0.1, seed=2)
+        assert torch.equal(g, want)
+
+
+def test_one_process_per_worker_with_rows(deft):
+    """DistributedWorker as the only rank of an NCCL group: rows are the dense gradient there too."""
+    import os
+    import torch.distributed as dist
+    from paper_2307_03500_b200.distributed import DistributedWorker
+    from paper_2307_03500_b200.pipeline import RowGradient
+    os.environ["MASTER_ADDR"], os.environ["MASTER_PORT"] = "127.0.0.1", "29541"
+    rng = np.random.default_rng(43)
+    vocab, width, n = 250, 36, 70
+    dist.init_process_group("nccl", rank=0, world_size=1)
+    try:
+        a, b = (DistributedWorker([vocab * width, 5000], 0.02, "deft", device="cuda:0") for _ in range(2))
+        ws = deft.alloc_embed_workspace(n, vocab, width)
+        for t in range(2):
+            row = RowGradient(0, torch.from_numpy(ids_of(rng, n, vocab, "zipf")).cuda(), randn(rng, (n, width), "f16"), p=0.5, seed=t)
+            grad = randn(rng, (vocab * width + 5000,), "f32")
+            dense = grad.clone()
+            deft.deft_embed_grad(row.grad_out, row.ids, dense[:vocab * width].view(vocab, width), ws, p=0.5, seed=t)
+            x, y = a.step(grad, [row]), b.step(dense)
+            assert torch.equal(x.union, y.union) and torch.equal(x.mean, y.mean) and x.error == y.error
+            assert torch.equal(a.e, b.e)
+    finally:
+        dist.destroy_process_group()
