@@ -177,7 +177,16 @@ k_accum_norms(float* __restrict__ e, const float* __restrict__ g, int64_t n,
             const double tot = block_sum(acc, sh);
             if (threadIdx.x == 0) partial[t + l] = tot;
         } else {
-            // tile crosses layer boundaries (or is the ragged tail): one piece per layer
+            // tile crosses layer boundaries (or is the ragged tail): one piece per layer, one after the other; the whole
+            // tile is on its way to L2 before the first piece waits (a line per thread)
+            if (!kStage) {
+                static_assert(kTileA == 32 * kNormThreads, "a line of 32 elements per thread");
+                const int64_t line = lo + 32 * (int64_t)threadIdx.x;
+                if (line < hi) {
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(e + line));
+                    if (kHasGrad) asm volatile("prefetch.global.L2 [%0];" ::"l"(g + line));
+                }
+            }
             int64_t ps = lo;
             while (ps < hi) {
                 const int64_t lend = __ldg(ls + l + 1);
