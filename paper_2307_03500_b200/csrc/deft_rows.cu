@@ -25,9 +25,11 @@ constexpr int kEmbedRounds = 3;  // ... fewer where a thread waits for an id bef
 constexpr int kBlocksOne = 8;    // CTAs an SM holds where threads take one row (32 registers) ...
 constexpr int kBlocksDeep = 4;   // ... and where they take several (64)
 
-// Rows in flight of a thread that loads `words` words of each.
-__host__ __device__ constexpr int deep_of(int words) {
-    return kInFlight / words < 2 ? 2 : (kInFlight / words > kMostDeep ? kMostDeep : kInFlight / words);
+// Rows in flight of a thread that loads `words` words of each; two where the rows are not 16-byte aligned (their pieces and
+// tests take the registers that four would: dropout 32768 x 1020 bf16 39 against 50 us).
+__host__ __device__ constexpr int deep_of(int words, int align) {
+    const int fit = kInFlight / words < 2 || align != 16 ? 2 : kInFlight / words;
+    return fit > kMostDeep ? kMostDeep : fit;
 }
 
 // How the matrix is split: `units` (groups of a row, or slices of it) times `stride` rows are taken at a time.
@@ -55,8 +57,8 @@ struct Place {
 // What an id outside the table is looked up in: a share of a row at most.
 __device__ __align__(16) const char g_zeros[256 * sizeof(float)] = {};
 
-// kAlign != 0: eight columns of this thread; else this lane's share of the slice.  kFull: none of the group's (slice's)
-// columns lies beyond the row's end; left = columns from the first one to the end.
+// kAlign != 0: eight columns of this thread; else this lane's share of the slice.  kFull: the group (slice) has all its
+// columns; left = columns from its first one to the row's end.
 template <bool kFull, typename T, int kAlign>
 __device__ __forceinline__ void fetch_share(const T* p, int left, Raw8<T, kAlign>& raw) {
     if constexpr (kAlign != 0) fetch8<kFull>(p, left, raw);
@@ -64,7 +66,7 @@ __device__ __forceinline__ void fetch_share(const T* p, int left, Raw8<T, kAlign
 }
 template <bool kFull, typename T, int kAlign>
 __device__ __forceinline__ void store_share(T* p, int left, const float (&v)[kGroup]) {
-    if constexpr (kAlign != 0) store8<T, kAlign>(p, kFull ? kGroup : left, v);
+    if constexpr (kAlign != 0) store8<kFull, T, kAlign>(p, left, v);
     else store_dealt<kFull>(p, left, v);
 }
 template <int kAlign>
@@ -72,6 +74,10 @@ __device__ __forceinline__ void drop_share(float (&v)[kGroup], const DropArgs& d
     if constexpr (kAlign != 0) drop8<true>(v, d, offset, row, unit);
     else drop8_dealt<true>(v, d, offset, row, unit);
 }
+
+// Whether threads whose group (slice) is whole run code of their own.  With 8-byte alignment nearly every row ends in a
+// broken group, whose warp would run both: there all threads test their pieces (lookup 32768 x 1020 bf16 35 against 44 us).
+template <int kAlign> __device__ constexpr bool full_apart() { return kAlign != 8; }
 
 template <bool kFull, int kDeep, bool kPos, typename TW, typename TO, typename Id, int kAlign>
 __device__ __forceinline__ void embed_rows(const EmbedArgs& a, const RowSplit& split, const FastDiv& pos_rows, const Place<kAlign>& at, int left) {
@@ -121,9 +127,10 @@ template <int kDeep, bool kPos, typename TW, typename TO, typename Id, int kAlig
 __global__ void __launch_bounds__(kRowThreads, kDeep == 1 ? kBlocksOne : kBlocksDeep) k_embed(const __grid_constant__ EmbedArgs a, const RowSplit split, const FastDiv pos_rows) {
     const Place<kAlign> at(split);
     if (at.row >= split.stride) return;
-    const int64_t left = a.width - at.col;
-    if (left >= at.kSpan) embed_rows<true, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, at.kSpan);
-    else embed_rows<false, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, (int)left);
+    const int left = (int)min(a.width - at.col, (int64_t)at.kSpan);
+    constexpr bool kApart = full_apart<kAlign>();
+    if (kApart && left == at.kSpan) embed_rows<kApart, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, left);
+    else embed_rows<false, kDeep, kPos, TW, TO, Id, kAlign>(a, split, pos_rows, at, left);
 }
 
 template <bool kFull, int kDeep, bool kAdd, typename TX, typename TY, int kAlign>
@@ -160,9 +167,10 @@ template <int kDeep, bool kAdd, typename TX, typename TY, int kAlign>
 __global__ void __launch_bounds__(kRowThreads, kDeep == 1 ? kBlocksOne : kBlocksDeep) k_dropout(const __grid_constant__ DropoutArgs a, const RowSplit split) {
     const Place<kAlign> at(split);
     if (at.row >= split.stride) return;
-    const int64_t left = a.cols - at.col;
-    if (left >= at.kSpan) dropout_rows<true, kDeep, kAdd, TX, TY, kAlign>(a, split, at, at.kSpan);
-    else dropout_rows<false, kDeep, kAdd, TX, TY, kAlign>(a, split, at, (int)left);
+    const int left = (int)min(a.cols - at.col, (int64_t)at.kSpan);
+    constexpr bool kApart = full_apart<kAlign>();
+    if (kApart && left == at.kSpan) dropout_rows<kApart, kDeep, kAdd, TX, TY, kAlign>(a, split, at, left);
+    else dropout_rows<false, kDeep, kAdd, TX, TY, kAlign>(a, split, at, left);
 }
 
 // Threads take up to kMostEach rows each, as many as leave every SM several rounds of CTAs (the last round is rarely
@@ -210,7 +218,7 @@ deft_status launch_embed(const EmbedArgs& a, int table_type, int out_type, int i
                 auto run = [&](auto kernel) { kernel<<<blocks, kRowThreads, 0, stream>>>(a, split, pos_rows); };
                 auto with_id = [&](auto id) {
                     using Id = decltype(id);
-                    constexpr int kDeep = deep_of((int)sizeof(TW) * 2);
+                    constexpr int kDeep = deep_of((int)sizeof(TW) * 2, kAlign);
                     if (split.stride == split.rows) a.pos ? run(k_embed<1, true, TW, TO, Id, kAlign>) : run(k_embed<1, false, TW, TO, Id, kAlign>);
                     else a.pos ? run(k_embed<kDeep, true, TW, TO, Id, kAlign>) : run(k_embed<kDeep, false, TW, TO, Id, kAlign>);
                 };
@@ -239,7 +247,7 @@ deft_status launch_dropout(const DropoutArgs& a, int x_type, int y_type, cudaStr
                 using TX = decltype(x);
                 using TY = decltype(y);
                 constexpr int kAlign = decltype(al)::value;
-                constexpr int kPlain = deep_of((int)sizeof(TX) * 2), kBoth = deep_of((int)sizeof(TX) * 2 + (int)sizeof(TY) * 2);
+                constexpr int kPlain = deep_of((int)sizeof(TX) * 2, kAlign), kBoth = deep_of((int)sizeof(TX) * 2 + (int)sizeof(TY) * 2, kAlign);
                 if (split.stride == split.rows) a.add ? run(k_dropout<1, true, TX, TY, kAlign>) : run(k_dropout<1, false, TX, TY, kAlign>);
                 else a.add ? run(k_dropout<kBoth, true, TX, TY, kAlign>) : run(k_dropout<kPlain, false, TX, TY, kAlign>);
                 DEFT_CUDA_TRY(cudaGetLastError());

@@ -141,6 +141,7 @@ struct Raw8 {
 // every group of the matrix starts on such a boundary (base and row pitch are multiples of it).  A piece that starts
 // inside the row is read whole (what lies behind the row's end in it is not used); pieces behind the end are not
 // touched.  Plain loads: what is read may be what the same thread writes afterwards (dropout in place, rows added to).
+// kFull: left is eight or more.
 template <bool kFull, typename T, int kAlign>
 __device__ __forceinline__ void fetch8(const T* p, int left, Raw8<T, kAlign>& raw) {
     using P = typename Raw8<T, kAlign>::P;
@@ -150,23 +151,24 @@ __device__ __forceinline__ void fetch8(const T* p, int left, Raw8<T, kAlign>& ra
         if (kFull || i * per < left) raw.piece[i] = reinterpret_cast<const P*>(p)[i];
 }
 
-template <typename T, int kAlign>
-__device__ __forceinline__ void store8(T* p, int count, const float (&v)[kGroup]) {   // the first `count` of them
-    if constexpr (kAlign != 0) {
-        if (count == kGroup) {
-            using P = typename Piece<kAlign>::type;
-            constexpr int per = kAlign / (int)sizeof(T), pieces = kGroup / per;
-            P raw[pieces];
+// Writes the first `left` of a group (or all eight): whole pieces, and the elements of one that the row's end crosses.
+template <bool kFull, typename T, int kAlign>
+__device__ __forceinline__ void store8(T* p, int left, const float (&v)[kGroup]) {
+    using P = typename Piece<kAlign>::type;
+    constexpr int per = kAlign / (int)sizeof(T), pieces = kGroup / per;
+    P raw[pieces];
 #pragma unroll
-            for (int i = 0; i < kGroup; ++i) reinterpret_cast<T*>(raw)[i] = from_f32<T>(v[i]);
+    for (int i = 0; i < kGroup; ++i) reinterpret_cast<T*>(raw)[i] = from_f32<T>(v[i]);
 #pragma unroll
-            for (int i = 0; i < pieces; ++i) reinterpret_cast<P*>(p)[i] = raw[i];
-            return;
+    for (int i = 0; i < pieces; ++i) {
+        if (kFull || (i + 1) * per <= left) {
+            reinterpret_cast<P*>(p)[i] = raw[i];
+        } else {
+#pragma unroll
+            for (int j = 0; j < per; ++j)
+                if (i * per + j < left) p[i * per + j] = reinterpret_cast<const T*>(raw)[i * per + j];
         }
     }
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i)
-        if (i < count) p[i] = from_f32<T>(v[i]);
 }
 
 // Eight fp32 values to a 32-byte boundary.
