@@ -516,7 +516,7 @@ DEFT_API deft_status deft_embed(const void* table_d, int32_t table_type, int64_t
  *               written, rows without tokens become 0.  accumulate != 0: G is added to the rows that have
  *               tokens (one fp32 round-to-nearest add per element), the others are neither read nor
  *               written: the residual itself (see deft_layer_norms_part), or a gradient vector that holds
- *               a tied output layer's gradient.
+ *               a tied output layer's gradient.  Must not overlap the inputs.
  *   skip_id     a row that gets no gradient; -1: none
  *   ws_d        deft_embed_workspace_bytes(n, rows, width), 256-byte aligned; holds nothing between
  *               calls.  Calls that share a workspace must not overlap on the GPU.

@@ -71,8 +71,8 @@ __device__ __forceinline__ void store_share(T* p, int left, const float (&v)[kGr
 }
 template <int kAlign>
 __device__ __forceinline__ void drop_share(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t unit) {
-    if constexpr (kAlign != 0) drop8<true>(v, d, offset, row, unit);
-    else drop8_dealt<true>(v, d, offset, row, unit);
+    if constexpr (kAlign != 0) drop8(v, d, offset, row, unit);
+    else drop8_dealt(v, d, offset, row, unit);
 }
 
 // Whether threads whose group (slice) is whole run code of their own.  With 8-byte alignment nearly every row ends in a

@@ -55,18 +55,16 @@ __device__ __forceinline__ void kept2(uint32_t word, uint32_t threshold, bool& e
     odd = word >= threshold;
 }
 
-// Applies a group's mask to v: dropped elements become +0 whatever they were.
-template <bool kScale>
+// Applies a group's mask to v: kept elements are multiplied by the gain, dropped ones become +0 whatever they were.
 __device__ __forceinline__ void drop8(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t group) {
     const uint4 w = drop_words(d, offset, row, group);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float a = kScale ? v[2 * i] * d.gain : v[2 * i], b = kScale ? v[2 * i + 1] * d.gain : v[2 * i + 1];
         bool even, odd;
         kept2(u[i], d.threshold, even, odd);
-        v[2 * i] = even ? a : 0.0f;
-        v[2 * i + 1] = odd ? b : 0.0f;
+        v[2 * i] = even ? __fmul_rn(v[2 * i], d.gain) : 0.0f;
+        v[2 * i + 1] = odd ? __fmul_rn(v[2 * i + 1], d.gain) : 0.0f;
     }
 }
 
@@ -87,9 +85,8 @@ __device__ __forceinline__ void for_kept_dealt(const DropArgs& d, uint64_t offse
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) f(k, (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7) & 1u) != 0);
 }
-template <bool kScale>
 __device__ __forceinline__ void drop8_dealt(float (&v)[kGroup], const DropArgs& d, uint64_t offset, uint32_t row, uint32_t slice) {
-    for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { v[k] = kept ? (kScale ? v[k] * d.gain : v[k]) : 0.0f; });
+    for_kept_dealt(d, offset, row, slice, [&](int k, bool kept) { v[k] = kept ? __fmul_rn(v[k], d.gain) : 0.0f; });
 }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -179,8 +176,7 @@ __device__ __forceinline__ void store32(float* p, const float (&v)[kGroup]) {
 
 // A slice of 256 columns dealt out one by one: lane l has the columns 32 k + l, so that loads and stores of a matrix whose
 // rows start on no vector boundary are whole sectors all the same (eight consecutive elements per lane would touch 32
-// sectors with every load).  kFull: the slice has all
-// 256; else `left` (from its first column to the row's end).
+// sectors with every load).  kFull: the slice has all 256; else the first `left`.
 template <bool kFull, typename T>
 __device__ __forceinline__ void fetch_dealt(const T* p, int left, Raw8<T, 0>& raw) {
     const int lane = threadIdx.x & 31;
