@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 constexpr int kReduceThreads = 128;
 constexpr int kReduceBlocks = 8; // CTAs an SM holds (64 registers a thread; with 48 it spills)
 constexpr int kJoin = 32;        // units whose partial sums one warp adds up
-constexpr int kClearing = 2;     // clearing CTAs per SM
+constexpr int kClearing = 2;     // clearing CTAs per SM beside many sums
 constexpr int kRing = 6144;      // bytes of shared memory a warp's copies go to: 192 KB on an SM
 
 struct ReduceArgs {
@@ -574,9 +574,13 @@ deft_status launch_embed_grad(const EmbedGradArgs& a, int dy_type, int id_bytes,
     const uint32_t skip = a.skip_id >= 0 && a.skip_id < a.rows ? (uint32_t)a.skip_id : kNoRow;
     const GradWs w = grad_ws(a.n, a.rows, a.width);
     constexpr int64_t kWarps = kReduceThreads / 32;
-    const int64_t most = kClearing * (int64_t)sm_count(), needed = (a.rows + kWarps - 1) / kWarps;
-    const int clear_blocks = a.accumulate ? 0 : (int)(needed < most ? needed : most);
-    const int64_t blocks = ((int64_t)w.units * w.slices + kWarps - 1) / kWarps + clear_blocks;
+    // kClearing CTAs on each SM clear; where the sums take two of the places there, all others (one token into 100000 x 512:
+    // 42 against 54 us, 700 x 1500 into 33278 rows 47 against 50; with half of the places taken it costs 2 us of 35)
+    const int64_t sms = sm_count(), sum_blocks = ((int64_t)w.units * w.slices + kWarps - 1) / kWarps;
+    const int64_t clearing = sum_blocks <= 2 * sms ? kReduceBlocks - 2 : kClearing;
+    const int64_t needed = (a.rows + kWarps - 1) / kWarps;
+    const int clear_blocks = a.accumulate ? 0 : (int)(needed < clearing * sms ? needed : clearing * sms);
+    const int64_t blocks = sum_blocks + clear_blocks;
     if (blocks > 0x7fffffff) return DEFT_ERR_TOO_LARGE;
     GroupOut out{reinterpret_cast<uint2*>(a.ws + w.sorted), reinterpret_cast<uint2*>(a.ws + w.row_tab), reinterpret_cast<uint32_t*>(a.ws + w.total),
                  reinterpret_cast<uint32_t*>(a.ws + w.arrived), w.arrived_n};
