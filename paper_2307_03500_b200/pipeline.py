@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import math
 from dataclasses import dataclass
+from operator import index
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -78,42 +79,62 @@ class DeftStep:
         self._ws_rows: Optional[torch.Tensor] = None   # workspace of the row-sparse gradients, grown when needed
 
     # -- before step 1: row-sparse gradients straight into the residual (device) --------------
-    def add_rows(self, resid: torch.Tensor, rows: Sequence[RowGradient], stream=None) -> np.ndarray:
-        """Adds every RowGradient to its table's part of `resid`, in order; returns the parts that now hold their
-        gradient as int64 [parts, 2] (ascending)."""
-        if not rows:
-            return np.empty((0, 2), dtype=np.int64)
-        todo, parts, need = [], set(), 0
+    def _row_calls(self, resid: torch.Tensor, rows: Sequence[RowGradient]):
+        """What `_issue_rows` takes: per RowGradient its tensors and numbers, the parts, the workspace's bytes.  Refuses
+        whatever the calls themselves would refuse, so that none of them does after an earlier one has added its rows."""
+        calls, parts, need = [], set(), 0
         if resid.dim() != 1 or resid.numel() != self.n_g or resid.dtype != torch.float32 or not resid.is_contiguous():
             raise ValueError("resid: a flat float32 tensor of n_g elements")
-        for r in rows:                      # everything is checked before anything is added
+        for r in rows:
             if not 0 <= r.tensor < len(self.tensor_start) - 1:
                 raise ValueError("no tensor %d" % r.tensor)
             a, b = int(self.tensor_start[r.tensor]), int(self.tensor_start[r.tensor + 1])
-            n, width, _ = deft._matrix(r.grad_out, "grad_out")
+            n, width, pitch = deft._matrix(r.grad_out, "grad_out")
             deft._type(r.grad_out), deft._ids(r.ids), deft._offset(r.offset_d)
-            deft._device(resid, r.grad_out, r.ids, r.offset_d)
+            deft._device(resid, self.layer_start_d, r.grad_out, r.ids, r.offset_d)
+            if any(t is not None and t.data_ptr() % t.element_size() for t in (resid, r.grad_out, r.ids, r.offset_d)):
+                raise ValueError("tensors that start on a boundary of their elements expected")
             if width < 1 or (b - a) % width:
                 raise ValueError("tensor %d has no rows of %d elements" % (r.tensor, width))
             if r.ids.numel() != n:
                 raise ValueError("one id for every row of grad_out expected")
-            if not (0.0 <= r.p < 1.0 and math.isfinite(r.scale)):
+            if pitch >= 1 << 30:
+                raise ValueError("grad_out: rows less than 2^30 elements apart expected")
+            numbers = dict(skip_id=index(r.skip_id), scale=float(r.scale), p=float(r.p), seed=index(r.seed), offset=index(r.offset))
+            if not (0.0 <= numbers["p"] < 1.0 and math.isfinite(numbers["scale"])):
                 raise ValueError("p in [0, 1) and a finite scale expected")
-            size = deft.deft_embed_workspace_bytes(r.ids.numel(), (b - a) // width, width)
+            size = deft.deft_embed_workspace_bytes(n, (b - a) // width, width)
             if size == 0:
                 raise deft.DeftError("deft_embed_workspace_bytes", deft.ERR_INVALID_ARG)
             need = max(need, size)
             parts.add((a, b))
-            todo.append((r, a, b, width))
+            calls.append((r, a, b, width, numbers))
         if len(parts) > deft.MAX_PARTS:
             raise ValueError("at most %d tensors may have their gradient by rows" % deft.MAX_PARTS)
-        if need and (self._ws_rows is None or self._ws_rows.numel() < need):
+        return calls, parts, need
+
+    def check_rows(self, resid: torch.Tensor, grad: Optional[torch.Tensor], rows: Sequence[RowGradient]):
+        """Refuses what a step of these vectors and rows would refuse, before anything is added to `resid`."""
+        for name, t in (("resid", resid), ("grad", grad)):
+            if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != self.n_g or t.data_ptr() % 16):
+                raise ValueError("%s: a contiguous float32 tensor of n_g elements on a 16-byte boundary expected" % name)
+        if deft._device(resid, grad, self.layer_start_d) != torch.cuda.current_device():
+            raise ValueError("the step's device must be the current one")
+        return self._row_calls(resid, rows)
+
+    def add_rows(self, resid: torch.Tensor, rows: Sequence[RowGradient], stream=None) -> np.ndarray:
+        """Adds every RowGradient to its table's part of `resid`, in order; returns the parts that now hold their
+        gradient as int64 [parts, 2] (ascending).  A call that is refused has added nothing."""
+        return self._issue_rows(resid, self._row_calls(resid, rows), stream) if rows else np.empty((0, 2), dtype=np.int64)
+
+    def _issue_rows(self, resid: torch.Tensor, checked, stream=None) -> np.ndarray:
+        calls, parts, need = checked
+        if self._ws_rows is None or self._ws_rows.numel() < need:
             with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
                 self._ws_rows = torch.empty(need, dtype=torch.uint8, device=self.device)
-        for r, a, b, width in todo:
+        for r, a, b, width, numbers in calls:
             deft.deft_embed_grad(r.grad_out, r.ids, resid[a:b].view(-1, width), self._ws_rows, accumulate=True,
-                                 skip_id=r.skip_id, scale=r.scale, p=r.p, seed=r.seed, offset=r.offset,
-                                 offset_d=r.offset_d, stream=stream)
+                                 offset_d=r.offset_d, stream=stream, **numbers)
         return np.array(sorted(parts), dtype=np.int64).reshape(-1, 2)
 
     # -- step 1: accumulate + norms (device) ------------------------------------------------
@@ -122,7 +143,8 @@ class DeftStep:
         read in their parts."""
         if grad is not None and grad.numel() != self.n_g:
             raise ValueError("grad: a tensor of n_g elements")
-        deft.deft_layer_norms_part(resid, grad, self.add_rows(resid, rows), self.layer_start_d, self.norms_d, self.ws)
+        parts = self._issue_rows(resid, self.check_rows(resid, grad, rows)) if rows else ()
+        deft.deft_layer_norms_part(resid, grad, parts, self.layer_start_d, self.norms_d, self.ws)
         self.norms_h.copy_(self.norms_d, non_blocking=True)
         torch.cuda.current_stream().synchronize()
         return self.norms_h.numpy()
@@ -202,14 +224,21 @@ class DeftStep:
                 if e.cuda_event == 0:   # torch creates the handle lazily, on first record
                     e.record()
                 flat.append(e.cuda_event)
+            if len(flat) != 4:
+                raise ValueError("events: four CUDA events")
             ev = (ctypes.c_void_p * 4)(*flat)
         st = torch.cuda.current_stream(self.device) if stream is None else stream
-        parts = self.add_rows(resid, rows, st) if rows else None
+        iteration, rank, parts = int(iteration), int(rank), None
+        if rows:
+            checked = self.check_rows(resid, grad, rows)
+            if iteration < 0 or not -1 <= rank < self.N:
+                raise ValueError("iteration at least 0 and a rank in [-1, %d) expected" % self.N)
+            parts = self._issue_rows(resid, checked, st)
         status = deft.lib().deft_step_part(
             ctypes.c_void_p(resid.data_ptr()), None if grad is None else ctypes.c_void_p(grad.data_ptr()), self.n_g,
             None if parts is None else ctypes.c_void_p(parts.ctypes.data), 0 if parts is None else len(parts),
-            f["ls_h"], f["ls_d"], self.L, self.N, int(self.k), int(self.mode), int(self.cost_model), int(iteration),
-            int(rank), f["norms_d"], f["norms_h"], f["k_l"], f["sum_k"], f["bins"], f["load"], f["plan_h"],
+            f["ls_h"], f["ls_d"], self.L, self.N, int(self.k), int(self.mode), int(self.cost_model), iteration,
+            rank, f["norms_d"], f["norms_h"], f["k_l"], f["sum_k"], f["bins"], f["load"], f["plan_h"],
             f["plan_cap"], f["plan_d"], f["val_d"], f["idx_d"], f["out_cap"], f["ws"], f["ws_bytes"], ev,
             ctypes.c_void_p(st.cuda_stream))
         deft._check("deft_step_part", status, allow_warn=True)
@@ -225,6 +254,8 @@ class DeftStep:
              per_rank: bool = False, rows: Sequence[RowGradient] = ()):
         """accumulate + norms -> plan -> (selection, residual update) for every rank.  Returns the plan and,
         per rank, views of its selected (values, indices)."""
+        if rows and iteration < 0:
+            raise ValueError("iteration at least 0 expected")
         norms = self.layer_norms(resid, grad, rows)
         plan = self.plan(norms, iteration)
         self.select_and_update_all(resid, plan, events, per_rank)

@@ -80,6 +80,12 @@ class MultiWorkerSim:
         `pipeline.RowGradient`s; its gradient is not read in their parts.  Returns
         (actual density, error after the update)."""
         ds, N, t = self.ds, self.N, self.iteration
+        if rows:                                                   # all workers' arguments before any residual changes
+            if len(rows) < N or len(grads) < N:
+                raise ValueError("grads and rows of all %d workers expected" % N)
+            rows = [list(rows[r] or ()) for r in range(N)]
+            for r in range(N):
+                ds.check_rows(self.e[r], grads[r], rows[r])
         norms_all = []
         for r in range(N):                                         # line 5: acc_r = e_r + g_r (in place)
             norms_all.append(ds.layer_norms(self.e[r], grads[r], rows[r] if rows else ()).copy())

@@ -1,0 +1,54 @@
+"""The checks of a step with row gradients, without a GPU: the device calls are replaced by a recorder, and a refused call
+must not have issued any."""
+from dataclasses import replace
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2307_03500_b200 import build as deft_build
+
+deft_build.build()
+from paper_2307_03500_b200 import deft  # noqa: E402
+from paper_2307_03500_b200.pipeline import DeftStep, RowGradient  # noqa: E402
+
+VOCAB, WIDTH, N_TOKENS = 30, 8, 6
+
+
+@pytest.fixture
+def step(monkeypatch):
+    """A DeftStep over [12, VOCAB * WIDTH, 100] elements on the host; step.calls: the gradients that would have been added."""
+    sizes = [12, VOCAB * WIDTH, 100]
+    ds = object.__new__(DeftStep)
+    ds.device, ds.N, ds.n_g = torch.device("cpu"), 2, sum(sizes)
+    ds.tensor_start = np.concatenate([[0], np.cumsum(sizes)])
+    ds.layer_start_d = torch.from_numpy(ds.tensor_start)
+    ds._ws_rows = None
+    ds.calls = []
+    monkeypatch.setattr(deft, "_device", lambda *tensors: 0)
+    monkeypatch.setattr(deft, "deft_embed_grad", lambda grad_out, ids, grad, ws, **kw: ds.calls.append((grad, ws, kw)))
+    return ds
+
+
+def _row(**kw):
+    row = RowGradient(1, torch.arange(N_TOKENS), torch.ones(N_TOKENS, WIDTH), scale=0.5, p=0.25, seed=3)
+    return replace(row, **kw)
+
+
+def test_good_rows_reach_the_call(step):
+    e = torch.zeros(step.n_g)
+    parts = step.add_rows(e, [_row(), _row(seed=-1, offset=2 ** 64 + 5)])
+    assert parts.tolist() == [[12, 12 + VOCAB * WIDTH]] and len(step.calls) == 2
+    assert all(g.data_ptr() == e[12:].data_ptr() and tuple(g.shape) == (VOCAB, WIDTH) and kw["accumulate"] for g, _, kw in step.calls)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(seed="x"), dict(offset=None), dict(skip_id="x"), dict(scale=None), dict(scale=float("inf")), dict(p=1.0), dict(p=float("nan")),
+    dict(tensor=3), dict(tensor=0), dict(ids=torch.arange(5)), dict(grad_out=torch.ones(N_TOKENS, WIDTH).double()),
+    dict(grad_out=torch.empty(2 ** 30 + 8, dtype=torch.bfloat16).as_strided((2, WIDTH), (2 ** 30, 1)), ids=torch.arange(2)),
+], ids=lambda kw: "-".join(kw))
+def test_a_refused_row_leaves_the_rows_before_it_out(step, bad):
+    """What the second gradient's own call would refuse is refused before the first one is added."""
+    with pytest.raises((ValueError, TypeError, deft.DeftError)):
+        step.add_rows(torch.zeros(step.n_g), [_row(), _row(**bad)])
+    assert step.calls == []
