@@ -76,7 +76,6 @@ class DeftStep:
         self._plan_pin = torch.empty(nbytes, dtype=torch.uint8).pin_memory()
         self.plan_h = self._plan_pin.numpy()
         self.plan_d = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self._ws_rows: Optional[torch.Tensor] = None   # workspace of the row-sparse gradients, grown when needed
 
     # -- before step 1: row-sparse gradients straight into the residual (device) --------------
     def _row_calls(self, resid: torch.Tensor, rows: Sequence[RowGradient]):
@@ -124,16 +123,18 @@ class DeftStep:
 
     def add_rows(self, resid: torch.Tensor, rows: Sequence[RowGradient], stream=None) -> np.ndarray:
         """Adds every RowGradient to its table's part of `resid`, in order; returns the parts that now hold their
-        gradient as int64 [parts, 2] (ascending).  A call that is refused has added nothing."""
+        gradient as int64 [parts, 2] (ascending).  A call that is refused has added nothing.  Does not wait for the GPU;
+        calls on several streams may overlap (on residuals of their own)."""
         return self._issue_rows(resid, self._row_calls(resid, rows), stream) if rows else np.empty((0, 2), dtype=np.int64)
 
     def _issue_rows(self, resid: torch.Tensor, checked, stream=None) -> np.ndarray:
         calls, parts, need = checked
-        if self._ws_rows is None or self._ws_rows.numel() < need:
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                self._ws_rows = torch.empty(need, dtype=torch.uint8, device=self.device)
+        # A workspace of this call's own, from the allocator's blocks of the stream it runs on: nothing waits for the GPU here,
+        # so calls on other streams, and replays of a captured call, may still be at work in theirs.
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            ws = torch.empty(need, dtype=torch.uint8, device=resid.device)
         for r, a, b, width, numbers in calls:
-            deft.deft_embed_grad(r.grad_out, r.ids, resid[a:b].view(-1, width), self._ws_rows, accumulate=True,
+            deft.deft_embed_grad(r.grad_out, r.ids, resid[a:b].view(-1, width), ws, accumulate=True,
                                  offset_d=r.offset_d, stream=stream, **numbers)
         return np.array(sorted(parts), dtype=np.int64).reshape(-1, 2)
 
@@ -233,7 +234,7 @@ class DeftStep:
             checked = self.check_rows(resid, grad, rows)
             if iteration < 0 or not -1 <= rank < self.N:
                 raise ValueError("iteration at least 0 and a rank in [-1, %d) expected" % self.N)
-            parts = self._issue_rows(resid, checked, st)
+            parts = self._issue_rows(resid, checked, stream)
         status = deft.lib().deft_step_part(
             ctypes.c_void_p(resid.data_ptr()), None if grad is None else ctypes.c_void_p(grad.data_ptr()), self.n_g,
             None if parts is None else ctypes.c_void_p(parts.ctypes.data), 0 if parts is None else len(parts),

@@ -91,3 +91,65 @@ def test_refused_simulation_leaves_every_residual(deft):
         assert all(not e.any() for e in sim.e)
     assert sim.step([g0, g1], [[row], [row]]) == other.step([g0, g1], [[row], [row]])
     assert all(torch.equal(a, b) for a, b in zip(sim.e, other.e))
+
+
+def _row_batch(rng, n, vocab, width):
+    from paper_2307_03500_b200.pipeline import RowGradient
+    return RowGradient(0, torch.from_numpy(rng.integers(0, vocab, n)).cuda(),
+                       torch.from_numpy(rng.standard_normal((n, width)).astype(np.float32)).cuda(), p=0.1, seed=n)
+
+
+def _added(deft, ds, row, vocab, width):
+    """What add_rows leaves in a residual of zeros."""
+    want = torch.zeros(ds.n_g, device="cuda")
+    deft.deft_embed_grad(row.grad_out, row.ids, want[:vocab * width].view(vocab, width),
+                         deft.alloc_embed_workspace(row.ids.numel(), vocab, width), accumulate=True, p=row.p, seed=row.seed)
+    return want
+
+
+def test_rows_added_on_several_streams_at_once(deft):
+    """Calls of different sizes on three streams without a wait between them, each on a residual of its own."""
+    from paper_2307_03500_b200.pipeline import DeftStep
+    rng = np.random.default_rng(57)
+    vocab, width = 4000, 256
+    ds = DeftStep([vocab * width, 1000], 2, 0.01)
+    batches = [[_row_batch(rng, n, vocab, width) for n in sizes] for sizes in ((700, 20000, 64), (30000, 5, 3000), (64, 9000, 30000))]
+    want = [[_added(deft, ds, row, vocab, width) for row in rows] for rows in batches]
+    got = [[torch.zeros_like(w) for w in ws] for ws in want]
+    streams = [torch.cuda.Stream() for _ in batches]
+    torch.cuda.synchronize()
+    for i in range(3):
+        for s, rows, out in zip(streams, batches, got):
+            ds.add_rows(out[i], [rows[i]], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for ws, gs in zip(want, got) for a, b in zip(ws, gs))
+
+
+def test_captured_rows_and_larger_calls_after(deft):
+    """A captured call keeps its workspace when later, larger calls on the same object need more."""
+    from paper_2307_03500_b200.pipeline import DeftStep
+    rng = np.random.default_rng(59)
+    vocab, width = 2000, 136
+    ds = DeftStep([vocab * width, 1000], 2, 0.01)
+    small, large = _row_batch(rng, 900, vocab, width), _row_batch(rng, 40000, vocab, width)
+    want_small, want_large = _added(deft, ds, small, vocab, width), _added(deft, ds, large, vocab, width)
+    a, b = torch.zeros(ds.n_g, device="cuda"), torch.zeros(ds.n_g, device="cuda")
+    graphs = []
+    for out in (a, b):
+        graph = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            out.zero_()
+            ds.add_rows(out, [small])
+        graphs.append(graph)
+        torch.cuda.synchronize()
+    for _ in range(2):
+        e = torch.zeros(ds.n_g, device="cuda")
+        ds.add_rows(e, [large])
+        junk = [torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]   # over anything that was let go
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(e, want_large) and torch.equal(a, want_small) and torch.equal(b, want_small)
+        del junk

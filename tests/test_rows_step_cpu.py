@@ -23,7 +23,6 @@ def step(monkeypatch):
     ds.device, ds.N, ds.n_g = torch.device("cpu"), 2, sum(sizes)
     ds.tensor_start = np.concatenate([[0], np.cumsum(sizes)])
     ds.layer_start_d = torch.from_numpy(ds.tensor_start)
-    ds._ws_rows = None
     ds.calls = []
     monkeypatch.setattr(deft, "_device", lambda *tensors: 0)
     monkeypatch.setattr(deft, "deft_embed_grad", lambda grad_out, ids, grad, ws, **kw: ds.calls.append((grad, ws, kw)))
@@ -52,3 +51,36 @@ def test_a_refused_row_leaves_the_rows_before_it_out(step, bad):
     with pytest.raises((ValueError, TypeError, deft.DeftError)):
         step.add_rows(torch.zeros(step.n_g), [_row(), _row(**bad)])
     assert step.calls == []
+
+
+def test_no_call_uses_the_workspace_of_another_stream(step, monkeypatch):
+    """add_rows does not wait for the GPU: a workspace that two streams share, or one that is let go on another stream than it is
+    used on, would be written by two calls at once."""
+    current, made, empty = ["default"], {}, torch.empty
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            current.append(self.stream)
+
+        def __exit__(self, *exc):
+            current.pop()
+
+    def recorded(*args, **kw):
+        t = empty(*args, **kw)
+        made[t.data_ptr()] = current[-1]
+        return t
+
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch, "empty", recorded)
+    e, more = torch.zeros(step.n_g), _row(ids=torch.arange(200) % VOCAB, grad_out=torch.ones(200, WIDTH))
+    used = {}
+    for stream, row in (("A", _row()), (None, _row()), ("B", more), ("A", _row()), (None, more), ("A", more)):
+        step.calls.clear()
+        step.add_rows(e, [row, row], stream=stream)
+        for _, ws, kw in step.calls:
+            assert made[ws.data_ptr()] == (stream or "default") and kw["stream"] == stream
+            used.setdefault(ws.data_ptr(), (ws, set()))[1].add(stream)
+    assert all(len(streams) == 1 for _, streams in used.values())
