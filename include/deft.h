@@ -497,6 +497,7 @@ DEFT_API deft_status deft_step_part(float* resid_acc_d, const float* grad_d, int
  *   table_d  [rows, width], table_type; ids_d int32 or int64 (id_bytes 4 or 8)
  *   pos_d    NULL, or [pos_rows, width] of table_type: position rows, added before dropout
  *   out_d    [n, width], out_type; must not overlap the inputs.  n may be 0.
+ *   scale    finite in fp32
  * Errors: INVALID_ARG, TOO_LARGE (n, rows or width beyond 2^31 - 1), CUDA.
  */
 DEFT_API deft_status deft_embed(const void* table_d, int32_t table_type, int64_t rows, int64_t width,
@@ -517,6 +518,7 @@ DEFT_API deft_status deft_embed(const void* table_d, int32_t table_type, int64_t
  *               tokens (one fp32 round-to-nearest add per element), the others are neither read nor
  *               written: the residual itself (see deft_layer_norms_part), or a gradient vector that holds
  *               a tied output layer's gradient.  Must not overlap the inputs.
+ *   scale       finite in fp32, and times the gain of the kept elements too
  *   skip_id     a row that gets no gradient; -1: none
  *   ws_d        deft_embed_workspace_bytes(n, rows, width), 256-byte aligned; holds nothing between
  *               calls.  Calls that share a workspace must not overlap on the GPU.

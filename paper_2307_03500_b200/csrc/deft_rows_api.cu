@@ -10,6 +10,7 @@ constexpr int64_t kMaxTokens = 2147483647LL;   // token positions, rows and colu
 constexpr int64_t kMaxWidth = (1LL << 30) - 1;   // of the gradient's matrices: a row's bytes are a 32-bit number
 
 bool type_ok(int32_t t) { return t == DEFT_F32 || t == DEFT_BF16 || t == DEFT_F16; }
+bool fits_f32(double x) { return std::isfinite((float)x); }   // what the kernels multiply by is fp32: no product with an infinity
 bool elem_aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // A [rows, cols] matrix of a type: its pitch reaches over a row, its base is aligned to the element.
@@ -44,7 +45,7 @@ deft_status deft_embed(const void* table_d, int32_t table_type, int64_t rows, in
                        int64_t ld_pos, double p, uint64_t seed, uint64_t offset, const uint64_t* offset_d, void* out_d,
                        int32_t out_type, int64_t ld_out, void* stream) {
     if (n < 0 || rows < 1 || width < 1 || !type_ok(table_type) || !type_ok(out_type) || (id_bytes != 4 && id_bytes != 8) ||
-        !std::isfinite(scale))
+        !fits_f32(scale))
         return DEFT_ERR_INVALID_ARG;
     EmbedArgs a{};
     double gain;
@@ -79,12 +80,12 @@ deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_type, int64
                             int32_t id_bytes, int64_t n, int64_t rows, int64_t width, int64_t skip_id, double scale, double p,
                             uint64_t seed, uint64_t offset, const uint64_t* offset_d, float* grad_d, int32_t accumulate,
                             void* ws_d, size_t ws_bytes, void* stream) {
-    if (n < 0 || rows < 1 || width < 1 || !type_ok(grad_out_type) || (id_bytes != 4 && id_bytes != 8) || !std::isfinite(scale) ||
-        !grad_d || !elem_aligned(grad_d, 4) || !ws_d || !elem_aligned(ws_d, 256))
+    if (n < 0 || rows < 1 || width < 1 || !type_ok(grad_out_type) || (id_bytes != 4 && id_bytes != 8) || !grad_d ||
+        !elem_aligned(grad_d, 4) || !ws_d || !elem_aligned(ws_d, 256))
         return DEFT_ERR_INVALID_ARG;
     EmbedGradArgs a{};
     double gain;
-    if (!drop_args(p, seed, offset, offset_d, &a.drop, &gain)) return DEFT_ERR_INVALID_ARG;
+    if (!drop_args(p, seed, offset, offset_d, &a.drop, &gain) || !fits_f32(scale * gain)) return DEFT_ERR_INVALID_ARG;
     if (n > kMaxTokens || width > kMaxWidth || rows > DEFT_EMBED_MAX_ROWS || (n > 0 && ld_grad_out > kMaxWidth)) return DEFT_ERR_TOO_LARGE;
     if (n > 0 && (!matrix_ok(grad_out_d, grad_out_type, n, width, ld_grad_out) || !ids_d || !elem_aligned(ids_d, (size_t)id_bytes)))
         return DEFT_ERR_INVALID_ARG;

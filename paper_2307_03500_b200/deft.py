@@ -7,6 +7,7 @@ if the CUDA library is missing or fails to load, importing a device call raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Tuple
 
@@ -699,6 +700,12 @@ def _offset(offset_d) -> Optional[int]:
     if offset_d.numel() != 1 or offset_d.dtype not in (torch.int64, torch.uint64):
         raise ValueError("offset_d: one 64-bit integer")
     return offset_d.data_ptr()
+
+
+def _factor_fits(scale: float, p: float) -> bool:
+    """Whether scale times the gain of the elements that dropout keeps is finite in fp32 (0 <= p < 1)."""
+    x = scale * (65536.0 / (65536.0 - min(65535.0, math.floor(p * 65536.0 + 0.5))))
+    return abs(x) < 2.0 ** 128 - 2.0 ** 103          # from there on the nearest fp32 number is an infinity
 
 
 _U64 = (1 << 64) - 1

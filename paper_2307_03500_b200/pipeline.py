@@ -100,8 +100,8 @@ class DeftStep:
             if pitch >= 1 << 30:
                 raise ValueError("grad_out: rows less than 2^30 elements apart expected")
             numbers = dict(skip_id=index(r.skip_id), scale=float(r.scale), p=float(r.p), seed=index(r.seed), offset=index(r.offset))
-            if not (0.0 <= numbers["p"] < 1.0 and math.isfinite(numbers["scale"])):
-                raise ValueError("p in [0, 1) and a finite scale expected")
+            if not (0.0 <= numbers["p"] < 1.0 and deft._factor_fits(numbers["scale"], numbers["p"])):
+                raise ValueError("p in [0, 1) and a scale that is finite in fp32, times the gain of p too, expected")
             size = deft.deft_embed_workspace_bytes(n, (b - a) // width, width)
             if size == 0:
                 raise deft.DeftError("deft_embed_workspace_bytes", deft.ERR_INVALID_ARG)

@@ -84,3 +84,18 @@ def test_no_call_uses_the_workspace_of_another_stream(step, monkeypatch):
             assert made[ws.data_ptr()] == (stream or "default") and kw["stream"] == stream
             used.setdefault(ws.data_ptr(), (ws, set()))[1].add(stream)
     assert all(len(streams) == 1 for _, streams in used.values())
+
+
+@pytest.mark.parametrize("scale,p,ok", [(1e39, 0.0, False), (-1e308, 0.0, False), (2.0 ** 128 - 2.0 ** 103, 0.0, False), (2.0 ** 128 - 2.0 ** 104, 0.0, True),
+                                        (3e38, 0.25, False), (-2.5e38, 0.25, True), (1e35, 0.9999, False), (1e33, 1 - 1e-9, True), (1e34, 1 - 1e-9, False)])
+def test_scales_that_overflow_fp32_are_refused_before_the_first_row(step, scale, p, ok):
+    """The same answer as the call's own, whose checks do not need a device when there are no tokens."""
+    status = deft.lib().deft_embed_grad(None, deft.F32, 0, None, 8, 0, VOCAB, WIDTH, -1, scale, p, 0, 0, None, 0x10000, 1, 0x10000, 1 << 30, None)
+    assert status == (deft.OK if ok else deft.ERR_INVALID_ARG)
+    rows = [_row(), _row(scale=scale, p=p)]
+    if ok:
+        step.add_rows(torch.zeros(step.n_g), rows)
+    else:
+        with pytest.raises(ValueError):
+            step.add_rows(torch.zeros(step.n_g), rows)
+    assert len(step.calls) == (2 if ok else 0)
