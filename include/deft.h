@@ -535,7 +535,8 @@ DEFT_API deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_ty
 
 /*
  * Dropout of a [rows, cols] matrix: y = add + D(x).  Its gradient is the same call on the incoming
- * gradient with add = NULL.  y may be x (same type and pitch) or add, but must not overlap them otherwise.
+ * gradient with add = NULL.  y may be x (same type and pitch) or add (same pitch); a y that overlaps them otherwise is
+ * refused.
  *   add_d  NULL, or [rows, cols] of y_type (a residual stream)
  * Errors: INVALID_ARG, TOO_LARGE (rows or cols beyond 2^31 - 1), CUDA.
  */

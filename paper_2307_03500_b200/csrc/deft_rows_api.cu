@@ -1,5 +1,6 @@
 // C-ABI entry points of the row operators: argument checks and launches.
 #include <cmath>
+#include <utility>
 
 #include "deft_rows.cuh"
 
@@ -16,6 +17,38 @@ bool elem_aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintpt
 // A [rows, cols] matrix of a type: its pitch reaches over a row, its base is aligned to the element.
 bool matrix_ok(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t ld) {
     return p && ld >= cols && ld <= (1LL << 60) / rows && elem_aligned(p, type_bytes(type));   // offsets fit 64 bits
+}
+
+// Rows of a matrix in bytes.
+struct Span { uintptr_t base; uint64_t row, pitch; };
+Span span_of(const void* p, int32_t type, int64_t cols, int64_t ld, int64_t rows) {
+    const uint64_t row = (uint64_t)cols * type_bytes(type);
+    return Span{reinterpret_cast<uintptr_t>(p), row, rows == 1 ? row : (uint64_t)ld * type_bytes(type)};
+}
+
+// Whether two matrices of `rows` rows share a byte of their elements (columns of one buffer, or rows between each other's,
+// do not).
+bool overlap(Span a, Span b, int64_t rows) {
+    if (a.base > b.base) std::swap(a, b);
+    const uint64_t apart = b.base - a.base, last = (uint64_t)(rows - 1);
+    if (apart >= last * a.pitch + a.row) return false;
+    if (a.pitch == b.pitch) {            // every row of b lies `at` behind a's row `below` further down
+        const uint64_t below = apart / a.pitch, at = apart % a.pitch;
+        return at < a.row || (at + b.row > a.pitch && below < last);
+    }
+    // both lists of rows ascend: the later of two rows that do not meet waits for the other list's next one
+    for (uint64_t i = 0, j = 0; i <= last && j <= last;) {
+        const uint64_t x = i * a.pitch, y = apart + j * b.pitch;
+        if (x + a.row <= y) ++i;
+        else if (y + b.row <= x) ++j;
+        else return true;
+    }
+    return false;
+}
+
+// Whether y may be written while `in` is read: apart, or element for element the same place.
+bool in_place_or_apart(Span y, Span in, bool same_type, int64_t rows) {
+    return (y.base == in.base && y.pitch == in.pitch && same_type) || !overlap(y, in, rows);
 }
 
 // Fills d from the dropout arguments; false if they are invalid.  p is rounded to a multiple of 2^-16 (at most
@@ -116,6 +149,10 @@ deft_status deft_dropout(const void* x_d, int32_t x_type, int64_t ld_x, const vo
     if (rows > kMaxTokens || cols > kMaxTokens) return DEFT_ERR_TOO_LARGE;
     if (!matrix_ok(x_d, x_type, rows, cols, ld_x) || !matrix_ok(y_d, y_type, rows, cols, ld_y) ||
         (add_d && !matrix_ok(add_d, y_type, rows, cols, ld_add)))
+        return DEFT_ERR_INVALID_ARG;
+    const Span y = span_of(y_d, y_type, cols, ld_y, rows);
+    if (!in_place_or_apart(y, span_of(x_d, x_type, cols, ld_x, rows), x_type == y_type, rows) ||
+        (add_d && !in_place_or_apart(y, span_of(add_d, y_type, cols, ld_add, rows), true, rows)))
         return DEFT_ERR_INVALID_ARG;
     a.x = x_d;
     a.ld_x = ld_x;

@@ -153,3 +153,41 @@ def test_captured_rows_and_larger_calls_after(deft):
         torch.cuda.synchronize()
         assert torch.equal(e, want_large) and torch.equal(a, want_small) and torch.equal(b, want_small)
         del junk
+
+
+def test_dropout_beside_its_inputs_in_one_buffer(deft):
+    """Outputs that are x or add element for element, or lie between or right behind their rows, give what separate ones give."""
+    rows, cols, p = 50, 24, 0.3
+    g = torch.Generator(device="cuda").manual_seed(5)
+    fresh = lambda *shape: torch.randn(*shape, device="cuda", generator=g)  # noqa: E731
+
+    def check(x, y, add=None):
+        want = torch.empty((rows, cols), dtype=y.dtype, device="cuda")
+        deft.deft_dropout(x.clone(), want, add=None if add is None else add.clone(), p=p, seed=9)
+        deft.deft_dropout(x, y, add=add, p=p, seed=9)
+        assert torch.equal(y, want)
+
+    buf = fresh(2 * rows + 1, 3 * cols)
+    left, middle, right = (buf[:rows, i * cols:(i + 1) * cols] for i in range(3))
+    check(left, middle, right)                                       # columns side by side
+    check(right, left)
+    half = buf.view(torch.bfloat16)[:rows, 3 * cols:4 * cols]        # the same pitch in bytes, other elements
+    check(left, half)
+    check(left, buf[1:2 * rows + 1:2, cols:2 * cols])                # twice the pitch, between the rows
+    check(buf[:2 * rows:2, :cols], buf[1:2 * rows + 1:2, :cols], buf[1:2 * rows + 1:2, 2 * cols:])
+    check(left, left)
+    check(left, right, right)
+    check(left, left, left)
+    flat = fresh(2 * rows * cols)
+    x, y = flat[:rows * cols].view(rows, cols), flat[rows * cols:].view(rows, cols)
+    check(x, y)                                                      # right behind, and right before
+    check(y, x)
+    one = fresh(1, 3 * cols)
+    out = torch.empty((1, cols), device="cuda")
+    deft.deft_dropout(one[:, :cols], out, p=p, seed=9)
+    deft.deft_dropout(one[:, :cols], one[:, :cols], p=p, seed=9)     # a single row has no pitch
+    assert torch.equal(one[:, :cols], out)
+    with pytest.raises(deft.DeftError):
+        deft.deft_dropout(buf[:rows, :cols], buf[:rows, cols // 2:cols // 2 + cols], p=p)
+    with pytest.raises(deft.DeftError):
+        deft.deft_dropout(left, buf.view(torch.bfloat16)[:rows, :cols], p=p)

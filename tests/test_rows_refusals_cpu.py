@@ -26,3 +26,18 @@ def test_scales_that_overflow_with_the_gain():
                          (1e35, 0.99, True), (-3e38, 0.25, False)]:
         assert _grad(scale=scale, p=p, **nothing) == (deft.OK if ok else deft.ERR_INVALID_ARG)
     assert _embed(n=0, scale=FLT_MAX, table=None, ids=None, out=None) == deft.OK
+
+
+@pytest.mark.parametrize("kw", [
+    dict(ty=1), dict(tx=1), dict(tx=1, ty=2),                                   # x's place, but other elements
+    dict(ld_x=9), dict(ld_y=9), dict(ld_y=16),                                  # ... or another pitch
+    dict(y=A + 4), dict(x=A + 4), dict(y=A + 3 * 32 + 28), dict(x=A + 3 * 32),  # shifted by an element, or as far as the last row
+    dict(y=A + 40, ld_x=16, ld_y=16), dict(y=A + 64 + 28, ld_x=16, ld_y=16),    # the same pitch: into its own row's end, a later row's start
+    dict(y=A + 4, rows=1), dict(y=A, ty=1, rows=1, ld_x=100),
+    dict(x=2 * A, add=A, ld_add=9), dict(x=2 * A, add=A, ld_add=8, y=A + 4), dict(x=2 * A, add=A + 64, ld_add=8),
+    dict(y=A + 32, ld_x=16, ld_y=24),                                           # different pitches: y's second row is x's third
+    dict(rows=2 ** 20, y=A + 4 * (2 ** 23 - 1), ld_x=8, ld_y=9),
+], ids=lambda kw: ",".join("%s=%s" % i for i in kw.items()))
+def test_dropout_refuses_outputs_that_overlap_its_inputs(kw):
+    """y is x or add, element for element, or apart from both: anything else would be written before another thread reads it."""
+    assert _dropout(**kw) == deft.ERR_INVALID_ARG
