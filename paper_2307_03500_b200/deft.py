@@ -308,7 +308,7 @@ def _parts(parts):
 
 
 def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, stream=None) -> None:
-    """deft_layer_norms of a vector whose parts [(begin, end), ...] hold their gradient already."""
+    """deft_layer_norms of a vector whose parts [(begin, end), ...] hold their gradient already, on the tensors' device."""
     import torch
     n_g = resid_acc.numel()
     L = layer_start_d.numel() - 1
@@ -317,10 +317,9 @@ def deft_layer_norms_part(resid_acc, grad, parts, layer_start_d, norms_d, ws, st
     if norms_d.numel() < L:
         raise ValueError("norms_d too small")
     pt, n_parts = _parts(parts)
-    _check("deft_layer_norms_part",
-           lib().deft_layer_norms_part(_dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g, pt, n_parts,
-                                       _dp(layer_start_d, torch.int64), L, _dp(norms_d, torch.float64),
-                                       _dp(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    _call("deft_layer_norms_part", _device(resid_acc, grad, layer_start_d, norms_d, ws), stream,
+          _dp(resid_acc, torch.float32), _dp(grad, torch.float32), n_g, pt, n_parts, _dp(layer_start_d, torch.int64), L,
+          _dp(norms_d, torch.float64), _dp(ws), ws.numel() * ws.element_size())
 
 
 def deft_layer_norms_static(resid_acc, grad, layer_start_d, norms_d, stream=None) -> None:

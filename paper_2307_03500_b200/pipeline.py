@@ -147,7 +147,7 @@ class DeftStep:
         parts = self._issue_rows(resid, self.check_rows(resid, grad, rows)) if rows else ()
         deft.deft_layer_norms_part(resid, grad, parts, self.layer_start_d, self.norms_d, self.ws)
         self.norms_h.copy_(self.norms_d, non_blocking=True)
-        torch.cuda.current_stream().synchronize()
+        torch.cuda.current_stream(self.norms_d.device).synchronize()
         return self.norms_h.numpy()
 
     # -- steps 2 and 3: local k and bins (host) ---------------------------------------------

@@ -99,3 +99,43 @@ def test_scales_that_overflow_fp32_are_refused_before_the_first_row(step, scale,
         with pytest.raises(ValueError):
             step.add_rows(torch.zeros(step.n_g), rows)
     assert len(step.calls) == (2 if ok else 0)
+
+
+class _OnDevice:
+    """What the binding asks of a CUDA tensor."""
+    is_cuda = True
+
+    def __init__(self, device, dtype, n=8):
+        self.device, self.dtype, self.n = device, dtype, n
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 8 if self.dtype in (torch.int64, torch.float64) else 4
+
+    def data_ptr(self):
+        return 0x10000
+
+
+def test_norms_with_parts_on_the_device_of_the_tensors(monkeypatch):
+    """The call runs on the tensors' one device, which need not be the current one, and on that device's stream."""
+    issued = []
+    monkeypatch.setattr(deft, "_call", lambda name, device, stream, *args: issued.append((name, device, stream, args)), raising=False)
+    make = lambda devices: [_OnDevice(d, t) for d, t in  # noqa: E731
+                            zip(devices, (torch.float32, torch.float32, torch.int64, torch.float64, torch.uint8))]
+    for wrong in range(5):
+        e, g, start, norms, ws = make([2 if i == wrong else 1 for i in range(5)])
+        with pytest.raises(ValueError):
+            deft.deft_layer_norms_part(e, g, [(0, 4)], start, norms, ws)
+    assert not issued
+    e, g, start, norms, ws = make([1] * 5)
+    deft.deft_layer_norms_part(e, g, [(0, 4)], start, norms, ws, stream="s")
+    deft.deft_layer_norms_part(e, None, [], start, norms, ws)
+    assert [i[:3] for i in issued] == [("deft_layer_norms_part", 1, "s"), ("deft_layer_norms_part", 1, None)]
