@@ -79,38 +79,43 @@ class DeftStep:
 
     # -- before step 1: row-sparse gradients straight into the residual (device) --------------
     def _row_calls(self, resid: torch.Tensor, rows: Sequence[RowGradient]):
-        """What `_issue_rows` takes: per RowGradient its tensors and numbers, the parts, the workspace's bytes.  Refuses
-        whatever the calls themselves would refuse, so that none of them does after an earlier one has added its rows."""
+        """What `_issue_rows` takes: every RowGradient (whose tensors it keeps) and the arguments of its `deft_embed_grad`, the
+        parts, the workspace's bytes.
+        Refuses whatever those calls would refuse, so that none of them does after an earlier one has added its rows."""
         calls, parts, need = [], set(), 0
         if resid.dim() != 1 or resid.numel() != self.n_g or resid.dtype != torch.float32 or not resid.is_contiguous():
             raise ValueError("resid: a flat float32 tensor of n_g elements")
+        base = resid.data_ptr()
         for r in rows:
+            grad_out, ids, p = r.grad_out, r.ids, float(r.p)
             if not 0 <= r.tensor < len(self.tensor_start) - 1:
                 raise ValueError("no tensor %d" % r.tensor)
             a, b = int(self.tensor_start[r.tensor]), int(self.tensor_start[r.tensor + 1])
-            n, width, pitch = deft._matrix(r.grad_out, "grad_out")
-            deft._type(r.grad_out), deft._ids(r.ids), deft._offset(r.offset_d)
-            deft._device(resid, self.layer_start_d, r.grad_out, r.ids, r.offset_d)
-            if any(t is not None and t.data_ptr() % t.element_size() for t in (resid, r.grad_out, r.ids, r.offset_d)):
+            n, width, pitch = deft._matrix(grad_out, "grad_out")
+            kind, id_bytes, offset_d = deft._type(grad_out), deft._ids(ids), deft._offset(r.offset_d)
+            deft._device(resid, self.layer_start_d, grad_out, ids, r.offset_d)
+            dy, ids_d = grad_out.data_ptr(), ids.data_ptr()
+            if base % 4 or dy % grad_out.element_size() or ids_d % id_bytes or (offset_d or 0) % 8:
                 raise ValueError("tensors that start on a boundary of their elements expected")
             if width < 1 or (b - a) % width:
                 raise ValueError("tensor %d has no rows of %d elements" % (r.tensor, width))
-            if r.ids.numel() != n:
+            if ids.numel() != n:
                 raise ValueError("one id for every row of grad_out expected")
             if pitch >= 1 << 30:
                 raise ValueError("grad_out: rows less than 2^30 elements apart expected")
-            numbers = dict(skip_id=index(r.skip_id), scale=float(r.scale), p=float(r.p), seed=index(r.seed), offset=index(r.offset))
-            if not (0.0 <= numbers["p"] < 1.0 and deft._factor_fits(numbers["scale"], numbers["p"])):
+            scale = float(r.scale)
+            if not (0.0 <= p < 1.0 and deft._factor_fits(scale, p)):
                 raise ValueError("p in [0, 1) and a scale that is finite in fp32, times the gain of p too, expected")
             size = deft.deft_embed_workspace_bytes(n, (b - a) // width, width)
             if size == 0:
                 raise deft.DeftError("deft_embed_workspace_bytes", deft.ERR_INVALID_ARG)
             need = max(need, size)
             parts.add((a, b))
-            calls.append((r, a, b, width, numbers))
+            calls.append((r, (dy, kind, pitch, ids_d, id_bytes, n, (b - a) // width, width, index(r.skip_id), scale, p,
+                              index(r.seed) & deft._U64, index(r.offset) & deft._U64, offset_d, base + 4 * a, 1)))
         if len(parts) > deft.MAX_PARTS:
             raise ValueError("at most %d tensors may have their gradient by rows" % deft.MAX_PARTS)
-        return calls, parts, need
+        return calls, sorted(parts), need
 
     def check_rows(self, resid: torch.Tensor, grad: Optional[torch.Tensor], rows: Sequence[RowGradient]):
         """Refuses what a step of these vectors and rows would refuse, before anything is added to `resid`."""
@@ -125,18 +130,19 @@ class DeftStep:
         """Adds every RowGradient to its table's part of `resid`, in order; returns the parts that now hold their
         gradient as int64 [parts, 2] (ascending).  A call that is refused has added nothing.  Does not wait for the GPU;
         calls on several streams may overlap (on residuals of their own)."""
-        return self._issue_rows(resid, self._row_calls(resid, rows), stream) if rows else np.empty((0, 2), dtype=np.int64)
+        parts = self._issue_rows(resid, self._row_calls(resid, rows), stream) if rows else []
+        return np.array(parts, dtype=np.int64).reshape(-1, 2)
 
-    def _issue_rows(self, resid: torch.Tensor, checked, stream=None) -> np.ndarray:
+    def _issue_rows(self, resid: torch.Tensor, checked, stream=None):
         calls, parts, need = checked
         # A workspace of this call's own, from the allocator's blocks of the stream it runs on: nothing waits for the GPU here,
         # so calls on other streams, and replays of a captured call, may still be at work in theirs.
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             ws = torch.empty(need, dtype=torch.uint8, device=resid.device)
-        for r, a, b, width, numbers in calls:
-            deft.deft_embed_grad(r.grad_out, r.ids, resid[a:b].view(-1, width), ws, accumulate=True,
-                                 offset_d=r.offset_d, stream=stream, **numbers)
-        return np.array(sorted(parts), dtype=np.int64).reshape(-1, 2)
+        device, ws_d = resid.get_device(), ws.data_ptr()
+        for _, args in calls:
+            deft._call("deft_embed_grad", device, stream, *args, ws_d, need)
+        return parts
 
     # -- step 1: accumulate + norms (device) ------------------------------------------------
     def layer_norms(self, resid: torch.Tensor, grad: Optional[torch.Tensor], rows: Sequence[RowGradient] = ()) -> np.ndarray:
@@ -234,7 +240,7 @@ class DeftStep:
             checked = self.check_rows(resid, grad, rows)
             if iteration < 0 or not -1 <= rank < self.N:
                 raise ValueError("iteration at least 0 and a rank in [-1, %d) expected" % self.N)
-            parts = self._issue_rows(resid, checked, stream)
+            parts = np.array(self._issue_rows(resid, checked, stream), dtype=np.int64)
         status = deft.lib().deft_step_part(
             ctypes.c_void_p(resid.data_ptr()), None if grad is None else ctypes.c_void_p(grad.data_ptr()), self.n_g,
             None if parts is None else ctypes.c_void_p(parts.ctypes.data), 0 if parts is None else len(parts),

@@ -17,7 +17,7 @@ VOCAB, WIDTH, N_TOKENS = 30, 8, 6
 
 @pytest.fixture
 def step(monkeypatch):
-    """A DeftStep over [12, VOCAB * WIDTH, 100] elements on the host; step.calls: the gradients that would have been added."""
+    """A DeftStep over [12, VOCAB * WIDTH, 100] elements on the host; step.calls: what would have gone to the library."""
     sizes = [12, VOCAB * WIDTH, 100]
     ds = object.__new__(DeftStep)
     ds.device, ds.N, ds.n_g = torch.device("cpu"), 2, sum(sizes)
@@ -25,7 +25,7 @@ def step(monkeypatch):
     ds.layer_start_d = torch.from_numpy(ds.tensor_start)
     ds.calls = []
     monkeypatch.setattr(deft, "_device", lambda *tensors: 0)
-    monkeypatch.setattr(deft, "deft_embed_grad", lambda grad_out, ids, grad, ws, **kw: ds.calls.append((grad, ws, kw)))
+    monkeypatch.setattr(deft, "_call", lambda name, device, stream, *args: ds.calls.append((name, stream, args)))
     return ds
 
 
@@ -38,7 +38,10 @@ def test_good_rows_reach_the_call(step):
     e = torch.zeros(step.n_g)
     parts = step.add_rows(e, [_row(), _row(seed=-1, offset=2 ** 64 + 5)])
     assert parts.tolist() == [[12, 12 + VOCAB * WIDTH]] and len(step.calls) == 2
-    assert all(g.data_ptr() == e[12:].data_ptr() and tuple(g.shape) == (VOCAB, WIDTH) and kw["accumulate"] for g, _, kw in step.calls)
+    for (name, stream, args), (seed, offset) in zip(step.calls, ((3, 0), (2 ** 64 - 1, 5))):
+        assert (name, stream) == ("deft_embed_grad", None)
+        assert args[1:3] == (deft.F32, WIDTH) and args[4:14] == (8, N_TOKENS, VOCAB, WIDTH, -1, 0.5, 0.25, seed, offset, None)
+        assert args[14:16] == (e[12:].data_ptr(), 1) and args[17] >= deft.deft_embed_workspace_bytes(N_TOKENS, VOCAB, WIDTH)
 
 
 @pytest.mark.parametrize("bad", [
@@ -70,7 +73,7 @@ def test_no_call_uses_the_workspace_of_another_stream(step, monkeypatch):
 
     def recorded(*args, **kw):
         t = empty(*args, **kw)
-        made[t.data_ptr()] = current[-1]
+        made[t.data_ptr()] = (current[-1], t)        # (kept: its memory is not given out again)
         return t
 
     monkeypatch.setattr(torch.cuda, "stream", On)
@@ -80,10 +83,11 @@ def test_no_call_uses_the_workspace_of_another_stream(step, monkeypatch):
     for stream, row in (("A", _row()), (None, _row()), ("B", more), ("A", _row()), (None, more), ("A", more)):
         step.calls.clear()
         step.add_rows(e, [row, row], stream=stream)
-        for _, ws, kw in step.calls:
-            assert made[ws.data_ptr()] == (stream or "default") and kw["stream"] == stream
-            used.setdefault(ws.data_ptr(), (ws, set()))[1].add(stream)
-    assert all(len(streams) == 1 for _, streams in used.values())
+        for _, on, args in step.calls:
+            ws = args[16]
+            assert made[ws][0] == (stream or "default") and on == stream
+            used.setdefault(ws, set()).add(stream)
+    assert all(len(streams) == 1 for streams in used.values())
 
 
 @pytest.mark.parametrize("scale,p,ok", [(1e39, 0.0, False), (-1e308, 0.0, False), (2.0 ** 128 - 2.0 ** 103, 0.0, False), (2.0 ** 128 - 2.0 ** 104, 0.0, True),
@@ -99,6 +103,28 @@ def test_scales_that_overflow_fp32_are_refused_before_the_first_row(step, scale,
         with pytest.raises(ValueError):
             step.add_rows(torch.zeros(step.n_g), rows)
     assert len(step.calls) == (2 if ok else 0)
+
+
+def test_rows_made_on_the_way_live_until_their_calls(step, monkeypatch):
+    """Rows may come from a generator, which keeps none of them."""
+    import weakref
+    made = []
+
+    def rows():
+        for _ in range(3):
+            row = _row(grad_out=torch.ones(N_TOKENS, WIDTH))
+            made.append((weakref.ref(row.grad_out), row.grad_out.data_ptr()))
+            yield row
+            del row
+
+    def call(name, device, stream, *args):
+        ref, ptr = made[len(step.calls)]
+        assert ref() is not None and args[0] == ptr
+        step.calls.append(args)
+
+    monkeypatch.setattr(deft, "_call", call)
+    step.add_rows(torch.zeros(step.n_g), rows())
+    assert len(step.calls) == 3
 
 
 class _OnDevice:
