@@ -5,8 +5,9 @@
 // two rounds that depend on the column or the offset alone are computed once.  Loads of several rows are in flight before
 // the first is converted (converting each as it came made the kernel wait for every load: 0.44 instead of 0.17 ms).
 //
-// What bounds them: dropout of 65536 x 4096 bf16 the memory (172 us, 0.97 of the measured copy rate; 0.54 of the integer
-// pipes' time is the generator), of 16384 x 1024 with a residual added 18.5 us (0.84).  Lookup of 131072 x 1024 fp32 -> bf16
+// What bounds them: dropout of 65536 x 4096 bf16 the memory (174 us, 0.96 of the measured copy rate, in short runs; 187 us,
+// 0.89, in long ones, where the clocks fall and the generator's integer work, half of the pipes' time, shows), of 16384 x 1024
+// with a residual added 18.6 us (0.84), of 32768 x 1024 fp32 with one 68 us (0.92).  Lookup of 131072 x 1024 fp32 -> bf16
 // with positions and dropout 104 us (0.55 of the copy rate over the bytes it cannot do without; 0.84 GB move between
 // L2 and the SMs, because a table row is read again for each of its tokens): the wait for a table row behind its id,
 // with two rows in flight per thread.  Calls of up to a few hundred thousand elements: the launch (3 to 4 us).  Rows that start on no 8-byte boundary are taken by warps in slices of
@@ -22,8 +23,12 @@ constexpr int kMostDeep = 4;     // rows it has in flight, when a row's group is
 constexpr int kMostEach = 16;    // rows it takes in all
 constexpr int kRounds = 8;       // rounds of CTAs a launch has at least before threads take several rows ...
 constexpr int kEmbedRounds = 3;  // ... fewer where a thread waits for an id before it can load a row
-constexpr int kBlocksOne = 8;    // CTAs an SM holds where threads take one row (32 registers) ...
-constexpr int kBlocksDeep = 4;   // ... and where they take several (64)
+// CTAs an SM holds where threads take one row (32 registers) and where they take several (64).  Chosen on bf16 without
+// positions or residual, which fits.  181 of the 324 instances spill: most with single elements (dropout with a residual up to
+// 656 bytes stored and loaded), lookup of one row with positions (up to 408), fp32 dropout with a residual (304 with 16-byte
+// alignment).  Other bounds for those have not been measured.
+constexpr int kBlocksOne = 8;
+constexpr int kBlocksDeep = 4;
 
 // Rows in flight of a thread that loads `words` words of each; two where the rows are not 16-byte aligned (their pieces and
 // tests take the registers that four would: dropout 32768 x 1020 bf16 39 against 50 us).

@@ -11,7 +11,7 @@ namespace {
 
 // ---- 1. grouping ----
 // What bounds it: latency.  4.3 us for 700 tokens, 8.6 us for 16384 (one read of the ids, two prefixes, five barriers),
-// 4.2 + 10.6 us for 131072 with the splitting pass before it (33.7 without; at 16384 the two forms are level).
+// 4.2 + 10.6 us for 131072 with the splitting pass before it (33.7 without).
 // Table row v belongs to CTA v % kOwners.  Every CTA reads all ids (they stay in L2) and keeps its own: no CTA
 // needs anything from another, so there is no barrier over the grid and no pass over global counters.  With many
 // tokens that reading is most of the work (34 us for 131072), and k_split_tokens orders tiles of them by CTA first.
@@ -21,7 +21,7 @@ namespace {
 constexpr int kOwners = 128;                 // CTAs (a power of two below the 148 SMs)
 constexpr size_t kGroupSmem = 220 * 1024;
 constexpr int kTokenTile = 1024;             // tokens per tile of the splitting pass
-constexpr int64_t kSplitFrom = 16384;        // calls of more tokens split first (16384: 3.9 + 6.9 against 9.2 us, 20000: 11.2 against 12.3, 131072: 14.8 against 33.7)
+constexpr int64_t kSplitFrom = 16384;        // calls of more tokens split first (16384: 3.9 + 6.9 us against 9.2 without, 20000: 11.2 against 12.3, 131072: 14.8 against 33.7)
 constexpr int kSplitPitch = kOwners + 2;     // a tile's first entry of every CTA, and their number
 constexpr int kListMost = 1024;              // own tokens a warp remembers at most; one that has more reads the ids again
 
@@ -248,8 +248,8 @@ __global__ void __launch_bounds__(1024) k_group_tokens(const Id* __restrict__ id
 //
 // What bounds it, 131072 x 1024 bf16 added with dropout: 103 us for 464 MB, 0.70 of the measured copy rate; the
 // schedulers issue in 68 % of the cycles (137 instructions per token and 256 columns, 34 of them the generator's
-// products and exclusive ors): the integer pipes and the memory are both near what they give together.  Without
-// dropout it is the memory.  Small calls are bound by latency: 9 us for 700 x 1500, of which a third is the joins.
+// products and exclusive ors); no single resource is full.  The whole call takes 116 us, 109 without
+// dropout, 218 with fp32 input (floor 113).  Small calls are bound by latency: 9 us for 700 x 1500, of which a third is the joins.
 constexpr int kReduceThreads = 128;
 constexpr int kReduceBlocks = 8; // CTAs an SM holds (64 registers a thread; with 48 it spills)
 constexpr int kJoin = 32;        // units whose partial sums one warp adds up
