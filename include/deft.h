@@ -67,6 +67,19 @@ typedef int32_t deft_status;
 /* Largest table deft_embed_grad accepts (rows; its counters per row live in shared memory). */
 #define DEFT_EMBED_MAX_ROWS 3000000LL
 
+/* Longest row deft_layer_norm and its gradient take, largest vocabulary and number of entries of deft_distill, largest
+ * turned part of a head of deft_rotary. */
+#define DEFT_NORM_MAX_COLS 16384
+#define DEFT_DISTILL_MAX_VOCAB 262144
+#define DEFT_DISTILL_MAX_TOP 1024
+#define DEFT_ROTARY_MAX_ROT 4096
+
+/* How deft_rotary_frequencies stretches the frequencies for contexts longer than the model was trained on. */
+#define DEFT_ROTARY_PLAIN  0
+#define DEFT_ROTARY_LINEAR 1
+#define DEFT_ROTARY_BASE   2
+#define DEFT_ROTARY_PARTS  3
+
 /* Largest layer a plan accepts (a layer's positions are 32-bit).  What one selection launch can
  * scan is smaller on today's devices: see deft_select_launch_max_elems(). */
 #define DEFT_MAX_LAYER_ELEMS 2147483647LL
@@ -543,6 +556,117 @@ DEFT_API deft_status deft_embed_grad(const void* grad_out_d, int32_t grad_out_ty
 DEFT_API deft_status deft_dropout(const void* x_d, int32_t x_type, int64_t ld_x, const void* add_d, int64_t ld_add,
                                   void* y_d, int32_t y_type, int64_t ld_y, int64_t rows, int64_t cols, double p,
                                   uint64_t seed, uint64_t offset, const uint64_t* offset_d, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Dense row operators: what lies between a language model's lookup and its loss, as far as it is no contraction.  The
+ * conventions are those of the row operators above (matrices with a pitch, any element alignment, whole 16-byte granules
+ * read, elements alone written, fp32 arithmetic, one rounding at the end).  Rows whose matrices start on the same
+ * place of a 16-byte granule in every matrix of a call (equal offsets and pitches modulo 8 elements; contiguous ones do) are
+ * fastest.  Small vectors (weights, statistics, losses, sums) must not overlap anything the call writes.
+ * ---------------------------------------------------------------------------------------- */
+
+/*
+ * Layer norm of every row of s = x + add: with m = mean(s), v = mean((s - m)^2) and r = 1 / sqrt(v + eps)
+ *     y = (s - m) r gamma + beta.
+ *   x_d       [rows, cols], x_type;  add_d NULL, or the same (a residual stream's branch)
+ *   sum_d     NULL, or [rows, cols] of x_type: s, rounded (what the next block adds to and the gradient reads; y is
+ *             formed from the sum before it is rounded).  Needs add_d
+ *   gamma_d, beta_d  [cols] of w_type; NULL: ones, zeros
+ *   y_d       [rows, cols], y_type
+ *   mean_d, rstd_d   NULL, or [rows] fp32: m and r for the gradient
+ * sum and y may be x or add, element for element (same type and pitch); otherwise, and from each other, they are apart.
+ * Errors: INVALID_ARG (eps negative or not finite), TOO_LARGE (cols beyond DEFT_NORM_MAX_COLS, rows beyond 2^31 - 1), CUDA.
+ */
+DEFT_API deft_status deft_layer_norm(const void* x_d, int32_t x_type, int64_t ld_x, const void* add_d, int64_t ld_add,
+                                     void* sum_d, int64_t ld_sum, const void* gamma_d, const void* beta_d, int32_t w_type,
+                                     void* y_d, int32_t y_type, int64_t ld_y, int64_t rows, int64_t cols, double eps,
+                                     float* mean_d, float* rstd_d, void* stream);
+
+/*
+ * Gradient of deft_layer_norm: with h = (x - mean) rstd and d = grad_out gamma, per row
+ *     grad_x = rstd (d - mean(d) - h mean(d h)) + add,
+ * and over the rows  grad_gamma = scale sum(grad_out h),  grad_beta = scale sum(grad_out).
+ *   grad_out_d [rows, cols], grad_out_type;  x_d [rows, cols], x_type: what was normalised (x, or the sum)
+ *   mean_d, rstd_d [rows] fp32, from the forward call;  gamma_d NULL (ones), or [cols] of w_type
+ *   add_d      NULL, or [rows, cols] of x_type: the gradient that reaches x past the norm
+ *   grad_x_d   NULL (not wanted), or [rows, cols] of x_type; may be grad_out, x or add, element for element
+ *   grad_gamma_d, grad_beta_d  NULL (not wanted), or [cols] fp32: usually their parts of the flat vector.  accumulate = 0:
+ *              written; accumulate != 0: added, one fp32 round-to-nearest add per element (the residual, or a
+ *              gradient vector that holds other shares).  Sums are fp32 in a fixed order: the same bits on every call.
+ *   scale      finite in fp32; of these two alone
+ *   ws_d       deft_layer_norm_workspace_bytes(rows, cols), 256-byte aligned; NULL where neither of the two is wanted.
+ *              Holds nothing between calls; calls that share it must not overlap on the GPU.  Enough for fewer rows and columns.
+ * Errors: INVALID_ARG (nothing wanted), CAPACITY (workspace), TOO_LARGE (as deft_layer_norm), CUDA.
+ */
+DEFT_API size_t deft_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+DEFT_API deft_status deft_layer_norm_grad(const void* grad_out_d, int32_t grad_out_type, int64_t ld_grad_out, const void* x_d,
+                                          int32_t x_type, int64_t ld_x, const float* mean_d, const float* rstd_d,
+                                          const void* gamma_d, int32_t w_type, const void* add_d, int64_t ld_add,
+                                          void* grad_x_d, int64_t ld_grad_x, float* grad_gamma_d, float* grad_beta_d,
+                                          int64_t rows, int64_t cols, int32_t accumulate, double scale, void* ws_d,
+                                          size_t ws_bytes, void* stream);
+
+/*
+ * Frequencies of rotary positions (host): pair i of rot / 2 turns by f_i radians per position, f_i = base^(-2 i / rot), stretched
+ *   DEFT_ROTARY_LINEAR  f_i / factor (interpolated positions)
+ *   DEFT_ROTARY_BASE    base times factor^(rot / (rot - 2)): the slowest pair as with LINEAR, the fastest as it was
+ *   DEFT_ROTARY_PARTS   f_i (c + (1 - c) / factor), c = (u - low) / (high - low) within [0, 1], u = original f_i / (2 pi) the turns
+ *                       over the context trained on (Peng et al., "YaRN", 2023; there low = 1, high = 32, and
+ *                       deft_rotary's gain = 1 + ln(factor) / 10)
+ *   turns_h[rot / 2] out  frac(f_i / (2 pi)) in units of 2^-64, rounded: times a position, modulo 2^64, the angle
+ * factor is not read for PLAIN, original, low and high for PARTS only.
+ * Errors: INVALID_ARG (rot odd or below 2, base below 1, factor not positive, original not positive, high not above low,
+ * a number not finite, an unknown scaling), TOO_LARGE (rot beyond DEFT_ROTARY_MAX_ROT).
+ */
+DEFT_API deft_status deft_rotary_frequencies(int32_t rot, double base, int32_t scaling, double factor, double original,
+                                             double low, double high, uint64_t* turns_h);
+
+/*
+ * Rotary positions of x [batch, tokens, heads, dim]: the pair i (a, b) of a token at position t becomes
+ *     gain (a cos w - b sin w),  gain (a sin w + b cos w),   w = 2 pi frac(t turns[i] 2^-64).
+ * The angle is exact to a rounding of the cosine and sine for every 64-bit position, negative ones too.
+ *   x_strides_h, y_strides_h  HOST [3]: elements between batches, tokens and heads; a head's columns are contiguous
+ *   turns_d      [rot / 2] (DEVICE, 8-byte aligned);  rot <= dim: columns from rot on are copied
+ *   interleaved  0: pair i is (i, i + rot / 2); else (2 i, 2 i + 1)
+ *   inverse      != 0: angles negated, which is the gradient (of the same gain)
+ *   gain         finite in fp32
+ *   pos_d        NULL (a token's number within its batch), or [batch * tokens] int32 or int64 (pos_bytes 4 or 8)
+ * y may be x, element for element (what is copied stays); otherwise they are apart.  x may repeat elements (stride 0), y not.
+ * Errors: INVALID_ARG (also: outputs that overlap each other, or x without being it; strides that differ between the
+ * two count as overlapping where their ranges of memory meet), TOO_LARGE (batch * tokens beyond 2^31 - 1, heads * dim
+ * beyond 2^30, rot beyond DEFT_ROTARY_MAX_ROT), CUDA.
+ */
+DEFT_API deft_status deft_rotary(const void* x_d, const int64_t* x_strides_h, void* y_d, const int64_t* y_strides_h, int32_t type,
+                                 int64_t batch, int64_t tokens, int64_t heads, int64_t dim, const uint64_t* turns_d, int64_t rot,
+                                 int32_t interleaved, int32_t inverse, double gain, const void* pos_d, int32_t pos_bytes,
+                                 void* stream);
+
+/*
+ * Distillation from a teacher's top logits, per row: with z the student's logits, p = softmax(z / T), the teacher's entries
+ * (id_j, t_j), j < top, and log q_j = t_j / T - L
+ *     loss = weight T^2 (sum_j q_j (log q_j - log p[id_j]) + q' (log q' - log p')),
+ *     grad = scale weight T (p m - q - q' p outside the entries / p'),   m = sum q + q',
+ * q[v] the sum of the q_j with id_j = v (an id may come twice).  Two forms:
+ *   teacher_lse_d NULL: L is the log-sum-exp of the row's valid t_j / T; q' = 0
+ *   else          [rows] fp32: L, the teacher's own over its whole vocabulary at T; q' = max(0, 1 - sum q) is what it gives
+ *                 to the rest, p' the student's share of the columns that no entry names (formed as their sum, not as a difference;
+ *                 q' = 0 where none of them has a logit above -inf)
+ * One read of the logits, whose gradient is written in the same call.
+ *   logits_d  [rows, vocab], type;  grad_d NULL, or [rows, vocab] of the same type: may be the logits, element for element
+ *   ids_d     [rows, top] int32 or int64 (id_bytes 4 or 8); entries with an id outside [0, vocab) are left out (padding)
+ *   teacher_d [rows, top], teacher_type
+ *   weight_d  NULL (ones), or [rows] fp32: of a row of weight 0 nothing is read, its loss and gradient are 0
+ *   loss_d    NULL, or [rows] fp32;  scale: of the gradient alone, finite in fp32 (and times the temperature)
+ * An entry with q_j = 0 (t_j = -inf) adds nothing; a row without entries of any q has loss 0 and, without teacher_lse, gradient
+ * 0.  Sums run in a fixed order: the same bits on every call.
+ * Errors: INVALID_ARG (neither loss nor grad, temperature outside [1e-6, 1e6]), TOO_LARGE (rows beyond 2^28 - 1, vocab beyond
+ * DEFT_DISTILL_MAX_VOCAB, top beyond DEFT_DISTILL_MAX_TOP), CUDA.
+ */
+DEFT_API deft_status deft_distill(const void* logits_d, int32_t type, int64_t ld_logits, int64_t rows, int64_t vocab,
+                                  const void* ids_d, int32_t id_bytes, int64_t ld_ids, const void* teacher_d,
+                                  int32_t teacher_type, int64_t ld_teacher, int64_t top, const float* teacher_lse_d,
+                                  double temperature, const float* weight_d, double scale, float* loss_d, void* grad_d,
+                                  int64_t ld_grad, void* stream);
 
 /*
  * Comparison sparsifiers of Section 3 (not part of DEFT; they reuse its selection kernel).

@@ -306,4 +306,31 @@ deft_status deft_bin_layers(const int32_t* bin_of_layer_h, int32_t L, int32_t bi
     return DEFT_OK;
 }
 
+deft_status deft_rotary_frequencies(int32_t rot, double base, int32_t scaling, double factor, double original, double low,
+                                    double high, uint64_t* turns_h) {
+    if (!turns_h || rot < 2 || (rot & 1) || !std::isfinite(base) || base < 1.0 || scaling < DEFT_ROTARY_PLAIN || scaling > DEFT_ROTARY_PARTS)
+        return DEFT_ERR_INVALID_ARG;
+    if (scaling != DEFT_ROTARY_PLAIN && !(std::isfinite(factor) && factor > 0.0)) return DEFT_ERR_INVALID_ARG;
+    if (scaling == DEFT_ROTARY_PARTS && !(std::isfinite(original) && original > 0.0 && std::isfinite(low) && std::isfinite(high) && high > low))
+        return DEFT_ERR_INVALID_ARG;
+    if (rot > DEFT_ROTARY_MAX_ROT) return DEFT_ERR_TOO_LARGE;
+    // 64 bits of a turn need more than a double holds: extended precision throughout
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    long double b = base;
+    if (scaling == DEFT_ROTARY_BASE && rot > 2) b *= powl((long double)factor, (long double)rot / (rot - 2));
+    for (int32_t i = 0; i < rot / 2; ++i) {
+        long double f = powl(b, -2.0L * i / rot);
+        if (scaling == DEFT_ROTARY_LINEAR) f /= factor;
+        if (scaling == DEFT_ROTARY_PARTS) {
+            long double c = ((long double)original * f / two_pi - low) / ((long double)high - low);
+            c = c < 0.0L ? 0.0L : (c > 1.0L ? 1.0L : c);
+            f *= c + (1.0L - c) / factor;
+        }
+        const long double turn = fmodl(f / two_pi, 1.0L);
+        const long double units = floorl(turn * 18446744073709551616.0L + 0.5L);   // 2^64; a whole turn is none
+        turns_h[i] = units >= 18446744073709551616.0L ? 0u : (uint64_t)units;
+    }
+    return DEFT_OK;
+}
+
 }  // extern "C"

@@ -1,0 +1,174 @@
+// Rotary positions: pairs of a head's columns turned by an angle that grows with the token's position.
+//
+// A frequency is a number of turns per position in units of 2^-64, so that the product with a position, taken modulo
+// 2^64, is the angle modulo a turn, exactly: far positions cost no accuracy.  A CTA takes a few tokens: their cosines and
+// sines once into shared memory, then all heads with them.
+#include "deft_dense.cuh"
+
+namespace deft {
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotSmem = 32 * 1024;
+
+// kVec elements of a row, in pieces of up to 16 bytes, or (kSingle) one by one.
+template <typename T, int kVec, bool kSingle>
+struct Vec {
+    static constexpr int kBytes = kVec * (int)sizeof(T), kPiece = kSingle ? (int)sizeof(T) : (kBytes < 16 ? kBytes : 16), kPieces = kBytes / kPiece;
+    using P = typename Piece<kPiece>::type;
+    P piece[kPieces];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) piece[i] = reinterpret_cast<const P*>(p)[i];
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) reinterpret_cast<P*>(p)[i] = piece[i];
+    }
+    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(piece)[i]); }
+    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(piece)[i] = from_f32<T>(v); }
+};
+
+struct RotarySplit {
+    FastDiv units, heads, per_token;     // of a head: vectors of pairs, then vectors that are copied; heads; their product
+    int turned;                          // units of a head that are turned
+    int tokens;                          // of a CTA
+};
+
+// The cosine and sine of a fraction of a turn (unsigned, 2^-64 turns): what is left after the nearest quarter turn is exact
+// to 2^-28 turns in fp32.
+__device__ __forceinline__ float2 cos_sin(uint64_t turns) {
+    const uint32_t t = (uint32_t)(turns >> 32) + (uint32_t)((turns >> 31) & 1u);
+    const uint32_t quarter = (t + 0x20000000u) >> 30;
+    const int32_t rest = (int32_t)(t - (quarter << 30));             // in [-2^29, 2^29)
+    float s, c;
+    sincospif((float)rest * 4.656612873077392578125e-10f, &s, &c);   // 2^-31: half turns
+    const bool swap = quarter & 1;
+    const float cc = swap ? s : c, ss = swap ? c : s;
+    return make_float2(quarter == 1 || quarter == 2 ? -cc : cc, quarter == 2 || quarter == 3 ? -ss : ss);
+}
+
+template <typename T, int kVec, bool kPairs, bool kSingle>
+__global__ void __launch_bounds__(kRotThreads) k_rotary(const __grid_constant__ RotaryArgs a, const RotarySplit split, const FastDiv tokens) {
+    extern __shared__ float2 table[];    // [tokens of the CTA][rot / 2]
+    const int half = a.rot >> 1;
+    const uint32_t all = (uint32_t)(a.batch * a.tokens);
+    const uint32_t first = blockIdx.x * (uint32_t)split.tokens;
+    const int have = (int)min((uint32_t)split.tokens, all - first);
+    for (int i = threadIdx.x; i < have * half; i += kRotThreads) {
+        const int k = i / half, p = i - k * half;
+        const uint32_t token = first + k;
+        int64_t pos;
+        if (!a.pos) pos = token - tokens.div(token) * tokens.d;
+        else pos = a.pos_bytes == 8 ? static_cast<const int64_t*>(a.pos)[token] : static_cast<const int32_t*>(a.pos)[token];
+        float2 cs = cos_sin((uint64_t)pos * a.turns[p]);
+        table[i] = make_float2(cs.x * a.gain_cos, cs.y * a.gain_sin);
+    }
+    __syncthreads();
+    const T* x = static_cast<const T*>(a.x);
+    T* y = static_cast<T*>(a.y);
+    const uint32_t items = (uint32_t)have * split.per_token.d;
+    for (uint32_t i = threadIdx.x; i < items; i += kRotThreads) {
+        const uint32_t k = split.per_token.div(i), in = i - k * split.per_token.d;
+        const uint32_t head = split.units.div(in), unit = in - head * split.units.d;
+        const uint32_t token = first + k, b = tokens.div(token), t = token - b * tokens.d;
+        const T* from = x + (int64_t)b * a.x_batch + (int64_t)t * a.x_token + (int64_t)head * a.x_head;
+        T* to = y + (int64_t)b * a.y_batch + (int64_t)t * a.y_token + (int64_t)head * a.y_head;
+        const float2* cs = table + k * half;
+        Vec<T, kVec, kSingle> u, v;
+        if ((int)unit >= split.turned) {
+            const int c = a.rot + ((int)unit - split.turned) * kVec;
+            if (!kSingle || c + kVec <= a.dim) {
+                u.load(from + c);
+                u.store(to + c);
+            } else {
+                for (int e = c; e < a.dim; ++e) to[e] = from[e];
+            }
+        } else if (kPairs) {
+            const int c = (int)unit * kVec;
+            u.load(from + c);
+#pragma unroll
+            for (int e = 0; e < kVec; e += 2) {
+                const float2 w = cs[(c + e) >> 1];
+                const float p = u.get(e), q = u.get(e + 1);
+                v.set(e, p * w.x - q * w.y);
+                v.set(e + 1, p * w.y + q * w.x);
+            }
+            v.store(to + c);
+        } else {
+            const int c = (int)unit * kVec;
+            u.load(from + c);
+            v.load(from + half + c);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float2 w = cs[c + e];
+                const float p = u.get(e), q = v.get(e);
+                u.set(e, p * w.x - q * w.y);
+                v.set(e, p * w.y + q * w.x);
+            }
+            u.store(to + c);
+            v.store(to + half + c);
+        }
+    }
+}
+
+// Elements a thread takes at a time: as many as every head's row and the borders in it are aligned to (strides of dimensions
+// of one element are 0).
+inline int vec_of(const RotaryArgs& a, size_t elem) {
+    const int64_t inner = (a.interleaved ? a.rot : a.rot / 2) | a.dim;
+    const int64_t strides = a.x_head | a.x_token | a.x_batch | a.y_head | a.y_token | a.y_batch;
+    const uint64_t bytes = (uint64_t)((inner | strides) * (int64_t)elem) | reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y);
+    for (int v = 8; v > 1; v /= 2) {
+        const size_t piece = v * elem < 16 ? v * elem : 16;
+        if ((inner & (v - 1)) == 0 && (bytes & (piece - 1)) == 0) return v;
+    }
+    return 1;
+}
+
+}  // namespace
+
+deft_status launch_rotary(const RotaryArgs& a, int type, cudaStream_t stream) {
+    const int vec = vec_of(a, type_bytes(type));
+    const bool single = a.interleaved && vec == 1;       // a pair is two elements, however it is aligned
+    const int step = single ? 2 : vec, half = a.rot / 2;
+    RotarySplit s{};
+    s.turned = (a.interleaved ? a.rot : half) / step;
+    const int64_t units = s.turned + (a.x == a.y ? 0 : (a.dim - a.rot + step - 1) / step);
+    const int64_t all = a.batch * a.tokens;
+    const int64_t per_token = units * a.heads;
+    int64_t tokens = (4 * kRotThreads + per_token - 1) / per_token;
+    const int64_t fit = kRotSmem / ((int64_t)half * (int64_t)sizeof(float2));
+    if (tokens > fit) tokens = fit;
+    if (tokens > all) tokens = all;
+    while (tokens > 1 && (all + tokens - 1) / tokens < 2 * 148) tokens = (tokens + 1) / 2;
+    s.tokens = (int)tokens;
+    s.units = fast_div((uint32_t)units);
+    s.heads = fast_div((uint32_t)a.heads);
+    s.per_token = fast_div((uint32_t)per_token);
+    const unsigned blocks = (unsigned)((all + tokens - 1) / tokens);
+    const size_t smem = (size_t)tokens * half * sizeof(float2);
+    const FastDiv t = fast_div((uint32_t)a.tokens);
+    return with_type(type, [&](auto e) -> deft_status {
+        using T = decltype(e);
+        auto run = [&](auto kernel) { kernel<<<blocks, kRotThreads, smem, stream>>>(a, s, t); };
+        if (a.interleaved) {
+            switch (vec) {
+                case 8: run(k_rotary<T, 8, true, false>); break;
+                case 4: run(k_rotary<T, 4, true, false>); break;
+                case 2: run(k_rotary<T, 2, true, false>); break;
+                default: run(k_rotary<T, 2, true, true>); break;
+            }
+        } else {
+            switch (vec) {
+                case 8: run(k_rotary<T, 8, false, false>); break;
+                case 4: run(k_rotary<T, 4, false, false>); break;
+                case 2: run(k_rotary<T, 2, false, false>); break;
+                default: run(k_rotary<T, 1, false, true>); break;
+            }
+        }
+        DEFT_CUDA_TRY(cudaGetLastError());
+        return DEFT_OK;
+    });
+}
+
+}  // namespace deft

@@ -108,6 +108,18 @@ def lib() -> ctypes.CDLL:
         L.deft_embed_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, i64, f64, f64, u64, u64, vp, vp, i32, vp, sz, vp]
         L.deft_dropout.restype = i32
         L.deft_dropout.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, i64, i64, f64, u64, u64, vp, vp]
+        L.deft_layer_norm.restype = i32
+        L.deft_layer_norm.argtypes = [vp, i32, i64, vp, i64, vp, i64, vp, vp, i32, vp, i32, i64, i64, i64, f64, vp, vp, vp]
+        L.deft_layer_norm_workspace_bytes.restype = sz
+        L.deft_layer_norm_workspace_bytes.argtypes = [i64, i64]
+        L.deft_layer_norm_grad.restype = i32
+        L.deft_layer_norm_grad.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, vp, i32, vp, i64, vp, i64, vp, vp, i64, i64, i32, f64, vp, sz, vp]
+        L.deft_rotary_frequencies.restype = i32
+        L.deft_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp]
+        L.deft_rotary.restype = i32
+        L.deft_rotary.argtypes = [vp, vp, vp, vp, i32, i64, i64, i64, i64, vp, i64, i32, i32, f64, vp, i32, vp]
+        L.deft_distill.restype = i32
+        L.deft_distill.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, i32, i64, i64, vp, f64, vp, f64, vp, vp, i64, vp]
         L.deft_workspace_init.restype = i32
         L.deft_workspace_init.argtypes = [vp, sz, i32, vp]
         L.deft_threshold_select.restype = i32
@@ -773,3 +785,161 @@ def deft_dropout(x, y, add=None, p: float = 0.5, seed: int = 0, offset: int = 0,
     dev = _device(y, x, add, offset_d)
     _call("deft_dropout", dev, stream, x.data_ptr(), _type(x), ld_x, None if add is None else add.data_ptr(), ld_add, y.data_ptr(), _type(y), ld_y,
           rows, cols, p, seed & _U64, offset & _U64, _offset(offset_d))
+
+
+# ------------------------------------------------------------------------------------------
+# dense row operators: layer norm and its gradient, rotary positions, distillation loss
+# ------------------------------------------------------------------------------------------
+NORM_MAX_COLS = 16384
+DISTILL_MAX_VOCAB = 262144
+DISTILL_MAX_TOP = 1024
+ROTARY_MAX_ROT = 4096
+_ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def _vector(t, name: str, count: int, dtype=None) -> Optional[int]:
+    """The pointer of a contiguous vector of `count` elements (None: not given); fp32 unless dtype says otherwise."""
+    if t is None:
+        return None
+    if dtype is None:
+        import torch
+        dtype = torch.float32
+    if t.numel() != count or not t.is_contiguous() or t.dtype != dtype:
+        raise ValueError("%s: a contiguous %s tensor of %d elements expected" % (name, dtype, count))
+    return t.data_ptr()
+
+
+def _like(t, name: str, shape, dtype) -> Tuple[Optional[int], int]:
+    """Pointer and pitch of a matrix of a given shape and type (None: not given)."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError("%s: a %s tensor of %s expected" % (name, dtype, tuple(shape)))
+    return t.data_ptr(), _matrix(t, name)[2]
+
+
+def _weights(gamma, beta, cols: int) -> Tuple[Optional[int], Optional[int], int]:
+    first = gamma if gamma is not None else beta
+    if first is None:
+        return None, None, F32
+    return _vector(gamma, "gamma", cols, first.dtype), _vector(beta, "beta", cols, first.dtype), _type(first)
+
+
+def deft_layer_norm(x, y, gamma=None, beta=None, eps: float = 1e-5, add=None, sum=None, mean=None, rstd=None, stream=None) -> None:
+    """y = layer norm of the rows (the last dimension) of x + add; the sum goes to `sum`, the statistics that the
+    gradient needs to mean and rstd (fp32, one number per row)."""
+    rows, cols, ld_x = _matrix(x, "x")
+    if y.shape != x.shape:
+        raise ValueError("x and y disagree")
+    ld_y = _matrix(y, "y")[2]
+    p_add, ld_add = _like(add, "add", x.shape, x.dtype)
+    p_sum, ld_sum = _like(sum, "sum", x.shape, x.dtype)
+    p_gamma, p_beta, w_type = _weights(gamma, beta, cols)
+    dev = _device(y, x, add, sum, gamma, beta, mean, rstd)
+    _call("deft_layer_norm", dev, stream, x.data_ptr(), _type(x), ld_x, p_add, ld_add, p_sum, ld_sum, p_gamma, p_beta, w_type, y.data_ptr(),
+          _type(y), ld_y, rows, cols, eps, _vector(mean, "mean", rows), _vector(rstd, "rstd", rows))
+
+
+def deft_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().deft_layer_norm_workspace_bytes(int(rows), int(cols)))
+
+
+def alloc_layer_norm_workspace(rows: int, cols: int, device="cuda"):
+    """A torch uint8 tensor for deft_layer_norm_grad calls of up to `rows` rows of up to `cols` columns."""
+    import torch
+    size = deft_layer_norm_workspace_bytes(rows, cols)
+    if size == 0:
+        raise DeftError("deft_layer_norm_workspace_bytes", ERR_INVALID_ARG)
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def deft_layer_norm_grad(grad_out, x, mean, rstd, grad_x=None, gamma=None, add=None, grad_gamma=None, grad_beta=None, ws=None,
+                         accumulate: bool = False, scale: float = 1.0, stream=None) -> None:
+    """deft_layer_norm's gradient: with respect to x into grad_x (plus `add`, what reaches x past the norm), with respect to
+    gamma and beta into grad_gamma and grad_beta, fp32 vectors (usually views of the flat gradient vector or of the
+    residual), written, or with accumulate added to.  What is None is not computed."""
+    rows, cols, ld_x = _matrix(x, "x")
+    if grad_out.shape != x.shape:
+        raise ValueError("grad_out and x disagree")
+    ld_go = _matrix(grad_out, "grad_out")[2]
+    p_add, ld_add = _like(add, "add", x.shape, x.dtype)
+    p_gx, ld_gx = _like(grad_x, "grad_x", x.shape, x.dtype)
+    p_gamma, _, w_type = _weights(gamma, None, cols)
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("ws: a contiguous tensor")
+    dev = _device(x, grad_out, mean, rstd, grad_x, gamma, add, grad_gamma, grad_beta, ws)
+    _call("deft_layer_norm_grad", dev, stream, grad_out.data_ptr(), _type(grad_out), ld_go, x.data_ptr(), _type(x), ld_x, _vector(mean, "mean", rows),
+          _vector(rstd, "rstd", rows), p_gamma, w_type, p_add, ld_add, p_gx, ld_gx, _vector(grad_gamma, "grad_gamma", cols),
+          _vector(grad_beta, "grad_beta", cols), rows, cols, 1 if accumulate else 0, scale, None if ws is None else ws.data_ptr(),
+          0 if ws is None else ws.numel() * ws.element_size())
+
+
+def deft_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                            high: float = 32.0) -> np.ndarray:
+    """The frequencies of deft_rotary's rot / 2 pairs, an int64 array (the bits of unsigned fractions of a turn): base^(-2 i / rot) radians
+    per position, stretched for contexts `factor` times as long ("linear", "base", or "parts": by their turns over the `original`
+    context, kept from `high` turns on, stretched in full up to `low`)."""
+    if scaling not in _ROTARY_SCALINGS:
+        raise ValueError("scaling: one of %s" % ", ".join(_ROTARY_SCALINGS))
+    out = np.zeros(max(1, int(rot) // 2), dtype=np.int64)
+    if int(rot) <= ROTARY_MAX_ROT:
+        _check("deft_rotary_frequencies", lib().deft_rotary_frequencies(int(rot), base, _ROTARY_SCALINGS[scaling], factor, original, low, high, _hp(out)))
+    else:
+        raise DeftError("deft_rotary_frequencies", ERR_TOO_LARGE)
+    return out
+
+
+_Strides = ctypes.c_int64 * 3
+
+
+def _heads(t, name: str):
+    """(batch, tokens, heads, dim) and the strides of a [batch, tokens, heads, dim] or [tokens, heads, dim] tensor."""
+    if t.dim() not in (3, 4):
+        raise ValueError("%s: a [batch, tokens, heads, dim] or [tokens, heads, dim] tensor" % name)
+    if t.size(-1) > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the columns of a head must be contiguous" % name)
+    shape, strides = tuple(t.shape), t.stride()
+    return ((1,) + shape, _Strides(0, *strides[:2])) if t.dim() == 3 else (shape, _Strides(*strides[:3]))
+
+
+def deft_rotary(x, y, turns, positions=None, interleaved: bool = False, inverse: bool = False, gain: float = 1.0, stream=None) -> None:
+    """Rotary positions: the first 2 len(turns) columns of every head of x ([batch, tokens, heads, dim] or [tokens, heads, dim], any
+    strides of the first ones) turned by position times frequency; the others are copied.  y may be x.  turns:
+    deft_rotary_frequencies on the device.  positions: int64 or int32, one per token (None: its number in its sequence).  inverse: the
+    gradient with respect to x of the same call, applied to the gradient of y."""
+    import torch
+    shape, xs = _heads(x, "x")
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("x and y disagree")
+    ys = _heads(y, "y")[1]
+    if turns.dim() != 1 or not turns.is_contiguous() or turns.dtype not in (torch.int64, torch.uint64):
+        raise ValueError("turns: a contiguous vector of 64-bit integers")
+    pos_bytes = 0
+    if positions is not None:
+        if positions.shape != x.shape[:-2]:
+            raise ValueError("positions: one for each token expected")
+        pos_bytes = _ids(positions)
+    dev = _device(y, x, turns, positions)
+    _call("deft_rotary", dev, stream, x.data_ptr(), xs, y.data_ptr(), ys, _type(x), shape[0], shape[1], shape[2], shape[3], turns.data_ptr(),
+          2 * turns.numel(), 1 if interleaved else 0, 1 if inverse else 0, gain, None if positions is None else positions.data_ptr(), pos_bytes)
+
+
+def deft_distill(logits, top_ids, top_logits, loss=None, grad=None, teacher_lse=None, temperature: float = 1.0, weight=None, scale: float = 1.0,
+                 stream=None) -> None:
+    """temperature^2 KL(teacher || student) of every row of logits (the last dimension is the vocabulary) into loss (fp32, one number per
+    row) and scale times its gradient into grad (of the logits' type; may be the logits).  The teacher: its entries' ids and logits,
+    renormalised over them, or with teacher_lse (its own log-sum-exp at the temperature, one number per row) with one class for
+    all other tokens.  weight: fp32, one number per row; rows of weight 0 are not read."""
+    rows, vocab, ld = _matrix(logits, "logits")
+    if top_ids.shape != top_logits.shape or top_ids.dim() == 0 or top_ids.shape[:-1] != logits.shape[:-1]:
+        raise ValueError("logits, top_ids and top_logits disagree")
+    import torch
+    if top_ids.dtype not in (torch.int64, torch.int32):
+        raise ValueError("top_ids: an int64 or int32 tensor")
+    top, ld_ids = _matrix(top_ids, "top_ids")[1:]
+    ld_teacher = _matrix(top_logits, "top_logits")[2]
+    p_grad, ld_grad = _like(grad, "grad", logits.shape, logits.dtype)
+    dev = _device(logits, top_ids, top_logits, loss, grad, teacher_lse, weight)
+    _call("deft_distill", dev, stream, logits.data_ptr(), _type(logits), ld, rows, vocab, top_ids.data_ptr(), top_ids.element_size(), ld_ids,
+          top_logits.data_ptr(), _type(top_logits), ld_teacher, top, _vector(teacher_lse, "teacher_lse", rows), temperature,
+          _vector(weight, "weight", rows), scale, _vector(loss, "loss", rows), p_grad, ld_grad)
