@@ -1,9 +1,9 @@
 // Distillation from a teacher's top logits: per row T^2 KL(teacher || student) and its gradient.
 //
 // A row of logits is read once.  A cluster of 1 to 8 CTAs shares it: each copies a part of its 16-byte granules into
-// shared memory, takes the teacher's entries out of that part (they are few; what is left is the rest of the vocabulary, whose
-// sum must not come from a difference), sums the exponentials of the rest and of the entries apart, and the CTAs exchange
-// these sums.  The gradient is then formed from shared memory and written; the entries' elements last.
+// shared memory.  The first warp, meanwhile, works out the teacher's probabilities and marks the entries' elements: what is
+// left is the rest of the vocabulary, whose sum must not come from a difference.  All warps sum the powers of the rest,
+// the CTAs exchange their sums, and the gradient is formed from shared memory and written.
 #include <cooperative_groups.h>
 
 #include "deft_dense.cuh"
@@ -11,52 +11,69 @@
 namespace deft {
 namespace {
 
-namespace cg = cooperative_groups;
-
 constexpr int kMostCluster = 8;
-constexpr int kPartBytes = 52 * 1024;     // of a row, per CTA, where there are rows enough: four CTAs per SM
+constexpr int kMostThreads = 512;
+constexpr int kPartBytes = 51712;         // of a row, per CTA, where there are rows enough: four CTAs per SM
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-
-// What the CTAs of a row tell each other.  The two sums have a reference of their own each: the rest may lie far below the
-// entries, and its logarithm counts all the same.
-struct PartSums {
-    float rest_most, entry_most;           // the largest logits
-    float rest, entries;                   // sums of 2^((z - most) c1)
-    double cross;                          // sum over the part's entries of q (log q - z / T)
-};
-// What the logits of a sum are taken relative to: the largest, unless there is nothing but -inf.  (The difference is formed before
-// it is scaled: a logit of the type's lowest value times c1 would be beyond it.)
-__device__ __forceinline__ float reference(float most) { return most == -INFINITY ? 0.0f : most; }
-__device__ __forceinline__ float power(float z, float from, float c1) { return exp2_fast((z - from) * c1); }
-
-template <typename T> __device__ __forceinline__ T lowest();
-template <> __device__ __forceinline__ float lowest<float>() { return __int_as_float(0xff800000); }
-template <> __device__ __forceinline__ __nv_bfloat16 lowest<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
-template <> __device__ __forceinline__ __half lowest<__half>() { return __ushort_as_half(0xfc00); }
-
-// Takes an element out of shared memory: -inf takes its place.  True for the one thread that found it there first (an element
-// that was -inf has no share in any sum, whoever claims it).
-__device__ __forceinline__ bool claim(float* p) { return atomicExch(reinterpret_cast<unsigned*>(p), 0xff800000u) != 0xff800000u; }
-template <typename T>
-__device__ __forceinline__ bool claim(T* p) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    unsigned* word = reinterpret_cast<unsigned*>(at & ~(uintptr_t)3);
-    const int up = (at & 2) ? 16 : 0;
-    const T low = lowest<T>();
-    const unsigned mark = *reinterpret_cast<const unsigned short*>(&low);
-    unsigned was = *reinterpret_cast<volatile unsigned*>(word);
-    while (true) {
-        if (((was >> up) & 0xffffu) == mark) return false;
-        const unsigned seen = atomicCAS(word, was, (was & ~(0xffffu << up)) | (mark << up));
-        if (seen == was) return true;
-        was = seen;
-    }
+// Two fp32 numbers side by side: one instruction for both.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
 }
+__device__ __forceinline__ float2 unpair(uint64_t p) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+    const float2 v = unpair(x);
+    return pair(exp2_fast(v.x), exp2_fast(v.y));
+}
+
+// The natural logarithm of a positive float to 2^-26 or so, whatever its size: the exponent's part in 64 bits.
+__device__ __forceinline__ double log_of(float x) {
+    if (!(x > 0.0f && x < INFINITY)) return (double)logf(x);
+    int e = 0;
+    if (x < 1.17549435e-38f) x *= 16777216.0f, e = -24;
+    const int bits = __float_as_int(x) - 0x3f3504f3;          // of sqrt(1/2): the rest lies in [sqrt(1/2), sqrt(2))
+    e += bits >> 23;
+    return (double)e * 0.693147180559945309417 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3));
+}
+
+// Powers of a part's logits: 2^(z c1 - from), or, where that could lose them, 2^((z - from) c1).
+struct Reference {
+    bool careful;
+    float from;
+    double exponent;                       // what the powers are relative to, in powers of two
+};
+
+// What the CTAs of a row tell each other: two sums, the exponents they are relative to, and
+// sum over the part's entries of q (log q - z / T).
+struct PartSums {
+    double rest_at, entries_at, cross;
+    float rest, entries;
+};
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -68,38 +85,75 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Over the CTA; `slots` has 32 places and is free again after the next barrier.
-__device__ __forceinline__ float cta_max(float v, float* slots) {
-    v = warp_max(v);
-    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int warps = blockDim.x >> 5;
-    return warp_max((int)(threadIdx.x & 31) < warps ? slots[threadIdx.x & 31] : -INFINITY);
-}
-__device__ __forceinline__ float cta_sum(float v, float* slots) {
-    v = warp_sum(v);
-    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int warps = blockDim.x >> 5;
-    return warp_sum((int)(threadIdx.x & 31) < warps ? slots[threadIdx.x & 31] : 0.0f);
-}
-__device__ __forceinline__ double cta_sum(double v, double* slots) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int warps = blockDim.x >> 5;
-    v = (int)(threadIdx.x & 31) < warps ? slots[threadIdx.x & 31] : 0.0;
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// Over groups of eight lanes.
+template <typename F>
+__device__ __forceinline__ F eight_sum(F v) {
+#pragma unroll
+    for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ double eight_max(double v) {
+#pragma unroll
+    for (int o = 4; o; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+__device__ __forceinline__ float warps_max(const float* slots, int warps) {
+    const int lane = threadIdx.x & 31;
+    return warp_max(lane < warps ? slots[lane] : -INFINITY);
+}
+__device__ __forceinline__ float warps_sum(const float* slots, int warps) {
+    const int lane = threadIdx.x & 31;
+    return warp_sum(lane < warps ? slots[lane] : 0.0f);
+}
 
-template <typename T>
-struct Granule {
-    static constexpr int kPer = 16 / (int)sizeof(T);
+// Sixteen bytes of a row as pairs of fp32 numbers.
+template <typename T> struct Granule;
+template <>
+struct Granule<float> {
+    static constexpr int kPer = 4, kPairs = 2;
     uint4 raw;
-    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&raw)[i]); }
+    __device__ __forceinline__ uint64_t get(int i) const { return i ? pair(__uint_as_float(raw.z), __uint_as_float(raw.w)) : pair(__uint_as_float(raw.x), __uint_as_float(raw.y)); }
+    __device__ __forceinline__ void set(int i, uint64_t p) {
+        const float2 v = unpair(p);
+        if (i) raw.z = __float_as_uint(v.x), raw.w = __float_as_uint(v.y);
+        else raw.x = __float_as_uint(v.x), raw.y = __float_as_uint(v.y);
+    }
+};
+template <>
+struct Granule<__nv_bfloat16> {
+    static constexpr int kPer = 8, kPairs = 4;
+    uint4 raw;
+    __device__ __forceinline__ uint32_t& word(int i) { return i == 0 ? raw.x : (i == 1 ? raw.y : (i == 2 ? raw.z : raw.w)); }
+    __device__ __forceinline__ uint64_t get(int i) const {
+        const uint32_t w = const_cast<Granule*>(this)->word(i);
+        return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+    __device__ __forceinline__ void set(int i, uint64_t p) {
+        const float2 v = unpair(p);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+        word(i) = *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+template <>
+struct Granule<__half> {
+    static constexpr int kPer = 8, kPairs = 4;
+    uint4 raw;
+    __device__ __forceinline__ uint32_t& word(int i) { return i == 0 ? raw.x : (i == 1 ? raw.y : (i == 2 ? raw.z : raw.w)); }
+    __device__ __forceinline__ uint64_t get(int i) const {
+        const uint32_t w = const_cast<Granule*>(this)->word(i);
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        return pair(v.x, v.y);
+    }
+    __device__ __forceinline__ void set(int i, uint64_t p) {
+        const float2 v = unpair(p);
+        const __half2 h = __floats2half2_rn(v.x, v.y);
+        word(i) = *reinterpret_cast<const uint32_t*>(&h);
+    }
 };
 
 __device__ __forceinline__ float teacher_at(const DistillArgs& a, int64_t row, int j) {
@@ -114,201 +168,288 @@ __device__ __forceinline__ int id_at(const DistillArgs& a, int64_t row, int j) {
     return id >= 0 && id < a.vocab ? (int)id : -1;
 }
 
+// The teacher's entries of a row in shared memory, and a byte for each granule of the part: which of its elements are entries.
+struct Entries {
+    int* col;                              // column; -1: none; -2: another CTA's; -3 - column: not the first of its column
+    float *value, *prob;                   // t, then the student's logit; q
+    unsigned* marks;
+    __device__ __forceinline__ Entries(char* at, int top) : col(reinterpret_cast<int*>(at)) {
+        value = reinterpret_cast<float*>(col + top);
+        prob = value + top;
+        marks = reinterpret_cast<unsigned*>(prob + top);
+    }
+    __device__ __forceinline__ unsigned marked(int granule) const { return reinterpret_cast<const unsigned char*>(marks)[granule]; }
+};
+constexpr size_t kEntryBytes = 12;
+
+// What stands for an element without a share.
+template <typename T> __device__ __forceinline__ T lowest();
+template <> __device__ __forceinline__ float lowest<float>() { return __int_as_float(0xff800000); }
+template <> __device__ __forceinline__ __nv_bfloat16 lowest<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
+template <> __device__ __forceinline__ __half lowest<__half>() { return __ushort_as_half(0xfc00); }
+
+// The largest element of a granule.
 template <typename T>
-__global__ void __launch_bounds__(512) k_distill(const __grid_constant__ DistillArgs a, const int granules_most) {
+__device__ __forceinline__ float most_of(const Granule<T>& g) {
+    float most = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < Granule<T>::kPairs; ++p) {
+        const float2 v = unpair(g.get(p));
+        most = fmaxf(most, fmaxf(v.x, v.y));
+    }
+    return most;
+}
+template <typename T, bool kCareful>
+__device__ __forceinline__ uint64_t powers(uint64_t z, uint64_t c, uint64_t minus_from) {
+    return exp2_pair(kCareful ? mul2(add2(z, minus_from), c) : fma2(z, c, minus_from));
+}
+// The sum of the powers of this thread's granules.  Entries become -inf on the way.
+template <typename T, bool kCareful>
+__device__ __forceinline__ float sum_powers(Granule<T>* cells, int n, const Entries& entry, const Reference& ref, float c1) {
+    const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from);
+    uint64_t s[2] = {0, 0};
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        Granule<T> g = cells[i];
+        const unsigned marked = entry.marked(i);
+        if (marked) {
+#pragma unroll
+            for (int e = 0; e < Granule<T>::kPer; ++e)
+                if (marked >> e & 1u) reinterpret_cast<T*>(&g.raw)[e] = lowest<T>();
+            cells[i] = g;
+        }
+#pragma unroll
+        for (int p = 0; p < Granule<T>::kPairs; ++p) s[p & 1] = add2(s[p & 1], powers<T, kCareful>(g.get(p), c, from));
+    }
+    const float2 v = unpair(add2(s[0], s[1]));
+    return v.x + v.y;
+}
+// The gradient of this thread's granules, entries left out.  kWhole: the gradient's granules lie like the logits'.
+template <typename T, bool kCareful, bool kWhole>
+__device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, const Entries& entry, int base, int vocab, T* g, const Reference& ref, float c1, float k1) {
+    constexpr int kPer = Granule<T>::kPer;
+    const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from), k = pair(k1, k1);
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const Granule<T> in = cells[i];
+        Granule<T> o;
+#pragma unroll
+        for (int p = 0; p < Granule<T>::kPairs; ++p) o.set(p, mul2(powers<T, kCareful>(in.get(p), c, from), k));
+        const int first = base + i * kPer;
+        const unsigned marked = entry.marked(i);
+        if (kWhole && !marked && first >= 0 && first + kPer <= vocab) {
+            *reinterpret_cast<uint4*>(g + first) = o.raw;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (first + e >= 0 && first + e < vocab && !(marked >> e & 1u)) g[first + e] = reinterpret_cast<const T*>(&o.raw)[e];
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant__ DistillArgs a, const int granules_most, const int ctas) {
     constexpr int kPer = Granule<T>::kPer;
     extern __shared__ __align__(16) char smem[];
     T* part = reinterpret_cast<T*>(smem);                                        // this CTA's granules
-    int* col = reinterpret_cast<int*>(smem + (size_t)granules_most * 16);         // [top] an entry's column, or -1
-    float* prob = reinterpret_cast<float*>(col + a.top);                          // [top] q
-    float* own = prob + a.top;                                                    // [top] the logit, where this CTA has it and claimed it
-    __shared__ float slots[3][32];
-    __shared__ double dslots[2][32];
-    __shared__ PartSums sums;
+    Granule<T>* cells = reinterpret_cast<Granule<T>*>(smem);
+    const Entries entry(smem + (size_t)granules_most * 16, a.top);
+    __shared__ float slots[2][kMostThreads / 32];
+    __shared__ PartSums sums[kMostCluster];
+    __shared__ double teacher_sum;                                               // of the q
     __shared__ int twice;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x, threads = blockDim.x;
-    const int64_t row = blockIdx.x / ctas;
+    const int tid = threadIdx.x, threads = blockDim.x, warps = threads >> 5, warp = tid >> 5, lane = tid & 31;
+    int rank = 0;
+    if (ctas > 1) {
+        asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // (waited for before others' shared memory is written)
+    }
+    const int64_t row = blockIdx.x / (unsigned)ctas;
     const T* z = static_cast<const T*>(a.logits) + row * a.ld;
     T* g = a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad : nullptr;
     // the row's granules, the first of which may begin before it; this CTA's share and its columns
     const int shift = (int)(reinterpret_cast<uintptr_t>(z) & 15u) / (int)sizeof(T);
     const int granules = (a.vocab + shift + kPer - 1) / kPer;
-    const int g0 = (int)((int64_t)granules * rank / ctas), g1 = (int)((int64_t)granules * (rank + 1) / ctas);
+    const int g0 = (int)((int64_t)granules * rank / ctas), g1 = (int)((int64_t)granules * (rank + 1) / ctas), n = g1 - g0;
     const int c0 = max(0, g0 * kPer - shift), c1 = min(a.vocab, g1 * kPer - shift);
     const int base = g0 * kPer - shift;                                          // column of part[0]
-    // where the gradient's 16-byte granules lie
-    const int g_shift = g ? (int)(reinterpret_cast<uintptr_t>(g) & 15u) / (int)sizeof(T) : 0;
 
     const float weight = a.weight ? a.weight[row] : 1.0f;
     if (weight == 0.0f) {                  // nothing is read of a row that does not count (the same for the whole cluster)
         if (g) for (int c = c0 + tid; c < c1; c += threads) g[c] = from_f32<T>(0.0f);
         if (a.loss && rank == 0 && tid == 0) a.loss[row] = 0.0f;
+        if (ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         return;
     }
-    const uint4* from = reinterpret_cast<const uint4*>(z - shift) + g0;
-    for (int i = tid; i < g1 - g0; i += threads)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)i * 16u), "l"(from + i) : "memory");
-    asm volatile("cp.async.commit_group;" ::: "memory");
-
-    // the teacher: log q_j = t_j / T - norm
-    if (tid == 0) twice = 0;
-    double norm;
-    if (a.teacher_lse) {
-        norm = (double)a.teacher_lse[row];
-    } else {
+    // every thread copies the granules that it works on
+    {
+        const uint4* from = reinterpret_cast<const uint4*>(z - shift) + g0;
+        for (int i = tid; i < n; i += threads)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)i * 16u), "l"(from + i) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // the entries, while the copies are under way: log q_j = t_j / T - norm.  (The loss is what is left of sums that nearly
+    // cancel: its terms are added in 64 bits.)
+    if (warp == 0) {
+        for (int i = lane; i < (n + 3) / 4; i += 32) entry.marks[i] = 0;
         float most = -INFINITY;
-        for (int j = tid; j < a.top; j += threads)
-            if (id_at(a, row, j) >= 0) most = fmaxf(most, teacher_at(a, row, j));
-        most = cta_max(most, slots[0]);
-        float sum = 0.0f;
-        for (int j = tid; j < a.top; j += threads)
-            if (id_at(a, row, j) >= 0 && most != -INFINITY) sum += expf((float)(((double)teacher_at(a, row, j) - (double)most) * a.inv_temp));
-        sum = cta_sum(sum, slots[1]);
-        norm = most == -INFINITY ? 0.0 : (double)most * a.inv_temp + log((double)sum);
-    }
-    // in 64 bits: the loss is what is left of sums that nearly cancel
-    double q_sum = 0.0;
-    for (int j = tid; j < a.top; j += threads) {
-        const int id = id_at(a, row, j);
-        const float q = id >= 0 ? expf((float)((double)teacher_at(a, row, j) * a.inv_temp - norm)) : 0.0f;
-        col[j] = id;
-        prob[j] = q;
-        q_sum += (double)q;
-    }
-    q_sum = cta_sum(q_sum, dslots[0]);
-
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();
-    // what the first and last granule hold beside the row
-    if (tid < kPer) {
-        if (base + tid < 0) part[tid] = lowest<T>();
-        const int last = (g1 - g0 - 1) * kPer + tid;
-        if (g1 > g0 && base + last >= a.vocab) part[last] = lowest<T>();
-    }
-    double cross = 0.0;
-    for (int j = tid; j < a.top; j += threads) {
-        const bool here = col[j] >= c0 && col[j] < c1;
-        const float v = here ? to_f32(part[col[j] - base]) : 0.0f;
-        own[j] = v;
-        if (here && prob[j] != 0.0f)
-            cross += (double)prob[j] * ((double)teacher_at(a, row, j) * a.inv_temp - norm - (double)v * ((double)a.c1 * 0.693147180559945309417));
-    }
-    __syncthreads();
-    float entry_most = -INFINITY, rest_most = -INFINITY;
-    for (int j = tid; j < a.top; j += threads) {
-        const bool here = col[j] >= c0 && col[j] < c1;
-        if (!here) {
-            if (col[j] >= 0) col[j] = -2;              // another CTA's
-        } else if (claim(part + (col[j] - base))) {
-            entry_most = fmaxf(entry_most, own[j]);
+        for (int j = lane; j < a.top; j += 32) {
+            const int id = id_at(a, row, j);
+            const float t = teacher_at(a, row, j);
+            entry.col[j] = id;
+            entry.value[j] = t;
+            if (id >= 0) most = fmaxf(most, t);
+        }
+        double norm;
+        if (a.teacher_lse) {
+            norm = (double)a.teacher_lse[row];
         } else {
-            if (own[j] != -INFINITY) twice = 1;
-            col[j] = -3 - col[j];                      // not the first of its column, or an element without any share: below -2
+            most = warp_max(most);
+            float sum = 0.0f;
+            for (int j = lane; j < a.top; j += 32)
+                if (entry.col[j] >= 0 && most != -INFINITY) sum += expf((float)(((double)entry.value[j] - (double)most) * a.inv_temp));
+            norm = most == -INFINITY ? 0.0 : (double)most * a.inv_temp + log_of(warp_sum(sum));
+        }
+        if (lane == 0) twice = 0;
+        __syncwarp();
+        double q_sum = 0.0, cross = 0.0;
+        float entry_most = -INFINITY;
+        bool again = false;
+        for (int j = lane; j < a.top; j += 32) {
+            const int col = entry.col[j];
+            if (col < 0) {
+                entry.prob[j] = 0.0f;
+                continue;
+            }
+            const double log_q = (double)entry.value[j] * a.inv_temp - norm;
+            const float q = expf((float)log_q);
+            entry.prob[j] = q;
+            q_sum += (double)q;
+            if (col < c0 || col >= c1) {
+                entry.col[j] = -2;
+                continue;
+            }
+            const float own = to_f32(z[col]);
+            entry.value[j] = own;
+            if (q != 0.0f) cross += (double)q * (log_q - (double)own * ((double)a.c1 * 0.693147180559945309417));
+            const int cell = (col - base) / kPer, bit = (cell & 3) * 8 + (col - base) % kPer;
+            if (atomicOr(entry.marks + (cell >> 2), 1u << bit) >> bit & 1u) {
+                entry.col[j] = -3 - col;
+                again = true;
+            } else {
+                entry_most = fmaxf(entry_most, own);
+            }
+        }
+        entry_most = warp_max(entry_most);
+        const float near = entry_most == -INFINITY ? 0.0f : entry_most;
+        float entries = 0.0f;
+        for (int j = lane; j < a.top; j += 32)
+            if (entry.col[j] >= 0) entries += exp2_fast((entry.value[j] - near) * a.c1);
+        entries = warp_sum(entries);
+        q_sum = warp_sum(q_sum);
+        cross = warp_sum(cross);
+        again = __any_sync(0xffffffffu, again);
+        if (lane == 0) {
+            teacher_sum = q_sum;
+            if (again) twice = 1;
+            sums[rank] = PartSums{0.0, (double)near * (double)a.c1, cross, 0.0f, entries};
         }
     }
-    entry_most = cta_max(entry_most, slots[2]);
-    const Granule<T>* cells = reinterpret_cast<const Granule<T>*>(part);
-    for (int i = tid; i < g1 - g0; i += threads) {
-        const Granule<T> c = cells[i];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) rest_most = fmaxf(rest_most, c.get(e));
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // what the first and last granule hold beside the row
+    if (n > 0 && tid == 0)
+        for (int c = base; c < 0; ++c) part[c - base] = lowest<T>();
+    if (n > 0 && tid == (n - 1) % threads)
+        for (int c = max(c1, base); c < base + n * kPer; ++c) part[c - base] = lowest<T>();
+    // what the powers are relative to: the largest of a granule of every thread, which is seldom far from the largest of all
+    {
+        const float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
+        if (lane == 0) slots[0][warp] = most;
     }
-    rest_most = cta_max(rest_most, slots[1]);
-    float from_rest = reference(rest_most), rest = 0.0f, entries = 0.0f;
-    for (int i = tid; i < g1 - g0; i += threads) {
-        const Granule<T> c = cells[i];
-        float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) s[e & 1] += power(c.get(e), from_rest, a.c1);
-        rest += s[0] + s[1];
+    __syncthreads();
+    Reference ref{false, 0.0f, 0.0};
+    {
+        const float most = warps_max(slots[0], warps);
+        ref.from = most == -INFINITY ? 0.0f : most * a.c1;
+        ref.exponent = (double)ref.from;
     }
-    float from_entry = reference(entry_most);
-    for (int j = tid; j < a.top; j += threads)
-        if (col[j] >= 0) entries += power(own[j], from_entry, a.c1);
-    rest = cta_sum(rest, slots[0]);
-    entries = cta_sum(entries, slots[2]);
-    cross = cta_sum(cross, dslots[1]);
+    float rest = warp_sum(sum_powers<T, false>(cells, n, entry, ref, a.c1));
+    if (lane == 0) slots[1][warp] = rest;
+    __syncthreads();
+    rest = warps_sum(slots[1], warps);
+    // the sample is too far off (or something is no number).  Powers and factors below 2^-126 are 0: within these bounds no
+    // probability above 2^-96 is lost
+    if (!(rest > 9.5367431640625e-07f && rest < 1073741824.0f)) {             // 2^-20, 2^30
+        float most = -INFINITY;
+        for (int i = tid; i < n; i += threads) most = fmaxf(most, most_of<T>(cells[i]));
+        most = warp_max(most);
+        if (lane == 0) slots[0][warp] = most;
+        __syncthreads();
+        most = warps_max(slots[0], warps);
+        ref.careful = true;
+        ref.from = most == -INFINITY ? 0.0f : most;
+        ref.exponent = (double)ref.from * (double)a.c1;
+        rest = warp_sum(sum_powers<T, true>(cells, n, entry, ref, a.c1));
+        __syncthreads();
+        if (lane == 0) slots[1][warp] = rest;
+        __syncthreads();
+        rest = warps_sum(slots[1], warps);
+    }
+    PartSums mine{};
+    if (ctas == 1 || warp == 0) {
+        mine = sums[rank];
+        mine.rest = rest;
+        mine.rest_at = ref.exponent;
+        __syncwarp();
+    }
     if (ctas > 1) {
-        if (tid == 0) sums = PartSums{rest_most, entry_most, rest, entries, cross};
-        cluster.sync();
-        rest_most = entry_most = -INFINITY;
-        for (int c = 0; c < ctas; ++c) {
-            const PartSums* o = cluster.map_shared_rank(&sums, c);
-            rest_most = fmaxf(rest_most, o->rest_most);
-            entry_most = fmaxf(entry_most, o->entry_most);
-        }
-        from_rest = reference(rest_most);
-        from_entry = reference(entry_most);
-        rest = entries = 0.0f;
-        cross = 0.0;
-        for (int c = 0; c < ctas; ++c) {               // (a part without any is 0, or NaN, whatever it is multiplied by)
-            const PartSums* o = cluster.map_shared_rank(&sums, c);
-            rest += o->rest_most == -INFINITY ? o->rest : o->rest * power(o->rest_most, from_rest, a.c1);
-            entries += o->entry_most == -INFINITY ? o->entries : o->entries * power(o->entry_most, from_entry, a.c1);
-            cross += o->cross;
-        }
-        cluster.sync();                    // nobody leaves while others read its sums
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all CTAs run: their shared memory may be written
+        if (tid < ctas) *cooperative_groups::this_cluster().map_shared_rank(&sums[rank], tid) = mine;
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if ((lane & 7) < ctas) mine = sums[lane & 7];
     }
-    // total: the sum over the vocabulary relative to from_all
-    const float from_all = rest_most == -INFINITY ? from_entry : (entry_most == -INFINITY ? from_rest : fmaxf(from_rest, from_entry));
-    const float rest_up = power(from_rest, from_all, a.c1);
-    const float total = (rest == 0.0f ? 0.0f : rest * rest_up) + (entries == 0.0f ? 0.0f : entries * power(from_entry, from_all, a.c1));
+    // a lane for each CTA's sums, four times over
+    const bool some = (lane & 7) < ctas;
+    const float rest_here = rest;
+    const double none = -(double)INFINITY, rest_at = some && !(mine.rest == 0.0f) ? mine.rest_at : none;
+    const double entries_at = some && !(mine.entries == 0.0f) ? mine.entries_at : none;
+    const double rest_most = eight_max(rest_at), all_most = fmax(rest_most, eight_max(entries_at));
+    const float total = eight_sum((rest_at == none ? 0.0f : mine.rest * exp2_fast((float)(rest_at - all_most))) +
+                                  (entries_at == none ? 0.0f : mine.entries * exp2_fast((float)(entries_at - all_most))));
+    rest = eight_sum(rest_at == none ? 0.0f : mine.rest * exp2_fast((float)(rest_at - rest_most)));
+    const double q_sum = teacher_sum;
     // the teacher's probability outside its entries; none where there is no other logit
     const float left = a.teacher_lse && !(rest == 0.0f) ? (float)fmax(0.0, 1.0 - q_sum) : 0.0f;
     const float mass = (float)(q_sum + (double)left);
-    if (a.loss && rank == 0 && tid == 0) {
-        const double by = (double)a.c1 * 0.693147180559945309417, lse = (double)from_all * by + log((double)total);
-        double loss = cross + q_sum * lse;
-        if (left > 0.0f) loss += (double)left * (log((double)left) - log((double)rest) - (double)from_rest * by + lse);
-        if (q_sum == 0.0 && left == 0.0f) loss = 0.0;
-        a.loss[row] = (float)(loss * (double)weight * a.loss_factor);
+    if (a.loss && rank == 0 && warp == 0) {
+        const double cross = eight_sum(some ? mine.cross : 0.0);
+        if (lane == 0) {
+            const double ln2 = 0.693147180559945309417, lse = all_most * ln2 + log_of(total);
+            double loss = cross + q_sum * lse;
+            if (left > 0.0f) loss += (double)left * (log_of(left) - log_of(rest) - rest_most * ln2 + lse);
+            if (q_sum == 0.0 && left == 0.0f) loss = 0.0;
+            a.loss[row] = (float)(loss * (double)weight * a.loss_factor);
+        }
     }
     if (!g) return;
     const float f = weight * a.grad_factor;
     const float k_top = mass / total * f;
-    // (rest = 0: nothing but -inf, whose share is 0, and NaN where the entries have none either)
-    const float k_rest = rest == 0.0f ? 0.0f * k_top : (mass * rest_up / total - left / rest) * f;
-    if (g_shift == shift) {
-        uint4* to = reinterpret_cast<uint4*>(g - shift) + g0;
-        for (int i = tid; i < g1 - g0; i += threads) {
-            const Granule<T> c = cells[i];
-            Granule<T> o;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) reinterpret_cast<T*>(&o.raw)[e] = from_f32<T>(power(c.get(e), from_rest, a.c1) * k_rest);
-            const int first = base + i * kPer;
-            if (first >= 0 && first + kPer <= a.vocab) {
-                to[i] = o.raw;
-            } else {
-#pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    if (first + e >= 0 && first + e < a.vocab) g[first + e] = reinterpret_cast<const T*>(&o.raw)[e];
-            }
-        }
-    } else {
-        for (int c = c0 + tid; c < c1; c += threads) g[c] = from_f32<T>(power(to_f32(part[c - base]), from_rest, a.c1) * k_rest);
-    }
-    __syncthreads();
+    // (a part with nothing but -inf: the share is 0, and NaN where the whole row has no other)
+    const float k_rest = rest_here == 0.0f ? 0.0f * k_top : (mass / total * exp2_fast((float)(ref.exponent - all_most)) - left / rest * exp2_fast((float)(ref.exponent - rest_most))) * f;
+    const bool whole = (reinterpret_cast<uintptr_t>(g) & 15u) == (reinterpret_cast<uintptr_t>(z) & 15u);
+    if (ref.careful) write_grad<T, true, false>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
+    else if (whole) write_grad<T, false, true>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
+    else write_grad<T, false, false>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
     // the entries' own elements: the probabilities of a column's entries added in their order
     for (int j = tid; j < a.top; j += threads) {
-        int c = col[j];
-        float v = own[j], q = prob[j];
-        if (c < -2) {                      // no share in the sums: an element that is -inf; its first entry writes it
-            c = -3 - c;
-            if (v > -INFINITY || v != v) continue;
-            bool earlier = false;
-            for (int i = 0; i < j; ++i) earlier |= col[i] == col[j];
-            if (earlier) continue;
-            for (int i = j + 1; i < a.top; ++i)
-                if (col[i] == col[j]) q += prob[i];
-        } else if (c < 0) {
-            continue;
-        } else if (twice) {
+        const int c = entry.col[j];
+        if (c < 0) continue;
+        float q = entry.prob[j];
+        if (twice) {
             q = 0.0f;
             for (int i = 0; i < a.top; ++i)
-                if (col[i] == c || col[i] == -3 - c) q += prob[i];
+                if (entry.col[i] == c || entry.col[i] == -3 - c) q += entry.prob[i];
         }
-        g[c] = from_f32<T>(power(v, from_all, a.c1) * k_top - q * f);
+        g[c] = from_f32<T>(exp2_fast((float)((double)entry.value[j] * (double)a.c1 - all_most)) * k_top - q * f);
     }
 }
 
@@ -321,10 +462,10 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     while (ctas < kMostCluster && a.rows * ctas < 2 * 148 && bytes / ctas > 8 * 1024) ctas *= 2;
     const int64_t blocks = a.rows * ctas;
     if (blocks > 0x7fffffffLL) return DEFT_ERR_TOO_LARGE;
-    const int granules = (int)((bytes + 15) / 16 / ctas + 2);
-    const size_t smem = (size_t)granules * 16 + (size_t)a.top * 12;
-    int threads = 128;
-    while (threads < 512 && granules > threads * 8) threads *= 2;
+    const int granules = ((int)((bytes + 15) / 16 / ctas) + 2 + 3) & ~3;
+    const size_t smem = (size_t)granules * 17 + (size_t)a.top * kEntryBytes;
+    int threads = 32;
+    while (threads < kMostThreads && granules > threads * 12) threads *= 2;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)ctas;
@@ -335,12 +476,12 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = ctas > 1 ? 1 : 0;
     return with_type(type, [&](auto t) -> deft_status {
         using T = decltype(t);
         auto kernel = k_distill<T>;
         if (smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, granules));
+        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, granules, ctas));
         return DEFT_OK;
     });
 }

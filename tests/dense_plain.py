@@ -147,8 +147,9 @@ def distill(logits, ids, teacher, teacher_lse=None, temperature=1.0, weight=None
             loss[r] = w * temperature ** 2 * value
             loss_tol[r] = abs(w) * temperature ** 2 * rel * (1 + (logs.max() if logs.size else 0.0) + far)
             grad[r] = scale * w * temperature * g
-            # powers of two below 2^-126 are 0: of what the largest logit's is 1, in both terms of an element
-            grad_tol[r] = abs(scale * w * temperature) * (rel * (p * (q.sum() + left) + target + (left + 1.0) * rest) + 2.0 ** -125)
+            # powers and their factors below 2^-126 are 0; they are relative to sums between 2^-20 and 2^30: at most 2^-96 is lost,
+            # in each of an element's two terms
+            grad_tol[r] = abs(scale * w * temperature) * (rel * (p * (q.sum() + left) + target + (left + 1.0) * rest) + 2.0 ** -95)
             if np.isnan(grad[r]).any():
                 grad_tol[r] = 0.0
     return torch.from_numpy(loss), torch.from_numpy(grad), torch.from_numpy(loss_tol), torch.from_numpy(grad_tol)
