@@ -12,7 +12,7 @@ namespace deft {
 namespace {
 
 constexpr int kMostCluster = 8;
-constexpr int kMostThreads = 512;
+constexpr int kMostThreads = 512;         // that work on the row
 constexpr int kPartBytes = 51712;         // of a row, per CTA, where there are rows enough: four CTAs per SM
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -203,50 +203,86 @@ template <typename T, bool kCareful>
 __device__ __forceinline__ uint64_t powers(uint64_t z, uint64_t c, uint64_t minus_from) {
     return exp2_pair(kCareful ? mul2(add2(z, minus_from), c) : fma2(z, c, minus_from));
 }
-// The sum of the powers of this thread's granules.  Entries become -inf on the way.
+// A granule of this thread without its entries.
+template <typename T>
+__device__ __forceinline__ Granule<T> rest_of(const Granule<T>* cells, int i, const Entries& entry) {
+    Granule<T> g = cells[i];
+    const unsigned marked = entry.marked(i);
+    if (marked) {
+#pragma unroll
+        for (int e = 0; e < Granule<T>::kPer; ++e)
+            if (marked >> e & 1u) reinterpret_cast<T*>(&g.raw)[e] = lowest<T>();
+    }
+    return g;
+}
+// The sum of the powers of this thread's granules.
 template <typename T, bool kCareful>
-__device__ __forceinline__ float sum_powers(Granule<T>* cells, int n, const Entries& entry, const Reference& ref, float c1) {
+__device__ __forceinline__ float sum_powers(const Granule<T>* cells, int n, int threads, const Entries& entry, const Reference& ref, float c1) {
     const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from);
     uint64_t s[2] = {0, 0};
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        Granule<T> g = cells[i];
-        const unsigned marked = entry.marked(i);
-        if (marked) {
-#pragma unroll
-            for (int e = 0; e < Granule<T>::kPer; ++e)
-                if (marked >> e & 1u) reinterpret_cast<T*>(&g.raw)[e] = lowest<T>();
-            cells[i] = g;
-        }
+    for (int i = threadIdx.x; i < n; i += threads) {
+        const Granule<T> g = rest_of(cells, i, entry);
 #pragma unroll
         for (int p = 0; p < Granule<T>::kPairs; ++p) s[p & 1] = add2(s[p & 1], powers<T, kCareful>(g.get(p), c, from));
     }
     const float2 v = unpair(add2(s[0], s[1]));
     return v.x + v.y;
 }
-// The gradient of this thread's granules, entries left out.  kWhole: the gradient's granules lie like the logits'.
+// The gradient of this thread's granules, as if there were no entries among them.  kWhole: the gradient's granules lie like the logits'.
 template <typename T, bool kCareful, bool kWhole>
-__device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, const Entries& entry, int base, int vocab, T* g, const Reference& ref, float c1, float k1) {
+__device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, int threads, int base, int vocab, T* g, const Reference& ref, float c1, float k1) {
     constexpr int kPer = Granule<T>::kPer;
     const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from), k = pair(k1, k1);
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = threadIdx.x; i < n; i += threads) {
         const Granule<T> in = cells[i];
         Granule<T> o;
 #pragma unroll
         for (int p = 0; p < Granule<T>::kPairs; ++p) o.set(p, mul2(powers<T, kCareful>(in.get(p), c, from), k));
         const int first = base + i * kPer;
-        const unsigned marked = entry.marked(i);
-        if (kWhole && !marked && first >= 0 && first + kPer <= vocab) {
+        if (kWhole && first >= 0 && first + kPer <= vocab) {
             *reinterpret_cast<uint4*>(g + first) = o.raw;
         } else {
-#pragma unroll
             for (int e = 0; e < kPer; ++e)
-                if (first + e >= 0 && first + e < vocab && !(marked >> e & 1u)) g[first + e] = reinterpret_cast<const T*>(&o.raw)[e];
+                if (first + e >= 0 && first + e < vocab) g[first + e] = reinterpret_cast<const T*>(&o.raw)[e];
         }
     }
 }
 
+// What the first warp works out for all: factors of the gradient, the exponent that the row's sum is relative to.
+struct Factors {
+    double all_at;
+    float rest, top;
+};
+
+// The loss of a row and the factors of its gradient from the CTAs' sums.  One warp; a lane for each CTA, four times over.
+__device__ __forceinline__ Factors factors_of(const DistillArgs& a, const PartSums& o, float rest_here, double here_at, double q_sum, float weight, int64_t row, bool write_loss) {
+    const double none = -(double)INFINITY, rest_at = !(o.rest == 0.0f) ? o.rest_at : none, entries_at = !(o.entries == 0.0f) ? o.entries_at : none;
+    const double rest_most = eight_max(rest_at), all_most = fmax(rest_most, eight_max(entries_at));
+    const float total = eight_sum((rest_at == none ? 0.0f : o.rest * exp2_fast((float)(rest_at - all_most))) +
+                                  (entries_at == none ? 0.0f : o.entries * exp2_fast((float)(entries_at - all_most))));
+    const float all_rest = eight_sum(rest_at == none ? 0.0f : o.rest * exp2_fast((float)(rest_at - rest_most)));
+    // the teacher's probability outside its entries; none where there is no other logit
+    const float left = a.teacher_lse && !(all_rest == 0.0f) ? (float)fmax(0.0, 1.0 - q_sum) : 0.0f;
+    const float mass = (float)(q_sum + (double)left);
+    const float f = weight * a.grad_factor, top = mass / total * f;
+    // (a part with nothing but -inf: the share is 0, and NaN where the whole row has no other)
+    const float rest = rest_here == 0.0f ? 0.0f * top : (mass / total * exp2_fast((float)(here_at - all_most)) - left / all_rest * exp2_fast((float)(here_at - rest_most))) * f;
+    if (write_loss) {
+        const double cross = eight_sum(o.cross);
+        if ((threadIdx.x & 31) == 0) {
+            const double ln2 = 0.693147180559945309417, lse = all_most * ln2 + log_of(total);
+            double loss = cross + q_sum * lse;
+            if (left > 0.0f) loss += (double)left * (log_of(left) - log_of(all_rest) - rest_most * ln2 + lse);
+            if (q_sum == 0.0 && left == 0.0f) loss = 0.0;
+            a.loss[row] = (float)(loss * (double)weight * a.loss_factor);
+        }
+    }
+    return Factors{all_most, rest, top};
+}
+
+// The last warp of a CTA works on the entries, the others on the part of the row.
 template <typename T>
-__global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant__ DistillArgs a, const int granules_most, const int ctas) {
+__global__ void __launch_bounds__(kMostThreads + 32, 1) k_distill(const __grid_constant__ DistillArgs a, const int granules_most, const int ctas) {
     constexpr int kPer = Granule<T>::kPer;
     extern __shared__ __align__(16) char smem[];
     T* part = reinterpret_cast<T*>(smem);                                        // this CTA's granules
@@ -254,9 +290,10 @@ __global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant_
     const Entries entry(smem + (size_t)granules_most * 16, a.top);
     __shared__ float slots[2][kMostThreads / 32];
     __shared__ PartSums sums[kMostCluster];
-    __shared__ double teacher_sum;                                               // of the q
+    __shared__ Factors factors;
     __shared__ int twice;
-    const int tid = threadIdx.x, threads = blockDim.x, warps = threads >> 5, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, threads = (int)blockDim.x - 32, warps = threads >> 5, warp = tid >> 5, lane = tid & 31;
+    const bool for_entries = warp == warps;
     int rank = 0;
     if (ctas > 1) {
         asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -274,93 +311,73 @@ __global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant_
 
     const float weight = a.weight ? a.weight[row] : 1.0f;
     if (weight == 0.0f) {                  // nothing is read of a row that does not count (the same for the whole cluster)
-        if (g) for (int c = c0 + tid; c < c1; c += threads) g[c] = from_f32<T>(0.0f);
+        if (g) for (int c = c0 + tid; c < c1; c += blockDim.x) g[c] = from_f32<T>(0.0f);
         if (a.loss && rank == 0 && tid == 0) a.loss[row] = 0.0f;
         if (ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         return;
     }
-    // every thread copies the granules that it works on
-    {
-        const uint4* from = reinterpret_cast<const uint4*>(z - shift) + g0;
-        for (int i = tid; i < n; i += threads)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)i * 16u), "l"(from + i) : "memory");
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    // the entries, while the copies are under way: log q_j = t_j / T - norm.  (The loss is what is left of sums that nearly
-    // cancel: its terms are added in 64 bits.)
-    if (warp == 0) {
+    double norm = 0.0, q_sum = 0.0, cross = 0.0;   // of the last warp: log q_j = t_j / T - norm; sums of q and, over the part's entries, q log q
+    if (for_entries) {
+        // (The loss is what is left of sums that nearly cancel: its terms are added in 64 bits.)
+        int id[2] = {-1, -1};
+        float t[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)        // the first entries' loads are under way together
+            if (lane + 32 * i < a.top) {
+                id[i] = id_at(a, row, lane + 32 * i);
+                t[i] = teacher_at(a, row, lane + 32 * i);
+            }
+        if (a.teacher_lse) norm = (double)a.teacher_lse[row];
         for (int i = lane; i < (n + 3) / 4; i += 32) entry.marks[i] = 0;
+        if (lane == 0) twice = 0;
         float most = -INFINITY;
-        for (int j = lane; j < a.top; j += 32) {
-            const int id = id_at(a, row, j);
-            const float t = teacher_at(a, row, j);
-            entry.col[j] = id;
-            entry.value[j] = t;
-            if (id >= 0) most = fmaxf(most, t);
-        }
-        double norm;
-        if (a.teacher_lse) {
-            norm = (double)a.teacher_lse[row];
-        } else {
+        auto keep = [&](int j, int col, float value) {
+            entry.col[j] = col;
+            entry.value[j] = value;
+            if (col >= 0) most = fmaxf(most, value);
+        };
+        if (lane < a.top) keep(lane, id[0], t[0]);
+        if (lane + 32 < a.top) keep(lane + 32, id[1], t[1]);
+        for (int j = lane + 64; j < a.top; j += 32) keep(j, id_at(a, row, j), teacher_at(a, row, j));
+        if (!a.teacher_lse) {
             most = warp_max(most);
             float sum = 0.0f;
             for (int j = lane; j < a.top; j += 32)
                 if (entry.col[j] >= 0 && most != -INFINITY) sum += expf((float)(((double)entry.value[j] - (double)most) * a.inv_temp));
             norm = most == -INFINITY ? 0.0 : (double)most * a.inv_temp + log_of(warp_sum(sum));
         }
-        if (lane == 0) twice = 0;
         __syncwarp();
-        double q_sum = 0.0, cross = 0.0;
-        float entry_most = -INFINITY;
-        bool again = false;
         for (int j = lane; j < a.top; j += 32) {
             const int col = entry.col[j];
-            if (col < 0) {
-                entry.prob[j] = 0.0f;
-                continue;
-            }
             const double log_q = (double)entry.value[j] * a.inv_temp - norm;
-            const float q = expf((float)log_q);
+            const float q = col >= 0 ? expf((float)log_q) : 0.0f;
             entry.prob[j] = q;
             q_sum += (double)q;
+            if (col < 0) continue;
             if (col < c0 || col >= c1) {
                 entry.col[j] = -2;
                 continue;
             }
-            const float own = to_f32(z[col]);
-            entry.value[j] = own;
-            if (q != 0.0f) cross += (double)q * (log_q - (double)own * ((double)a.c1 * 0.693147180559945309417));
+            if (q != 0.0f) cross += (double)q * log_q;
             const int cell = (col - base) / kPer, bit = (cell & 3) * 8 + (col - base) % kPer;
             if (atomicOr(entry.marks + (cell >> 2), 1u << bit) >> bit & 1u) {
                 entry.col[j] = -3 - col;
-                again = true;
-            } else {
-                entry_most = fmaxf(entry_most, own);
+                twice = 1;
             }
         }
-        entry_most = warp_max(entry_most);
-        const float near = entry_most == -INFINITY ? 0.0f : entry_most;
-        float entries = 0.0f;
-        for (int j = lane; j < a.top; j += 32)
-            if (entry.col[j] >= 0) entries += exp2_fast((entry.value[j] - near) * a.c1);
-        entries = warp_sum(entries);
         q_sum = warp_sum(q_sum);
-        cross = warp_sum(cross);
-        again = __any_sync(0xffffffffu, again);
-        if (lane == 0) {
-            teacher_sum = q_sum;
-            if (again) twice = 1;
-            sums[rank] = PartSums{0.0, (double)near * (double)a.c1, cross, 0.0f, entries};
-        }
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    // what the first and last granule hold beside the row
-    if (n > 0 && tid == 0)
-        for (int c = base; c < 0; ++c) part[c - base] = lowest<T>();
-    if (n > 0 && tid == (n - 1) % threads)
-        for (int c = max(c1, base); c < base + n * kPer; ++c) part[c - base] = lowest<T>();
-    // what the powers are relative to: the largest of a granule of every thread, which is seldom far from the largest of all
-    {
+    } else {
+        // every thread copies the granules that it works on
+        const uint4* from = reinterpret_cast<const uint4*>(z - shift) + g0;
+        for (int i = tid; i < n; i += threads)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)i * 16u), "l"(from + i) : "memory");
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        // what the first and last granule hold beside the row
+        if (n > 0 && tid == 0)
+            for (int c = base; c < 0; ++c) part[c - base] = lowest<T>();
+        if (n > 0 && tid == (n - 1) % threads)
+            for (int c = max(c1, base); c < base + n * kPer; ++c) part[c - base] = lowest<T>();
+        // what the powers are relative to: the largest of a granule of every thread, which is seldom far from the largest of all
         const float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
         if (lane == 0) slots[0][warp] = most;
     }
@@ -371,30 +388,54 @@ __global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant_
         ref.from = most == -INFINITY ? 0.0f : most * a.c1;
         ref.exponent = (double)ref.from;
     }
-    float rest = warp_sum(sum_powers<T, false>(cells, n, entry, ref, a.c1));
-    if (lane == 0) slots[1][warp] = rest;
+    if (for_entries) {                     // the entries' logits
+        float most = -INFINITY;
+        for (int j = lane; j < a.top; j += 32) {
+            const int col = entry.col[j];
+            if (col == -1 || col == -2) continue;
+            const float own = to_f32(part[(col < 0 ? -3 - col : col) - base]);
+            entry.value[j] = own;
+            if (entry.prob[j] != 0.0f) cross -= (double)entry.prob[j] * ((double)own * ((double)a.c1 * 0.693147180559945309417));
+            if (col >= 0) most = fmaxf(most, own);
+        }
+        most = warp_max(most);
+        const float near = most == -INFINITY ? 0.0f : most;
+        float entries = 0.0f;
+        for (int j = lane; j < a.top; j += 32)
+            if (entry.col[j] >= 0) entries += exp2_fast((entry.value[j] - near) * a.c1);
+        entries = warp_sum(entries);
+        cross = warp_sum(cross);
+        if (lane == 0) sums[rank] = PartSums{0.0, (double)near * (double)a.c1, cross, 0.0f, entries};
+        __syncwarp();
+    } else {
+        const float rest = warp_sum(sum_powers<T, false>(cells, n, threads, entry, ref, a.c1));
+        if (lane == 0) slots[1][warp] = rest;
+    }
     __syncthreads();
-    rest = warps_sum(slots[1], warps);
+    float rest = warps_sum(slots[1], warps);
     // the sample is too far off (or something is no number).  Powers and factors below 2^-126 are 0: within these bounds no
     // probability above 2^-96 is lost
     if (!(rest > 9.5367431640625e-07f && rest < 1073741824.0f)) {             // 2^-20, 2^30
-        float most = -INFINITY;
-        for (int i = tid; i < n; i += threads) most = fmaxf(most, most_of<T>(cells[i]));
-        most = warp_max(most);
-        if (lane == 0) slots[0][warp] = most;
+        if (!for_entries) {
+            float most = -INFINITY;
+            for (int i = tid; i < n; i += threads) most = fmaxf(most, most_of<T>(rest_of(cells, i, entry)));
+            most = warp_max(most);
+            if (lane == 0) slots[0][warp] = most;
+        }
         __syncthreads();
-        most = warps_max(slots[0], warps);
+        const float most = warps_max(slots[0], warps);
         ref.careful = true;
         ref.from = most == -INFINITY ? 0.0f : most;
         ref.exponent = (double)ref.from * (double)a.c1;
-        rest = warp_sum(sum_powers<T, true>(cells, n, entry, ref, a.c1));
-        __syncthreads();
-        if (lane == 0) slots[1][warp] = rest;
+        if (!for_entries) {
+            rest = warp_sum(sum_powers<T, true>(cells, n, threads, entry, ref, a.c1));
+            if (lane == 0) slots[1][warp] = rest;
+        }
         __syncthreads();
         rest = warps_sum(slots[1], warps);
     }
     PartSums mine{};
-    if (ctas == 1 || warp == 0) {
+    if (for_entries) {
         mine = sums[rank];
         mine.rest = rest;
         mine.rest_at = ref.exponent;
@@ -402,45 +443,32 @@ __global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant_
     }
     if (ctas > 1) {
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all CTAs run: their shared memory may be written
-        if (tid < ctas) *cooperative_groups::this_cluster().map_shared_rank(&sums[rank], tid) = mine;
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if ((lane & 7) < ctas) mine = sums[lane & 7];
-    }
-    // a lane for each CTA's sums, four times over
-    const bool some = (lane & 7) < ctas;
-    const float rest_here = rest;
-    const double none = -(double)INFINITY, rest_at = some && !(mine.rest == 0.0f) ? mine.rest_at : none;
-    const double entries_at = some && !(mine.entries == 0.0f) ? mine.entries_at : none;
-    const double rest_most = eight_max(rest_at), all_most = fmax(rest_most, eight_max(entries_at));
-    const float total = eight_sum((rest_at == none ? 0.0f : mine.rest * exp2_fast((float)(rest_at - all_most))) +
-                                  (entries_at == none ? 0.0f : mine.entries * exp2_fast((float)(entries_at - all_most))));
-    rest = eight_sum(rest_at == none ? 0.0f : mine.rest * exp2_fast((float)(rest_at - rest_most)));
-    const double q_sum = teacher_sum;
-    // the teacher's probability outside its entries; none where there is no other logit
-    const float left = a.teacher_lse && !(rest == 0.0f) ? (float)fmax(0.0, 1.0 - q_sum) : 0.0f;
-    const float mass = (float)(q_sum + (double)left);
-    if (a.loss && rank == 0 && warp == 0) {
-        const double cross = eight_sum(some ? mine.cross : 0.0);
-        if (lane == 0) {
-            const double ln2 = 0.693147180559945309417, lse = all_most * ln2 + log_of(total);
-            double loss = cross + q_sum * lse;
-            if (left > 0.0f) loss += (double)left * (log_of(left) - log_of(rest) - rest_most * ln2 + lse);
-            if (q_sum == 0.0 && left == 0.0f) loss = 0.0;
-            a.loss[row] = (float)(loss * (double)weight * a.loss_factor);
+        if (for_entries) {
+            if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&sums[rank], lane) = mine;
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        } else {
+            asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         }
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (for_entries) mine = sums[lane & 7];
+    }
+    if (for_entries) {
+        if ((lane & 7) >= ctas) mine = PartSums{};
+        const Factors k = factors_of(a, mine, rest, ref.exponent, q_sum, weight, row, a.loss && rank == 0);
+        if (lane == 0) factors = k;
     }
     if (!g) return;
-    const float f = weight * a.grad_factor;
-    const float k_top = mass / total * f;
-    // (a part with nothing but -inf: the share is 0, and NaN where the whole row has no other)
-    const float k_rest = rest_here == 0.0f ? 0.0f * k_top : (mass / total * exp2_fast((float)(ref.exponent - all_most)) - left / rest * exp2_fast((float)(ref.exponent - rest_most))) * f;
-    const bool whole = (reinterpret_cast<uintptr_t>(g) & 15u) == (reinterpret_cast<uintptr_t>(z) & 15u);
-    if (ref.careful) write_grad<T, true, false>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
-    else if (whole) write_grad<T, false, true>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
-    else write_grad<T, false, false>(cells, n, entry, base, a.vocab, g, ref, a.c1, k_rest);
+    __syncthreads();
+    const Factors k = factors;
+    if (!for_entries) {
+        const bool whole = (reinterpret_cast<uintptr_t>(g) & 15u) == (reinterpret_cast<uintptr_t>(z) & 15u);
+        if (ref.careful) write_grad<T, true, false>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
+        else if (whole) write_grad<T, false, true>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
+        else write_grad<T, false, false>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
+    }
+    __syncthreads();
     // the entries' own elements: the probabilities of a column's entries added in their order
-    for (int j = tid; j < a.top; j += threads) {
+    for (int j = tid; j < a.top; j += blockDim.x) {
         const int c = entry.col[j];
         if (c < 0) continue;
         float q = entry.prob[j];
@@ -449,7 +477,7 @@ __global__ void __launch_bounds__(kMostThreads) k_distill(const __grid_constant_
             for (int i = 0; i < a.top; ++i)
                 if (entry.col[i] == c || entry.col[i] == -3 - c) q += entry.prob[i];
         }
-        g[c] = from_f32<T>(exp2_fast((float)((double)entry.value[j] * (double)a.c1 - all_most)) * k_top - q * f);
+        g[c] = from_f32<T>(exp2_fast((float)((double)entry.value[j] * (double)a.c1 - k.all_at)) * k.top - q * (weight * a.grad_factor));
     }
 }
 
@@ -465,14 +493,14 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     const int granules = ((int)((bytes + 15) / 16 / ctas) + 2 + 3) & ~3;
     const size_t smem = (size_t)granules * 17 + (size_t)a.top * kEntryBytes;
     int threads = 32;
-    while (threads < kMostThreads && granules > threads * 12) threads *= 2;
+    while (threads < kMostThreads && granules > threads * 16) threads *= 2;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)ctas;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.blockDim = dim3((unsigned)threads + 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
