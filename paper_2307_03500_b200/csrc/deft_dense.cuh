@@ -45,8 +45,9 @@ struct DistillArgs {
     int64_t rows;
     int32_t vocab, top;
     int32_t id_bytes, teacher_type;
-    double inv_temp, loss_factor;        // 1 / T, T^2
-    float c1, grad_factor;               // log2(e) / T, scale * T
+    float it_hi, it_lo;                  // 1 / T in two pieces
+    float c1, by, by_lo;                 // log2(e) / T; that, as rounded, times ln 2 in two pieces
+    float loss_factor, grad_factor;      // T^2, scale * T
 };
 size_t layer_norm_grad_ws_bytes(int64_t rows, int64_t cols);
 deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cudaStream_t stream);

@@ -236,9 +236,13 @@ deft_status deft_distill(const void* logits_d, int32_t type, int64_t ld_logits, 
     a.top = (int32_t)top;
     a.id_bytes = id_bytes;
     a.teacher_type = teacher_type;
-    a.inv_temp = 1.0 / temperature;
-    a.loss_factor = temperature * temperature;
+    a.it_hi = (float)(1.0 / temperature);
+    a.it_lo = (float)(1.0 / temperature - (double)a.it_hi);
     a.c1 = (float)(1.442695040888963407360 / temperature);
+    const double by = (double)a.c1 * 0.693147180559945309417;
+    a.by = (float)by;
+    a.by_lo = (float)(by - (double)a.by);
+    a.loss_factor = (float)(temperature * temperature);
     a.grad_factor = (float)(scale * temperature);
     return launch_distill(a, type, static_cast<cudaStream_t>(stream));
 }

@@ -1,9 +1,11 @@
 // Distillation from a teacher's top logits: per row T^2 KL(teacher || student) and its gradient.
 //
-// A row of logits is read once.  A cluster of 1 to 8 CTAs shares it: each copies a part of its 16-byte granules into
-// shared memory.  The first warp, meanwhile, works out the teacher's probabilities and marks the entries' elements: what is
-// left is the rest of the vocabulary, whose sum must not come from a difference.  All warps sum the powers of the rest,
-// the CTAs exchange their sums, and the gradient is formed from shared memory and written.
+// A row of logits is read once.  A cluster of 1 to 8 CTAs shares it, each a part of its 16-byte granules in shared memory; a
+// thread works on the granules that it has copied.  While the part is on its way the threads work out the
+// teacher's probabilities, an entry each; then they take the entries' elements out of the part (-inf takes their place: what is
+// left is the rest of the vocabulary, whose sum must not come from a difference).  Every warp sums the powers of its
+// granules relative to a logit of its own, the last warp joins the sums, exchanges them with the other CTAs and has the loss and
+// the gradient's factors, with which the gradient is formed from shared memory and written; the entries' elements last.
 #include <cooperative_groups.h>
 
 #include "deft_dense.cuh"
@@ -13,7 +15,7 @@ namespace {
 
 constexpr int kMostCluster = 8;
 constexpr int kMostThreads = 512;         // that work on the row
-constexpr int kPartBytes = 51712;         // of a row, per CTA, where there are rows enough: four CTAs per SM
+constexpr int kPartBytes = 52224;         // of a row, per CTA: four CTAs per SM
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -51,28 +53,58 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
     return pair(exp2_fast(v.x), exp2_fast(v.y));
 }
 
-// The natural logarithm of a positive float to 2^-26 or so, whatever its size: the exponent's part in 64 bits.
-__device__ __forceinline__ double log_of(float x) {
-    if (!(x > 0.0f && x < INFINITY)) return (double)logf(x);
+// A sum of fp32 numbers and what its roundings have left out: the loss is what remains of terms that nearly cancel.
+struct Exact {
+    float hi, lo;
+    __device__ __forceinline__ void add(float x) {
+        const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
+        lo += __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b));
+        hi = s;
+    }
+    __device__ __forceinline__ void add(Exact x) {
+        add(x.hi);
+        lo += x.lo;
+    }
+    __device__ __forceinline__ void add_product(float a, float b) {
+        const float p = __fmul_rn(a, b);
+        add(p);
+        lo += __fmaf_rn(a, b, -p);
+    }
+};
+// d (hi + lo) + c; an infinite d stays what it is (the lower piece may be 0).
+__device__ __forceinline__ float scaled(float d, float hi, float lo, float c) {
+    const float y = __fmaf_rn(d, hi, c);
+    return isfinite(d) ? __fmaf_rn(d, lo, y) : y;
+}
+// The natural logarithm of a positive number: its exponent's part with ln 2 in two pieces, the first of which times an exponent is
+// exact (Cody and Waite), and the logarithm of the rest, which lies in [sqrt(1/2), sqrt(2)).
+__device__ __forceinline__ Exact log_of(float x) {
+    if (!(x > 0.0f && x < INFINITY)) return Exact{logf(x), 0.0f};
     int e = 0;
     if (x < 1.17549435e-38f) x *= 16777216.0f, e = -24;
-    const int bits = __float_as_int(x) - 0x3f3504f3;          // of sqrt(1/2): the rest lies in [sqrt(1/2), sqrt(2))
+    const int bits = __float_as_int(x) - 0x3f3504f3;          // of sqrt(1/2)
     e += bits >> 23;
-    return (double)e * 0.693147180559945309417 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3));
+    Exact y{(float)e * 0.693145751953125f, (float)e * 1.42860682030941723212e-6f};
+    y.add(logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3)));
+    return y;
 }
+__device__ __forceinline__ Exact shuffled(Exact x, int o) { return Exact{__shfl_xor_sync(0xffffffffu, x.hi, o), __shfl_xor_sync(0xffffffffu, x.lo, o)}; }
 
-// Powers of a part's logits: 2^(z c1 - from), or, where that could lose them, 2^((z - from) c1).
-struct Reference {
-    bool careful;
-    float from;
-    double exponent;                       // what the powers are relative to, in powers of two
+// Sums of powers 2^((z - near) c1) relative to a logit; near counts only where the sum is not 0.
+struct Powers {
+    float near, sum;
+};
+// What a warp has summed, and what the CTAs of a row tell each other: of the rest and of the entries the powers; over the
+// entries q (log q - (z - near) / T), and q.
+struct Sums {
+    Powers rest, entries;
+    Exact cross, q;
 };
 
-// What the CTAs of a row tell each other: two sums, the exponents they are relative to, and
-// sum over the part's entries of q (log q - z / T).
-struct PartSums {
-    double rest_at, entries_at, cross;
-    float rest, entries;
+// What the gradient of a row is formed with: an element's is A 2^((z - all) c1) - B 2^((z - rest) c1), an entry's own
+// A 2^((z - all) c1) - q f.
+struct Factors {
+    float all, rest, A, B;
 };
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -85,30 +117,35 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ double warp_sum(double v) {
+// The sum of what the lanes hold (over groups of kLanes), relative to the largest logit among them.
+template <int kLanes>
+__device__ __forceinline__ Powers joined(Powers p, float c1) {
+    float near = p.sum == 0.0f ? -INFINITY : p.near;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-// Over groups of eight lanes.
-template <typename F>
-__device__ __forceinline__ F eight_sum(F v) {
+    for (int o = kLanes / 2; o; o >>= 1) near = fmaxf(near, __shfl_xor_sync(0xffffffffu, near, o));
+    if (near == -INFINITY) near = 0.0f;
+    float sum = p.sum == 0.0f ? 0.0f : p.sum * exp2_fast((p.near - near) * c1);
 #pragma unroll
-    for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return Powers{near, sum};
 }
-__device__ __forceinline__ double eight_max(double v) {
+template <int kLanes>
+__device__ __forceinline__ Exact joined(Exact x) {
 #pragma unroll
-    for (int o = 4; o; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    for (int o = kLanes / 2; o; o >>= 1) x.add(shuffled(x, o));
+    return x;
 }
-__device__ __forceinline__ float warps_max(const float* slots, int warps) {
-    const int lane = threadIdx.x & 31;
-    return warp_max(lane < warps ? slots[lane] : -INFINITY);
-}
-__device__ __forceinline__ float warps_sum(const float* slots, int warps) {
-    const int lane = threadIdx.x & 31;
-    return warp_sum(lane < warps ? slots[lane] : 0.0f);
+// ... with the entries' terms, which change with what their logits are relative to: q (near - new near) / T.
+template <int kLanes>
+__device__ __forceinline__ Sums joined(const Sums& s, float c1, float by) {
+    Sums o;
+    o.rest = joined<kLanes>(s.rest, c1);
+    o.entries = joined<kLanes>(s.entries, c1);
+    Exact cross = s.cross;
+    if (s.q.hi != 0.0f && s.entries.near != o.entries.near) cross.add_product(-s.q.hi, (s.entries.near - o.entries.near) * by);
+    o.cross = joined<kLanes>(cross);
+    o.q = joined<kLanes>(s.q);
+    return o;
 }
 
 // Sixteen bytes of a row as pairs of fp32 numbers.
@@ -156,37 +193,67 @@ struct Granule<__half> {
     }
 };
 
-__device__ __forceinline__ float teacher_at(const DistillArgs& a, int64_t row, int j) {
-    const int64_t at = row * a.ld_teacher + j;
-    if (a.teacher_type == DEFT_F32) return static_cast<const float*>(a.teacher)[at];
-    if (a.teacher_type == DEFT_BF16) return to_f32(static_cast<const __nv_bfloat16*>(a.teacher)[at]);
-    return to_f32(static_cast<const __half*>(a.teacher)[at]);
+// An entry as it lies in memory: nothing waits for its loads before it is looked at.
+struct RawEntry {
+    uint32_t id, id_high, t;
+};
+__device__ __forceinline__ RawEntry entry_at(const DistillArgs& a, int64_t row, int j) {
+    RawEntry e{0, 0, 0};
+    const int64_t at = row * a.ld_teacher + j, id = row * a.ld_ids + j;
+    if (a.id_bytes == 8) {
+        const uint2 both = static_cast<const uint2*>(a.ids)[id];
+        e.id = both.x;
+        e.id_high = both.y;
+    } else {
+        e.id = static_cast<const uint32_t*>(a.ids)[id];
+    }
+    if (a.teacher_type == DEFT_F32) e.t = static_cast<const uint32_t*>(a.teacher)[at];
+    else e.t = static_cast<const uint16_t*>(a.teacher)[at];
+    return e;
 }
-__device__ __forceinline__ int id_at(const DistillArgs& a, int64_t row, int j) {
-    const int64_t at = row * a.ld_ids + j;
-    const int64_t id = a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
-    return id >= 0 && id < a.vocab ? (int)id : -1;
+// The entry's column, or -1.
+__device__ __forceinline__ int column_of(const DistillArgs& a, const RawEntry& e) { return e.id < (uint32_t)a.vocab && e.id_high == 0 ? (int)e.id : -1; }
+__device__ __forceinline__ float value_of(const DistillArgs& a, uint32_t t) {
+    if (a.teacher_type == DEFT_F32) return __uint_as_float(t);
+    return a.teacher_type == DEFT_BF16 ? to_f32(__ushort_as_bfloat16((unsigned short)t)) : to_f32(__ushort_as_half((unsigned short)t));
 }
 
-// The teacher's entries of a row in shared memory, and a byte for each granule of the part: which of its elements are entries.
+// A row's entries in shared memory.
 struct Entries {
     int* col;                              // column; -1: none; -2: another CTA's; -3 - column: not the first of its column
-    float *value, *prob;                   // t, then the student's logit; q
-    unsigned* marks;
+    float *log_q, *prob, *own;             // own: the student's logit
     __device__ __forceinline__ Entries(char* at, int top) : col(reinterpret_cast<int*>(at)) {
-        value = reinterpret_cast<float*>(col + top);
-        prob = value + top;
-        marks = reinterpret_cast<unsigned*>(prob + top);
+        log_q = reinterpret_cast<float*>(col + top);
+        prob = log_q + top;
+        own = prob + top;
     }
-    __device__ __forceinline__ unsigned marked(int granule) const { return reinterpret_cast<const unsigned char*>(marks)[granule]; }
 };
-constexpr size_t kEntryBytes = 12;
+constexpr size_t kEntryBytes = 16;
 
 // What stands for an element without a share.
 template <typename T> __device__ __forceinline__ T lowest();
 template <> __device__ __forceinline__ float lowest<float>() { return __int_as_float(0xff800000); }
 template <> __device__ __forceinline__ __nv_bfloat16 lowest<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
 template <> __device__ __forceinline__ __half lowest<__half>() { return __ushort_as_half(0xfc00); }
+
+// Takes an element out of a part and returns what was there: -inf for all but the first that asks.
+__device__ __forceinline__ float take(float* p) { return __uint_as_float(atomicExch(reinterpret_cast<unsigned*>(p), 0xff800000u)); }
+template <typename T>
+__device__ __forceinline__ float take(T* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    unsigned* word = reinterpret_cast<unsigned*>(at & ~(uintptr_t)3);
+    const int up = (at & 2) ? 16 : 0;
+    const T low = lowest<T>();
+    const unsigned mark = *reinterpret_cast<const unsigned short*>(&low);
+    unsigned was = *reinterpret_cast<volatile unsigned*>(word);
+    while (true) {
+        const unsigned seen = atomicCAS(word, was, (was & ~(0xffffu << up)) | (mark << up));
+        if (seen == was) break;
+        was = seen;
+    }
+    const unsigned short old = (unsigned short)(was >> up);
+    return to_f32(*reinterpret_cast<const T*>(&old));
+}
 
 // The largest element of a granule.
 template <typename T>
@@ -203,313 +270,334 @@ template <typename T, bool kCareful>
 __device__ __forceinline__ uint64_t powers(uint64_t z, uint64_t c, uint64_t minus_from) {
     return exp2_pair(kCareful ? mul2(add2(z, minus_from), c) : fma2(z, c, minus_from));
 }
-// A granule of this thread without its entries.
-template <typename T>
-__device__ __forceinline__ Granule<T> rest_of(const Granule<T>* cells, int i, const Entries& entry) {
-    Granule<T> g = cells[i];
-    const unsigned marked = entry.marked(i);
-    if (marked) {
-#pragma unroll
-        for (int e = 0; e < Granule<T>::kPer; ++e)
-            if (marked >> e & 1u) reinterpret_cast<T*>(&g.raw)[e] = lowest<T>();
-    }
-    return g;
-}
 // The sum of the powers of this thread's granules.
 template <typename T, bool kCareful>
-__device__ __forceinline__ float sum_powers(const Granule<T>* cells, int n, int threads, const Entries& entry, const Reference& ref, float c1) {
-    const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from);
+__device__ __forceinline__ float sum_powers(const Granule<T>* cells, int n, int threads, float from1, float c1) {
+    const uint64_t c = pair(c1, c1), from = pair(-from1, -from1);
     uint64_t s[2] = {0, 0};
     for (int i = threadIdx.x; i < n; i += threads) {
-        const Granule<T> g = rest_of(cells, i, entry);
+        const Granule<T> g = cells[i];
 #pragma unroll
         for (int p = 0; p < Granule<T>::kPairs; ++p) s[p & 1] = add2(s[p & 1], powers<T, kCareful>(g.get(p), c, from));
     }
     const float2 v = unpair(add2(s[0], s[1]));
     return v.x + v.y;
 }
-// The gradient of this thread's granules, as if there were no entries among them.  kWhole: the gradient's granules lie like the logits'.
-template <typename T, bool kCareful, bool kWhole>
-__device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, int threads, int base, int vocab, T* g, const Reference& ref, float c1, float k1) {
+// The first elements of a granule (col: the first one's column) that are the row's.
+template <typename T>
+__device__ __forceinline__ void put_some(const Granule<T>& o, int col, int vocab, T* g) {
+    for (int e = 0; e < Granule<T>::kPer; ++e)
+        if (col + e >= 0 && col + e < vocab) g[col + e] = reinterpret_cast<const T*>(&o.raw)[e];
+}
+// The gradient of this thread's granules, the entries' elements zero.  whole: the granules of the gradient lie like the logits';
+// inner: granules lo .. hi are the row's in full.
+template <typename T, bool kCareful>
+__device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, int base, int lo, int hi, int threads, int vocab, T* g, float from1, float c1, float k1) {
     constexpr int kPer = Granule<T>::kPer;
-    const uint64_t c = pair(c1, c1), from = pair(-ref.from, -ref.from), k = pair(k1, k1);
+    const uint64_t c = pair(c1, c1), from = pair(-from1, -from1), k = pair(k1, k1);
     for (int i = threadIdx.x; i < n; i += threads) {
         const Granule<T> in = cells[i];
         Granule<T> o;
 #pragma unroll
         for (int p = 0; p < Granule<T>::kPairs; ++p) o.set(p, mul2(powers<T, kCareful>(in.get(p), c, from), k));
-        const int first = base + i * kPer;
-        if (kWhole && first >= 0 && first + kPer <= vocab) {
-            *reinterpret_cast<uint4*>(g + first) = o.raw;
-        } else {
-            for (int e = 0; e < kPer; ++e)
-                if (first + e >= 0 && first + e < vocab) g[first + e] = reinterpret_cast<const T*>(&o.raw)[e];
-        }
+        if (i >= lo && i < hi) *reinterpret_cast<uint4*>(g + base + i * kPer) = o.raw;
+        else put_some(o, base + i * kPer, vocab, g);
     }
 }
 
-// What the first warp works out for all: factors of the gradient, the exponent that the row's sum is relative to.
-struct Factors {
-    double all_at;
-    float rest, top;
+// Barriers of a CTA: among the warps that work on the row, between them and the last warp.
+enum { kLanded = 1, kTaken, kSummed, kFactors, kWritten };
+template <int kId>
+__device__ __forceinline__ void bar_sync(int threads) {
+    __syncwarp();
+    asm volatile("bar.sync %0, %1;" ::"n"(kId), "r"(threads) : "memory");
+}
+template <int kId>
+__device__ __forceinline__ void bar_arrive(int threads) {
+    __syncwarp();
+    asm volatile("bar.arrive %0, %1;" ::"n"(kId), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_arrive_release() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// How a call is split: CTAs of a cluster, granules of a part; threads that work on the row.
+struct DistillShape {
+    int ctas, granules, threads;
+    size_t smem;
 };
 
-// The loss of a row and the factors of its gradient from the CTAs' sums.  One warp; a lane for each CTA, four times over.
-__device__ __forceinline__ Factors factors_of(const DistillArgs& a, const PartSums& o, float rest_here, double here_at, double q_sum, float weight, int64_t row, bool write_loss) {
-    const double none = -(double)INFINITY, rest_at = !(o.rest == 0.0f) ? o.rest_at : none, entries_at = !(o.entries == 0.0f) ? o.entries_at : none;
-    const double rest_most = eight_max(rest_at), all_most = fmax(rest_most, eight_max(entries_at));
-    const float total = eight_sum((rest_at == none ? 0.0f : o.rest * exp2_fast((float)(rest_at - all_most))) +
-                                  (entries_at == none ? 0.0f : o.entries * exp2_fast((float)(entries_at - all_most))));
-    const float all_rest = eight_sum(rest_at == none ? 0.0f : o.rest * exp2_fast((float)(rest_at - rest_most)));
-    // the teacher's probability outside its entries; none where there is no other logit
-    const float left = a.teacher_lse && !(all_rest == 0.0f) ? (float)fmax(0.0, 1.0 - q_sum) : 0.0f;
-    const float mass = (float)(q_sum + (double)left);
-    const float f = weight * a.grad_factor, top = mass / total * f;
-    // (a part with nothing but -inf: the share is 0, and NaN where the whole row has no other)
-    const float rest = rest_here == 0.0f ? 0.0f * top : (mass / total * exp2_fast((float)(here_at - all_most)) - left / all_rest * exp2_fast((float)(here_at - rest_most))) * f;
-    if (write_loss) {
-        const double cross = eight_sum(o.cross);
-        if ((threadIdx.x & 31) == 0) {
-            const double ln2 = 0.693147180559945309417, lse = all_most * ln2 + log_of(total);
-            double loss = cross + q_sum * lse;
-            if (left > 0.0f) loss += (double)left * (log_of(left) - log_of(all_rest) - rest_most * ln2 + lse);
-            if (q_sum == 0.0 && left == 0.0f) loss = 0.0;
-            a.loss[row] = (float)(loss * (double)weight * a.loss_factor);
-        }
-    }
-    return Factors{all_most, rest, top};
-}
-
-// The last warp of a CTA works on the entries, the others on the part of the row.
-template <typename T>
-__global__ void __launch_bounds__(kMostThreads + 32, 1) k_distill(const __grid_constant__ DistillArgs a, const int granules_most, const int ctas) {
+// kMost: threads that work on the row, at most; four CTAs of 256 fit an SM.
+template <typename T, int kMost>
+__global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(const __grid_constant__ DistillArgs a, const __grid_constant__ DistillShape shape) {
     constexpr int kPer = Granule<T>::kPer;
     extern __shared__ __align__(16) char smem[];
-    T* part = reinterpret_cast<T*>(smem);                                        // this CTA's granules
-    Granule<T>* cells = reinterpret_cast<Granule<T>*>(smem);
-    const Entries entry(smem + (size_t)granules_most * 16, a.top);
-    __shared__ float slots[2][kMostThreads / 32];
-    __shared__ PartSums sums[kMostCluster];
+    Granule<T>* const cells = reinterpret_cast<Granule<T>*>(smem);
+    __shared__ Sums warp_sums[kMost / 32], cta_sums[kMostCluster];
     __shared__ Factors factors;
-    __shared__ int twice;
-    const int tid = threadIdx.x, threads = (int)blockDim.x - 32, warps = threads >> 5, warp = tid >> 5, lane = tid & 31;
-    const bool for_entries = warp == warps;
+    __shared__ int twice;                  // the last row in which an entry found nothing in its place: another one's column, or -inf
+    const int ctas = shape.ctas, threads = shape.threads, warps = threads >> 5, all_threads = threads + 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int rank = 0;
+    int64_t row = blockIdx.x;
     if (ctas > 1) {
+        uint32_t cluster;
         asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // (waited for before others' shared memory is written)
+        asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(cluster));
+        row = cluster;
+        cluster_arrive();                  // (waited for before others' shared memory is written)
     }
-    const int64_t row = blockIdx.x / (unsigned)ctas;
-    const T* z = static_cast<const T*>(a.logits) + row * a.ld;
-    T* g = a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad : nullptr;
-    // the row's granules, the first of which may begin before it; this CTA's share and its columns
-    const int shift = (int)(reinterpret_cast<uintptr_t>(z) & 15u) / (int)sizeof(T);
-    const int granules = (a.vocab + shift + kPer - 1) / kPer;
-    const int g0 = (int)((int64_t)granules * rank / ctas), g1 = (int)((int64_t)granules * (rank + 1) / ctas), n = g1 - g0;
-    const int c0 = max(0, g0 * kPer - shift), c1 = min(a.vocab, g1 * kPer - shift);
-    const int base = g0 * kPer - shift;                                          // column of part[0]
-
+    T* const g = a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad : nullptr;
     const float weight = a.weight ? a.weight[row] : 1.0f;
-    if (weight == 0.0f) {                  // nothing is read of a row that does not count (the same for the whole cluster)
-        if (g) for (int c = c0 + tid; c < c1; c += blockDim.x) g[c] = from_f32<T>(0.0f);
-        if (a.loss && rank == 0 && tid == 0) a.loss[row] = 0.0f;
-        if (ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+    if (warp == warps) {                   // ---- the last warp ----
+        if (weight == 0.0f) {
+            if (a.loss && rank == 0 && lane == 0) a.loss[row] = 0.0f;
+            if (ctas > 1) cluster_wait();
+            return;
+        }
+        bar_sync<kSummed>(all_threads);
+        Sums s{};
+        if (lane < warps) s = warp_sums[lane];
+        s = joined<32>(s, a.c1, a.by);
+        if (ctas > 1) {
+            cluster_wait();                // all CTAs run: their shared memory may be written
+            if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&cta_sums[rank], lane) = s;
+            cluster_arrive_release();
+            cluster_wait();
+            s = Sums{};
+            if ((lane & 7) < ctas) s = cta_sums[lane & 7];
+            s = joined<8>(s, a.c1, a.by);
+        }
+        const float all = s.rest.sum == 0.0f ? s.entries.near : (s.entries.sum == 0.0f ? s.rest.near : fmaxf(s.rest.near, s.entries.near));
+        const float total = (s.rest.sum == 0.0f ? 0.0f : s.rest.sum * exp2_fast((s.rest.near - all) * a.c1)) +
+                            (s.entries.sum == 0.0f ? 0.0f : s.entries.sum * exp2_fast((s.entries.near - all) * a.c1));
+        // the teacher's probability outside its entries; none where there is no other logit
+        const float left = a.teacher_lse && !(s.rest.sum == 0.0f) ? fmaxf(0.0f, (1.0f - s.q.hi) - s.q.lo) : 0.0f;
+        if (g) {
+            const float f = weight * a.grad_factor;
+            if (lane == 0) factors = Factors{all, s.rest.near, (s.q.hi + (s.q.lo + left)) / total * f, left > 0.0f ? left / s.rest.sum * f : 0.0f};
+            bar_arrive<kFactors>(all_threads);
+        }
+        if (a.loss && rank == 0 && lane == 0) {
+            const Exact log_total = log_of(total);
+            Exact loss = s.cross;
+            if (s.q.hi != 0.0f) {
+                loss.add_product(s.q.hi, (all - s.entries.near) * a.by);
+                loss.add_product(s.q.hi, log_total.hi);
+                loss.lo += s.q.hi * log_total.lo;
+            }
+            if (left > 0.0f) {
+                const Exact log_left = log_of(left), log_rest = log_of(s.rest.sum);
+                Exact d = log_left;
+                d.add(Exact{-log_rest.hi, -log_rest.lo});
+                d.add((all - s.rest.near) * a.by);
+                d.add(log_total);
+                loss.add_product(left, d.hi);
+                loss.lo += left * d.lo;
+            }
+            const float value = loss.hi + loss.lo;
+            // (where a term is infinite, what its roundings have left out is no number)
+            a.loss[row] = (isfinite(loss.hi) ? value : loss.hi) * weight * a.loss_factor;
+        }
         return;
     }
-    double norm = 0.0, q_sum = 0.0, cross = 0.0;   // of the last warp: log q_j = t_j / T - norm; sums of q and, over the part's entries, q log q
-    if (for_entries) {
-        // (The loss is what is left of sums that nearly cancel: its terms are added in 64 bits.)
-        int id[2] = {-1, -1};
-        float t[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < 2; ++i)        // the first entries' loads are under way together
-            if (lane + 32 * i < a.top) {
-                id[i] = id_at(a, row, lane + 32 * i);
-                t[i] = teacher_at(a, row, lane + 32 * i);
+
+    // this CTA's granules of the row, the first of which may begin before it
+    const T* const z = static_cast<const T*>(a.logits) + row * a.ld;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(z) & 15u) / (int)sizeof(T);
+    const int first = rank * shape.granules, base = first * kPer - shift;        // column of the first element
+    const int n = max(0, min(shape.granules, (a.vocab + shift + kPer - 1) / kPer - first));
+    const bool whole = ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
+    const int lo = whole ? (base < 0 ? 1 : 0) : n, hi = whole ? min(n, (a.vocab - base) / kPer) : n;   // granules written in one piece
+    if (weight == 0.0f) {                  // nothing is read of a row that does not count
+        Granule<T> zero;
+        zero.raw = make_uint4(0, 0, 0, 0);
+        if (g)
+            for (int i = tid; i < n; i += threads) {
+                if (i >= lo && i < hi) *reinterpret_cast<uint4*>(g + base + i * kPer) = zero.raw;
+                else put_some(zero, base + i * kPer, a.vocab, g);
             }
-        if (a.teacher_lse) norm = (double)a.teacher_lse[row];
-        for (int i = lane; i < (n + 3) / 4; i += 32) entry.marks[i] = 0;
-        if (lane == 0) twice = 0;
-        float most = -INFINITY;
-        auto keep = [&](int j, int col, float value) {
-            entry.col[j] = col;
-            entry.value[j] = value;
-            if (col >= 0) most = fmaxf(most, value);
-        };
-        if (lane < a.top) keep(lane, id[0], t[0]);
-        if (lane + 32 < a.top) keep(lane + 32, id[1], t[1]);
-        for (int j = lane + 64; j < a.top; j += 32) keep(j, id_at(a, row, j), teacher_at(a, row, j));
-        if (!a.teacher_lse) {
-            most = warp_max(most);
-            float sum = 0.0f;
-            for (int j = lane; j < a.top; j += 32)
-                if (entry.col[j] >= 0 && most != -INFINITY) sum += expf((float)(((double)entry.value[j] - (double)most) * a.inv_temp));
-            norm = most == -INFINITY ? 0.0 : (double)most * a.inv_temp + log_of(warp_sum(sum));
-        }
-        __syncwarp();
-        for (int j = lane; j < a.top; j += 32) {
-            const int col = entry.col[j];
-            const double log_q = (double)entry.value[j] * a.inv_temp - norm;
-            const float q = col >= 0 ? expf((float)log_q) : 0.0f;
-            entry.prob[j] = q;
-            q_sum += (double)q;
-            if (col < 0) continue;
-            if (col < c0 || col >= c1) {
-                entry.col[j] = -2;
-                continue;
-            }
-            if (q != 0.0f) cross += (double)q * log_q;
-            const int cell = (col - base) / kPer, bit = (cell & 3) * 8 + (col - base) % kPer;
-            if (atomicOr(entry.marks + (cell >> 2), 1u << bit) >> bit & 1u) {
-                entry.col[j] = -3 - col;
-                twice = 1;
-            }
-        }
-        q_sum = warp_sum(q_sum);
-    } else {
-        // every thread copies the granules that it works on
-        const uint4* from = reinterpret_cast<const uint4*>(z - shift) + g0;
-        for (int i = tid; i < n; i += threads)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)i * 16u), "l"(from + i) : "memory");
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        // what the first and last granule hold beside the row
-        if (n > 0 && tid == 0)
-            for (int c = base; c < 0; ++c) part[c - base] = lowest<T>();
-        if (n > 0 && tid == (n - 1) % threads)
-            for (int c = max(c1, base); c < base + n * kPer; ++c) part[c - base] = lowest<T>();
-        // what the powers are relative to: the largest of a granule of every thread, which is seldom far from the largest of all
-        const float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
-        if (lane == 0) slots[0][warp] = most;
+        if (ctas > 1) cluster_wait();
+        return;
     }
-    __syncthreads();
-    Reference ref{false, 0.0f, 0.0};
+    // an entry for each thread: its load goes ahead of the copies
+    const Entries entry(smem + (size_t)shape.granules * 16, a.top);
+    const bool has_entries = warp * 32 < a.top;
+    if (tid == 0) twice = -1;
+    RawEntry raw{0, 0, 0};
+    float norm = 0.0f;
+    if (tid < a.top) raw = entry_at(a, row, tid);
+    if (has_entries && a.teacher_lse) norm = a.teacher_lse[row];
     {
-        const float most = warps_max(slots[0], warps);
-        ref.from = most == -INFINITY ? 0.0f : most * a.c1;
-        ref.exponent = (double)ref.from;
+        const T* from = z + base + tid * kPer;
+        uint32_t to = (uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)tid * 16u;
+        for (int i = tid; i < n; i += threads, from += threads * kPer, to += (uint32_t)threads * 16u)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (for_entries) {                     // the entries' logits
+    // the teacher, while the copies are under way: log q = (t - near) / T - norm
+    Exact q_sum{};
+    if (has_entries) {
+        float near = 0.0f;
+        if (!a.teacher_lse) {              // every warp goes through all entries
+            float most = -INFINITY, sum = 0.0f;
+            for (int j = lane; j < a.top; j += 32) {
+                const RawEntry e = entry_at(a, row, j);
+                if (column_of(a, e) >= 0) most = fmaxf(most, value_of(a, e.t));
+            }
+            most = warp_max(most);
+            if (most != -INFINITY) {
+                near = most;
+                for (int j = lane; j < a.top; j += 32) {
+                    const RawEntry e = entry_at(a, row, j);
+                    const float d = value_of(a, e.t) - near;
+                    if (column_of(a, e) >= 0) sum += expf(scaled(d, a.it_hi, a.it_lo, 0.0f));
+                }
+                const Exact log_sum = log_of(warp_sum(sum));
+                norm = log_sum.hi + log_sum.lo;
+            }
+        }
+        for (int j = tid; j < a.top; j += threads) {
+            if (j >= threads) raw = entry_at(a, row, j);
+            const int col = column_of(a, raw);
+            const bool valid = col >= 0;
+            const float d = value_of(a, raw.t) - near;
+            const float log_q = scaled(d, a.it_hi, a.it_lo, -norm), q = valid ? expf(log_q) : 0.0f;
+            const bool here = valid && col >= base && col < base + n * kPer;
+            entry.col[j] = valid && !here ? -2 : col;
+            entry.log_q[j] = log_q;
+            entry.prob[j] = q;
+            if (here) q_sum.add(q);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    T* const e = reinterpret_cast<T*>(smem) - base;
+    if (tid == 0)                          // what the first and last granule hold beside the row
+        for (int c = base; c < 0; ++c) e[c] = lowest<T>();
+    bar_sync<kLanded>(threads);
+    for (int c = max(a.vocab, base) + tid; c < base + n * kPer; c += threads) e[c] = lowest<T>();
+    Sums s{};
+    if (has_entries) {
         float most = -INFINITY;
-        for (int j = lane; j < a.top; j += 32) {
+        for (int j = tid; j < a.top; j += threads) {
             const int col = entry.col[j];
-            if (col == -1 || col == -2) continue;
-            const float own = to_f32(part[(col < 0 ? -3 - col : col) - base]);
-            entry.value[j] = own;
-            if (entry.prob[j] != 0.0f) cross -= (double)entry.prob[j] * ((double)own * ((double)a.c1 * 0.693147180559945309417));
-            if (col >= 0) most = fmaxf(most, own);
+            if (col < 0) continue;
+            float own = take(e + col);
+            if (own == -INFINITY) {        // another entry of this column was first, or the logit is -inf
+                own = to_f32(z[col]);
+                if (own != -INFINITY) entry.col[j] = -3 - col;
+                twice = (int)row;
+            } else {
+                most = fmaxf(most, own);
+            }
+            entry.own[j] = own;
         }
         most = warp_max(most);
-        const float near = most == -INFINITY ? 0.0f : most;
-        float entries = 0.0f;
-        for (int j = lane; j < a.top; j += 32)
-            if (entry.col[j] >= 0) entries += exp2_fast((entry.value[j] - near) * a.c1);
-        entries = warp_sum(entries);
-        cross = warp_sum(cross);
-        if (lane == 0) sums[rank] = PartSums{0.0, (double)near * (double)a.c1, cross, 0.0f, entries};
-        __syncwarp();
-    } else {
-        const float rest = warp_sum(sum_powers<T, false>(cells, n, threads, entry, ref, a.c1));
-        if (lane == 0) slots[1][warp] = rest;
-    }
-    __syncthreads();
-    float rest = warps_sum(slots[1], warps);
-    // the sample is too far off (or something is no number).  Powers and factors below 2^-126 are 0: within these bounds no
-    // probability above 2^-96 is lost
-    if (!(rest > 9.5367431640625e-07f && rest < 1073741824.0f)) {             // 2^-20, 2^30
-        if (!for_entries) {
-            float most = -INFINITY;
-            for (int i = tid; i < n; i += threads) most = fmaxf(most, most_of<T>(rest_of(cells, i, entry)));
-            most = warp_max(most);
-            if (lane == 0) slots[0][warp] = most;
+        s.entries.near = most == -INFINITY ? 0.0f : most;
+        for (int j = tid; j < a.top; j += threads) {
+            const int col = entry.col[j];
+            if (col == -1 || col == -2) continue;
+            const float own = entry.own[j], q = entry.prob[j], d = own - s.entries.near;
+            if (q != 0.0f) s.cross.add_product(q, scaled(-d, a.by, a.by_lo, entry.log_q[j]));
+            if (col >= 0) s.entries.sum += exp2_fast(d * a.c1);
         }
-        __syncthreads();
-        const float most = warps_max(slots[0], warps);
-        ref.careful = true;
-        ref.from = most == -INFINITY ? 0.0f : most;
-        ref.exponent = (double)ref.from * (double)a.c1;
-        if (!for_entries) {
-            rest = warp_sum(sum_powers<T, true>(cells, n, threads, entry, ref, a.c1));
-            if (lane == 0) slots[1][warp] = rest;
-        }
-        __syncthreads();
-        rest = warps_sum(slots[1], warps);
     }
-    PartSums mine{};
-    if (for_entries) {
-        mine = sums[rank];
-        mine.rest = rest;
-        mine.rest_at = ref.exponent;
-        __syncwarp();
+    bar_sync<kTaken>(threads);
+    // what the powers are relative to: the largest of a granule of every lane, which is seldom far from the largest of all
+    float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
+    bool careful = false;
+    s.rest.near = most == -INFINITY ? 0.0f : most;
+    float from = s.rest.near * a.c1;
+    // (from is rounded: what the powers are relative to instead of near)
+    float off = exp2_fast(__fmaf_rn(-s.rest.near, a.c1, from));
+    float rest = warp_sum(sum_powers<T, false>(cells, n, threads, from, a.c1));
+    // the sample is too far off (or something is no number).  Powers and factors below 2^-126 are 0: within these bounds
+    // no probability above 2^-96 is lost
+    if (!(rest > 9.5367431640625e-07f && rest < 1073741824.0f)) {                // 2^-20, 2^30
+        most = -INFINITY;
+        for (int c = tid; c < n; c += threads) most = fmaxf(most, most_of<T>(cells[c]));
+        most = warp_max(most);
+        careful = true;
+        s.rest.near = from = most == -INFINITY ? 0.0f : most;
+        off = 1.0f;
+        rest = warp_sum(sum_powers<T, true>(cells, n, threads, from, a.c1));
     }
+    s.rest.sum = rest * off;
+    if (has_entries) {
+        s.entries.sum = warp_sum(s.entries.sum);
+        s.cross = joined<32>(s.cross);
+        s.q = joined<32>(q_sum);
+    }
+    if (lane == 0) warp_sums[warp] = s;
+    bar_arrive<kSummed>(all_threads);
     if (ctas > 1) {
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all CTAs run: their shared memory may be written
-        if (for_entries) {
-            if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&sums[rank], lane) = mine;
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        } else {
-            asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        cluster_wait();
+        cluster_arrive();
+    }
+    if (g) {
+        bar_sync<kFactors>(all_threads);
+        const Factors f = factors;
+        // (nothing but -inf: the share is 0, and NaN where the whole row has no other)
+        const float k = rest == 0.0f ? 0.0f * f.A : (f.A * exp2_fast((s.rest.near - f.all) * a.c1) - f.B * exp2_fast((s.rest.near - f.rest) * a.c1)) * off;
+        if (careful) write_grad<T, true>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
+        else write_grad<T, false>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
+        bar_sync<kWritten>(threads);
+        // the entries' own elements: the probabilities of a column's entries added in their order
+        for (int j = tid; j < a.top; j += threads) {
+            const int c = entry.col[j];
+            if (c < 0) continue;
+            float q = entry.prob[j];
+            if (twice == (int)row) {
+                q = 0.0f;
+                for (int m = 0; m < a.top; ++m)
+                    if (entry.col[m] == c || entry.col[m] == -3 - c) q += entry.prob[m];
+            }
+            g[c] = from_f32<T>(exp2_fast((entry.own[j] - f.all) * a.c1) * f.A - q * (weight * a.grad_factor));
         }
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (for_entries) mine = sums[lane & 7];
     }
-    if (for_entries) {
-        if ((lane & 7) >= ctas) mine = PartSums{};
-        const Factors k = factors_of(a, mine, rest, ref.exponent, q_sum, weight, row, a.loss && rank == 0);
-        if (lane == 0) factors = k;
-    }
-    if (!g) return;
-    __syncthreads();
-    const Factors k = factors;
-    if (!for_entries) {
-        const bool whole = (reinterpret_cast<uintptr_t>(g) & 15u) == (reinterpret_cast<uintptr_t>(z) & 15u);
-        if (ref.careful) write_grad<T, true, false>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
-        else if (whole) write_grad<T, false, true>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
-        else write_grad<T, false, false>(cells, n, threads, base, a.vocab, g, ref, a.c1, k.rest);
-    }
-    __syncthreads();
-    // the entries' own elements: the probabilities of a column's entries added in their order
-    for (int j = tid; j < a.top; j += blockDim.x) {
-        const int c = entry.col[j];
-        if (c < 0) continue;
-        float q = entry.prob[j];
-        if (twice) {
-            q = 0.0f;
-            for (int i = 0; i < a.top; ++i)
-                if (entry.col[i] == c || entry.col[i] == -3 - c) q += entry.prob[i];
-        }
-        g[c] = from_f32<T>(exp2_fast((float)((double)entry.value[j] * (double)a.c1 - k.all_at)) * k.top - q * (weight * a.grad_factor));
-    }
+    if (ctas > 1) cluster_wait();
 }
 
 }  // namespace
 
 deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) {
     const int64_t elem = (int64_t)type_bytes(type), bytes = a.vocab * elem + 16;
-    int ctas = 1;
-    while (ctas < kMostCluster && bytes / ctas > kPartBytes) ctas *= 2;
-    while (ctas < kMostCluster && a.rows * ctas < 2 * 148 && bytes / ctas > 8 * 1024) ctas *= 2;
-    const int64_t blocks = a.rows * ctas;
-    if (blocks > 0x7fffffffLL) return DEFT_ERR_TOO_LARGE;
-    const int granules = ((int)((bytes + 15) / 16 / ctas) + 2 + 3) & ~3;
-    const size_t smem = (size_t)granules * 17 + (size_t)a.top * kEntryBytes;
-    int threads = 32;
-    while (threads < kMostThreads && granules > threads * 16) threads *= 2;
+    int64_t ctas = (bytes + kPartBytes - 1) / kPartBytes;
+    while (ctas < kMostCluster && a.rows * ctas < 2 * 148 && bytes / ctas > 8 * 1024) ctas *= 2;      // few rows
+    if (ctas > kMostCluster) ctas = kMostCluster;
+    if (a.rows * ctas > 0x7fffffffLL) return DEFT_ERR_TOO_LARGE;
+    DistillShape s{};
+    s.ctas = (int)ctas;
+    s.granules = (int)(((bytes + 15) / 16 + ctas - 1) / ctas);
+    s.threads = 32;
+    while (s.threads < kMostThreads && s.granules > s.threads * 16) s.threads *= 2;
+    s.smem = (size_t)s.granules * 16 + (size_t)a.top * kEntryBytes;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)ctas;
+    attr.val.clusterDim.x = (unsigned)s.ctas;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3((unsigned)threads + 32);
-    cfg.dynamicSmemBytes = smem;
+    cfg.gridDim = dim3((unsigned)(a.rows * ctas));
+    cfg.blockDim = dim3((unsigned)s.threads + 32);
+    cfg.dynamicSmemBytes = s.smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
-    cfg.numAttrs = ctas > 1 ? 1 : 0;
+    cfg.numAttrs = s.ctas > 1 ? 1 : 0;
     return with_type(type, [&](auto t) -> deft_status {
         using T = decltype(t);
-        auto kernel = k_distill<T>;
-        if (smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, granules, ctas));
+        auto kernel = s.threads > 256 ? k_distill<T, 512> : k_distill<T, 256>;
+        if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+        DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, s));
         return DEFT_OK;
     });
 }
