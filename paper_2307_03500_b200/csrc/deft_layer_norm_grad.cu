@@ -10,86 +10,137 @@ namespace {
 
 constexpr int kPartials = 2 * 148;   // CTAs that leave partial sums at most; a constant: a call's bits do not depend on the device
 
-template <bool kAdd, typename TD, typename TX, bool kAligned, int kGroups>
-__global__ void __launch_bounds__(kTeamMost) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
-    extern __shared__ __align__(16) float params[];      // gamma; at the end the CTA's sums for gamma and beta
+template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads>
+__global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
+    extern __shared__ __align__(16) char smem[];         // gamma and room for a second vector (at the end the CTA's sums), the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
-    using Group = RowGroup<kAligned>;
+    using Group = RowGroup<kFeed>;
+    using RawX = Raw8<TX, Group::template align<TX>()>;
+    using RawD = Raw8<TD, Group::template align<TD>()>;
+    constexpr int kRunsX = kGroup * (int)sizeof(TX) / 16, kRunsD = kGroup * (int)sizeof(TD) / 16;
+    constexpr int kAtX = kGroups * kRunsD, kAtAdd = kAtX + kGroups * kRunsX, kAll = kAtAdd + (kAdd ? kGroups * kRunsX : 0);
     Team team(shape, slots);
     const int places = shape.places;
-    const TD* dy = static_cast<const TD*>(a.dy);
-    const TX *x = static_cast<const TX*>(a.x), *add = static_cast<const TX*>(a.add);
+    float *params = reinterpret_cast<float*>(smem), *beta = params + places * kGroup;
+    Ring<kThreads, kAll> ring(smem + 2 * sizeof(float) * (size_t)(places * kGroup), shape.stages);
     const uint32_t rows = (uint32_t)a.rows;
-    Raw8<TX, Group::template align<TX>()> next_x[kGroups], next_add[kGroups];
-    Raw8<TD, Group::template align<TD>()> next_dy[kGroups];
-    float next_mean = 0.0f, next_rstd = 0.0f;
-    auto fetch = [&](uint32_t row) {
-        next_mean = a.mean[row];
-        next_rstd = a.rstd[row];
+    Group group[kGroups];
 #pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-            const Group g(team.at + j * team.size, team.shift, a.cols);
-            g.load(x + (int64_t)row * a.ld_x, next_x[j]);
-            g.load(dy + (int64_t)row * a.ld_dy, next_dy[j]);
-            if (kAdd) g.load(add + (int64_t)row * a.ld_add, next_add[j]);
+    for (int j = 0; j < kGroups; ++j) group[j].set(team.at + j * team.size, team.shift, a.cols);
+    const int col = group[0].col;
+    Walk<const TD> dy(static_cast<const TD*>(a.dy), a.ld_dy, team.row, team.stride, col, team.size);
+    Walk<const TX> x(static_cast<const TX*>(a.x), a.ld_x, team.row, team.stride, col, team.size);
+    Walk<const TX> add(static_cast<const TX*>(a.add), a.ld_add, team.row, team.stride, col, team.size);
+    Walk<TX> dx(static_cast<TX*>(a.dx), a.ld_dx, team.row, team.stride, col, team.size);
+    uint32_t ahead = team.row;
+    auto copy = [&](uint32_t stage) {
+        if (ahead < rows) {
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) {
+                group[j].copy(dy.group(j), ring.target(stage, j * kRunsD), ring.kRun);
+                group[j].copy(x.group(j), ring.target(stage, kAtX + j * kRunsX), ring.kRun);
+                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kRunsX), ring.kRun);
+            }
         }
+        ring.commit();
+        ahead += team.stride;
+        dy.next();
+        x.next();
+        if (kAdd) add.next();
     };
-    if (team.row < rows) fetch(team.row);
+    if constexpr (kFeed == Feed::kRing)
+        for (uint32_t s = 0; s != ring.fill; s += kAll * ring.kRun) copy(s);
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (team.row < rows) {
+        next_mean = a.mean[team.row];
+        next_rstd = a.rstd[team.row];
+    }
     fill_places(params, a.gamma, a.w_type, a.cols, places, team.shift, 1.0f);
     __syncthreads();
-    const float cols = (float)a.cols;
-    float dg[kGroups][kGroup] = {}, db[kGroups][kGroup] = {};
+    const float each = 1.0f / (float)a.cols;
+    Eight dg[kGroups] = {}, db[kGroups] = {};
     uint32_t turn_row = team.row - (uint32_t)team.team * (uint32_t)shape.step;
     for (uint32_t r = team.row; turn_row < rows; turn_row += team.stride, r += team.stride) {
-        const float mean = next_mean, rstd = next_rstd;
         const bool mine = r < rows;
-        float h[kGroups][kGroup], d[kGroups][kGroup], c1 = 0.0f, c2 = 0.0f;
-        Raw8<TX, Group::template align<TX>()> more[kGroups];
+        const uint64_t minus_mean = both(-next_mean), by = both(next_rstd);
+        if (r + team.stride < rows) {
+            next_mean = a.mean[r + team.stride];
+            next_rstd = a.rstd[r + team.stride];
+        }
+        if constexpr (kFeed == Feed::kRing) {
+            copy(ring.fill);
+            ring.wait();
+        }
+        Eight h[kGroups], d[kGroups];
+        uint64_t c1 = 0, c2 = 0;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
-            const int place = team.at + j * team.size;
-            const Group g(place, team.shift, a.cols);
-            float w[kGroup];
-            read_place(params, places, place < places ? place : 0, w);
-            next_x[j].unpack(h[j]);
-            next_dy[j].unpack(d[j]);
-            if (kAdd) more[j] = next_add[j];
+            RawX raw_x;
+            RawD raw_d;
+            if constexpr (kFeed == Feed::kRing) {
+                ring.read(j * kRunsD, raw_d);
+                ring.read(kAtX + j * kRunsX, raw_x);
+            } else if (mine) {
+                group[j].load(dy.group(j), raw_d);
+                group[j].load(x.group(j), raw_x);
+            }
+            d[j].from(raw_d);
+            h[j].from(raw_x);
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k) h[j][k] = (h[j][k] - mean) * rstd;
-            g.trim(h[j]);
-            g.trim(d[j]);
+            for (int i = 0; i < 4; ++i) h[j].p[i] = mul2(add2(h[j].p[i], minus_mean), by);
+            if (!group[j].whole) {
+                h[j].trim(group[j].lo, group[j].hi);
+                d[j].trim(group[j].lo, group[j].hi);
+            }
             if (mine) {
 #pragma unroll
-                for (int k = 0; k < kGroup; ++k) {
-                    db[j][k] += d[j][k];
-                    dg[j][k] += d[j][k] * h[j][k];
+                for (int i = 0; i < 4; ++i) {
+                    db[j].p[i] = add2(db[j].p[i], d[j].p[i]);
+                    dg[j].p[i] = fma2(d[j].p[i], h[j].p[i], dg[j].p[i]);
                 }
             }
+            Eight w;
+            read_place(params, places, group[j].any ? team.at + j * team.size : 0, w);
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k) {
-                d[j][k] *= w[k];
-                c1 += d[j][k];
-                c2 += d[j][k] * h[j][k];
+            for (int i = 0; i < 4; ++i) {
+                d[j].p[i] = mul2(d[j].p[i], w.p[i]);
+                c2 = fma2(d[j].p[i], h[j].p[i], c2);
+            }
+            c1 = add2(c1, d[j].sum());
+        }
+        if (a.dx) {
+            const float2 c = team.sum(folded(c1), folded(c2));
+            if (mine) {
+                const uint64_t minus_c1 = both(-(c.x * each)), minus_c2 = both(-(c.y * each));
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) {
+                    if (!group[j].any) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[j].p[i] = mul2(fma2(h[j].p[i], minus_c2, add2(d[j].p[i], minus_c1)), by);
+                    if (kAdd) {
+                        RawX raw;
+                        Eight m;
+                        if constexpr (kFeed == Feed::kRing) ring.read(kAtAdd + j * kRunsX, raw);
+                        else group[j].load(add.group(j), raw);
+                        m.from(raw);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d[j].p[i] = add2(d[j].p[i], m.p[i]);
+                    }
+                    group[j].store(dx.group(j), d[j]);
+                }
             }
         }
-        if (r + team.stride < rows) fetch(r + team.stride);
-        if (!a.dx) continue;
-        float2 c = team.sum(c1, c2);
-        if (!mine) continue;
-        c.x /= cols;
-        c.y /= cols;
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-            const Group g(team.at + j * team.size, team.shift, a.cols);
-#pragma unroll
-            for (int k = 0; k < kGroup; ++k) d[j][k] = rstd * (d[j][k] - c.x - h[j][k] * c.y);
-            if (kAdd) more[j].add_to(d[j]);
-            if (g.hi > g.lo) g.store(static_cast<TX*>(a.dx) + (int64_t)r * a.ld_dx, d[j]);
+        dx.next();
+        if constexpr (kFeed == Feed::kRing) {
+            ring.next();
+        } else {
+            dy.next();
+            x.next();
+            if (kAdd) add.next();
         }
     }
     if (!a.dgamma && !a.dbeta) return;
     // the teams' sums in order
-    float* beta = params + places * kGroup;
     for (int t = 0; t < team.teams; ++t) {
         __syncthreads();
         if (t != team.team) continue;
@@ -98,13 +149,13 @@ __global__ void __launch_bounds__(kTeamMost) k_layer_norm_grad(const __grid_cons
             const int place = team.at + j * team.size;
             if (place >= places) break;
             if (t) {
-                float was[kGroup];
+                Eight was;
                 read_place(params, places, place, was);
 #pragma unroll
-                for (int k = 0; k < kGroup; ++k) dg[j][k] += was[k];
+                for (int i = 0; i < 4; ++i) dg[j].p[i] = add2(dg[j].p[i], was.p[i]);
                 read_place(beta, places, place, was);
 #pragma unroll
-                for (int k = 0; k < kGroup; ++k) db[j][k] += was[k];
+                for (int i = 0; i < 4; ++i) db[j].p[i] = add2(db[j].p[i], was.p[i]);
             }
             write_place(params, places, place, dg[j]);
             write_place(beta, places, place, db[j]);
@@ -159,25 +210,37 @@ deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int 
         m.add(a.dy, a.ld_dy, type_bytes(dy_type));
         m.add(a.add, a.ld_add, type_bytes(x_type));
         m.add(a.dx, a.ld_dx, type_bytes(x_type));
-        const TeamShape s = team_shape(m, a.rows, a.cols, a.cols > kTeamMost * 16 - 8 ? 4 : 2, kPartials);
+        const int elem = (int)type_bytes(x_type);
+        const TeamShape s = team_shape(m, a.rows, a.cols, kGroup * ((int)type_bytes(dy_type) + elem * (a.add ? 2 : 1)), 2, 2, kPartials);
         blocks = s.blocks;
-        const size_t smem = 2 * sizeof(float) * (size_t)(s.places * kGroup);
         const deft_status st = with_type(dy_type, [&](auto d) {
             return with_type(x_type, [&](auto x) {
-                return with_groups(s.aligned ? s.groups : 4, [&](auto g) -> deft_status {
+                return with_groups(s.groups, [&](auto g) -> deft_status {
                     using TD = decltype(d);
                     using TX = decltype(x);
                     constexpr int kGroups = decltype(g)::value;
                     auto run = [&](auto kernel) -> deft_status {
-                        if (smem > 48 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-                        kernel<<<s.blocks, s.threads, smem, stream>>>(a, s);
+                        if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+                        kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
                         DEFT_CUDA_TRY(cudaGetLastError());
                         return DEFT_OK;
                     };
+                    auto fed = [&](auto feed) {
+                        constexpr Feed kFeed = decltype(feed)::value;
+                        auto sized = [&](auto threads) {
+                            constexpr int kThreads = decltype(threads)::value;
+                            return a.add ? run(k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads>) : run(k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads>);
+                        };
+                        if constexpr (kGroups == 4) {
+                            if (s.threads > kTeamThreads) return sized(AlignTag<kTeamMost>{});
+                        }
+                        return sized(AlignTag<kTeamThreads>{});
+                    };
                     if constexpr (kGroups == 4) {
-                        if (!s.aligned) return a.add ? run(k_layer_norm_grad<true, TD, TX, false, 4>) : run(k_layer_norm_grad<false, TD, TX, false, 4>);
+                        if (s.feed == Feed::kElements) return fed(FeedTag<Feed::kElements>{});
+                        if (s.feed == Feed::kLoads) return fed(FeedTag<Feed::kLoads>{});
                     }
-                    return a.add ? run(k_layer_norm_grad<true, TD, TX, true, kGroups>) : run(k_layer_norm_grad<false, TD, TX, true, kGroups>);
+                    return fed(FeedTag<Feed::kRing>{});
                 });
             });
         });

@@ -1,18 +1,27 @@
-// Rows in registers: how layer norm and its gradient split a matrix.
+// How layer norm and its gradient split a matrix, and how its rows reach them.
 //
 // A row belongs to a team of 4 to 512 threads; a thread has up to four of the row's groups of eight columns, every
-// `size`-th one.  Groups start on 16-byte boundaries whatever the row's address is: with odd widths the groups of row r are
+// `size`-th one, in registers.  Groups come through a ring of asynchronous copies in shared memory, a few rows ahead of the one that
+// is worked on, each thread its own (no barrier); loads into registers ahead of their use take the registers that the
+// weight sums need, and give half of the bytes in flight.  Groups start on 16-byte boundaries whatever the row's address is: with odd widths the groups of row r are
 // shifted left by (first + r ld) mod 8 columns, which suits 16-bit and 32-bit matrices alike as long as they agree in
 // `first` and `ld` modulo 8.  A CTA takes rows of one shift only (every step-th row), so that the shift is a
 // constant of the CTA and a thread's columns stay the same from row to row.
 #pragma once
 #include "deft_dense.cuh"
+#include "deft_pairs.cuh"
 
 namespace deft {
 
 constexpr int kTeamThreads = 256;        // of a CTA; more where a row takes more
 constexpr int kTeamMost = 512;
 constexpr int kTeamMostWarps = kTeamMost / 32;
+constexpr int kMostStages = 4;
+
+// How a thread gets its groups: through the ring, by 16-byte loads (where the ring finds no room), or element by element (rows that
+// no shift suits).
+enum class Feed { kRing, kLoads, kElements };
+template <Feed kFeed> struct FeedTag { static constexpr Feed value = kFeed; };
 
 // The geometry of a call.
 struct TeamShape {
@@ -21,7 +30,9 @@ struct TeamShape {
     int step;                            // rows r, r + step, ... have the same shift
     int first, ld;                       // the shift of row r is (first + r ld) mod 8
     unsigned blocks;                     // a multiple of step
-    bool aligned;                        // 16-byte pieces; else single elements
+    Feed feed;
+    int stages;                          // of the ring
+    size_t smem;
 };
 
 // The matrices of a call: whether one shift serves all of them.
@@ -42,95 +53,157 @@ struct ShiftFinder {
     }
 };
 
-inline TeamShape team_shape(const ShiftFinder& m, int64_t rows, int cols, int most, int64_t most_blocks) {
+// row_bytes: bytes of eight columns of all matrices that are read; params: fp32 vectors of the row's length in shared memory; per_sm:
+// CTAs of kTeamThreads threads with up to two groups each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
+// Rows of up to 4096 columns have two groups a thread (their registers leave room for enough warps), longer ones four.
+inline TeamShape team_shape(const ShiftFinder& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks) {
     TeamShape s{};
-    s.aligned = m.ok;
+    bool shifted = m.ok;
     const int count = m.half ? 3 : 7;    // shifts of 32-bit matrices alone count modulo 4
-    s.first = m.ok ? m.first & count : 0;
-    s.ld = m.ok ? m.ld & count : 0;
-    s.step = s.ld == 0 ? 1 : (s.ld == 4 ? 2 : (s.ld & 1 ? 8 : 4));
-    s.places = (cols + (s.step > 1 ? 7 : s.first) + kGroup - 1) / kGroup;
+    auto place = [&]() {
+        s.first = shifted ? m.first & count : 0;
+        s.ld = shifted ? m.ld & count : 0;
+        s.step = s.ld == 0 ? 1 : (s.ld == 4 ? 2 : (s.ld & 1 ? 8 : 4));
+        s.places = (cols + (s.step > 1 ? 7 : s.first) + kGroup - 1) / kGroup;
+    };
+    place();
     if (s.places > kTeamMost * 4) {      // the longest rows leave no room for a shift
-        s.aligned = false;
-        s.first = s.ld = 0;
-        s.step = 1;
-        s.places = (cols + kGroup - 1) / kGroup;
+        shifted = false;
+        place();
     }
+    const int most = s.places <= kTeamThreads * 2 ? 2 : 4;
+    if (most == 4) per_sm = s.places <= kTeamThreads * 4 ? 2 : 1;
     s.size = 4;
     while (s.size < kTeamMost && s.size * most < s.places) s.size *= 2;
     // few rows: more threads for each, so that all SMs' schedulers have work
     while (s.size < kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
     const int each = (s.places + s.size - 1) / s.size;
-    s.groups = each <= 1 ? 1 : (each <= 2 ? 2 : 4);
+    s.groups = most == 4 ? 4 : (each <= 1 ? 1 : 2);
     s.threads = s.size > kTeamThreads ? s.size : kTeamThreads;
+    if (most_blocks == 0) most_blocks = (int64_t)sm_count() * per_sm;
     const int64_t teams = s.threads / s.size, needed = ((rows + s.step - 1) / s.step + teams - 1) / teams;   // CTAs for the rows of a shift
     const int64_t most_each = most_blocks / s.step;
     s.blocks = (unsigned)((needed < most_each ? needed : most_each) * s.step);
+    // the ring: as many stages as a CTA's share of an SM's shared memory has room for, and as a team has rows
+    const size_t stage = (size_t)s.threads * s.groups * row_bytes;
+    s.smem = (size_t)params * sizeof(float) * (size_t)(s.places * kGroup);
+    const size_t share = (size_t)220 * 1024 / per_sm;
+    const int64_t turns = (needed * s.step + s.blocks - 1) / s.blocks;
+    s.stages = share > s.smem ? (int)((share - s.smem) / stage) : 0;
+    if (s.stages > kMostStages) s.stages = kMostStages;
+    if (s.stages > turns) s.stages = (int)turns;
+    s.feed = !shifted ? Feed::kElements : (s.stages >= 1 ? Feed::kRing : Feed::kLoads);
+    if (s.feed == Feed::kRing) s.smem += stage * s.stages;
+    else s.groups = 4;
     return s;
 }
 
-// One of a thread's groups: its columns, and which of them are the row's.
-template <bool kAligned>
+// One of a thread's groups: which of its elements are the row's.  Made once, as a CTA's rows all lie alike.
+template <Feed kFeed>
 struct RowGroup {
-    int col, lo, hi;                     // first column (may lie before the row); the group's elements lo .. hi are the row's
-    __device__ __forceinline__ RowGroup(int place, int shift, int cols) {
+    int col, lo, hi;                     // first column (may lie before the row); elements lo .. hi are the row's
+    bool whole, any;
+    __device__ __forceinline__ void set(int place, int shift, int cols) {
         col = place * kGroup - shift;
         lo = col < 0 ? -col : 0;
         hi = cols - col < kGroup ? cols - col : kGroup;
+        any = hi > lo;
+        whole = lo == 0 && hi == kGroup;
     }
-    __device__ __forceinline__ bool whole() const { return lo == 0 && hi == kGroup; }
-    __device__ __forceinline__ bool has(int k) const { return k >= lo && k < hi; }
-    template <typename T> static __host__ __device__ constexpr int align() { return kAligned ? 16 : (int)sizeof(T); }
+    template <typename T> static __host__ __device__ constexpr int align() { return kFeed != Feed::kElements ? 16 : (int)sizeof(T); }
+    // `row` points to the group's first column throughout.  16-byte pieces that hold an element of the row, to shared memory: the
+    // first piece to `to`, a second one `apart` bytes further.
+    template <typename T>
+    __device__ __forceinline__ void copy(const T* row, uint32_t to, uint32_t apart) const {
+        constexpr int pieces = kGroup * (int)sizeof(T) / 16, per = kGroup / pieces;
+        const char* from = reinterpret_cast<const char*>(row);
+#pragma unroll
+        for (int i = 0; i < pieces; ++i)
+            if (whole || ((i + 1) * per > lo && i * per < hi))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (uint32_t)i * apart), "l"(from + i * 16) : "memory");
+    }
     // Plain loads: a row may be overwritten by its own threads later.
     template <typename T>
     __device__ __forceinline__ void load(const T* row, Raw8<T, align<T>()>& raw) const {
         using R = Raw8<T, align<T>()>;
         constexpr int per = kGroup / R::kPieces;
-        const typename R::P* p = reinterpret_cast<const typename R::P*>(row + col);
-        if (whole()) {
+        const typename R::P* p = reinterpret_cast<const typename R::P*>(row);
 #pragma unroll
-            for (int i = 0; i < R::kPieces; ++i) raw.piece[i] = p[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < R::kPieces; ++i)
-                if ((i + 1) * per > lo && i * per < hi) raw.piece[i] = p[i];
-        }
-    }
-    // What is not the row's becomes zero.
-    __device__ __forceinline__ void trim(float (&v)[kGroup]) const {
-        if (whole()) return;
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) v[k] = has(k) ? v[k] : 0.0f;
+        for (int i = 0; i < R::kPieces; ++i)
+            if (whole || ((i + 1) * per > lo && i * per < hi)) raw.piece[i] = p[i];
     }
     template <typename T>
-    __device__ __forceinline__ void store(T* row, const float (&v)[kGroup]) const {
+    __device__ __forceinline__ void store(T* row, const Eight& v) const {
         using R = Raw8<T, align<T>()>;
-        constexpr int per = kGroup / R::kPieces;
         R raw;
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) reinterpret_cast<T*>(raw.piece)[k] = from_f32<T>(v[k]);
-        typename R::P* p = reinterpret_cast<typename R::P*>(row + col);
-        if (whole()) {
+        v.to(raw);
+        if (whole) {
+            typename R::P* p = reinterpret_cast<typename R::P*>(row);
 #pragma unroll
             for (int i = 0; i < R::kPieces; ++i) p[i] = raw.piece[i];
         } else {
 #pragma unroll
             for (int k = 0; k < kGroup; ++k)
-                if (has(k)) row[col + k] = reinterpret_cast<const T*>(raw.piece)[k];
+                if (k >= lo && k < hi) row[k] = reinterpret_cast<const T*>(raw.piece)[k];
         }
+    }
+};
+
+// A matrix's rows as a thread meets them: the address of its first group in the row that comes next, and the distance to its
+// next group.
+template <typename T>
+struct Walk {
+    T* at;
+    int64_t down;                        // elements to the next row of this team
+    int across;
+    __device__ __forceinline__ Walk(T* base, int64_t ld, uint32_t row, uint32_t stride, int col, int size)
+        : at(base ? base + (int64_t)row * ld + col : nullptr), down((int64_t)stride * ld), across(size * kGroup) {}
+    __device__ __forceinline__ T* group(int j) const { return at + j * across; }
+    __device__ __forceinline__ void next() { at += down; }
+};
+
+// The ring of a CTA.  A stage holds, for each matrix, group and piece, a run of 16 bytes for every thread.
+template <int kThreads, int kAll>
+struct Ring {
+    static constexpr uint32_t kRun = kThreads * 16u;
+    const char* mine;                    // this thread's place in the first run of the first stage, and the same as a shared address
+    uint32_t at;
+    uint32_t now, fill, end;             // the row's stage, the one that is filled meanwhile, behind the last: offsets
+    int ahead;                           // stages that may still be under way
+    __device__ __forceinline__ Ring(const char* base, int stages)
+        : mine(base + threadIdx.x * 16u), at((uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * 16u), now(0), fill((uint32_t)(stages - 1) * kAll * kRun),
+          end((uint32_t)stages * kAll * kRun), ahead(stages - 1) {}
+    __device__ __forceinline__ uint32_t target(uint32_t stage, int run) const { return at + stage + (uint32_t)run * kRun; }
+    template <typename T>
+    __device__ __forceinline__ void read(int run, Raw8<T, 16>& raw) const {
+#pragma unroll
+        for (int i = 0; i < Raw8<T, 16>::kPieces; ++i) raw.piece[i] = *reinterpret_cast<const uint4*>(mine + now + (uint32_t)(run + i) * kRun);
+    }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // Waits for the row's stage.
+    __device__ __forceinline__ void wait() const {
+        if (ahead >= 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (ahead == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    __device__ __forceinline__ void next() {
+        fill = now;
+        now += kAll * kRun;
+        if (now == end) now = 0;
     }
 };
 
 // Parameters and sums of the places in shared memory: the first halves of all groups, then the second ones, so that
 // consecutive threads' 16-byte accesses are consecutive.
 __device__ __forceinline__ int at_place(int places, int place, int k) { return ((k >> 2) * places + place) * 4 + (k & 3); }
-__device__ __forceinline__ void read_place(const float* s, int places, int place, float (&v)[kGroup]) {
-    const float4 a = reinterpret_cast<const float4*>(s)[place], b = reinterpret_cast<const float4*>(s)[places + place];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+__device__ __forceinline__ void read_place(const float* s, int places, int place, Eight& v) {
+    const ulonglong2 a = reinterpret_cast<const ulonglong2*>(s)[place], b = reinterpret_cast<const ulonglong2*>(s)[places + place];
+    v.p[0] = a.x, v.p[1] = a.y, v.p[2] = b.x, v.p[3] = b.y;
 }
-__device__ __forceinline__ void write_place(float* s, int places, int place, const float (&v)[kGroup]) {
-    reinterpret_cast<float4*>(s)[place] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(s)[places + place] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void write_place(float* s, int places, int place, const Eight& v) {
+    reinterpret_cast<ulonglong2*>(s)[place] = make_ulonglong2(v.p[0], v.p[1]);
+    reinterpret_cast<ulonglong2*>(s)[places + place] = make_ulonglong2(v.p[2], v.p[3]);
 }
 __device__ __forceinline__ float param(const void* p, int type, int i) {
     return type == DEFT_F32 ? static_cast<const float*>(p)[i]
@@ -160,12 +233,19 @@ struct Team {
     }
     // The sums of a and b over the team.  All threads of a CTA call it equally often.
     __device__ __forceinline__ float2 sum(float a, float b) {
-        const int in_warp = size < 32 ? size : 32;
-        for (int o = in_warp >> 1; o; o >>= 1) {
+        if (size < 32) {
+            for (int o = size >> 1; o; o >>= 1) {
+                a += __shfl_xor_sync(0xffffffffu, a, o);
+                b += __shfl_xor_sync(0xffffffffu, b, o);
+            }
+            return make_float2(a, b);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, o);
             b += __shfl_xor_sync(0xffffffffu, b, o);
         }
-        if (size <= 32) return make_float2(a, b);
+        if (size == 32) return make_float2(a, b);
         // two sets of slots in turn: whoever writes a set again has passed the barrier that all pass after they have read it
         const int warps = size >> 5;
         float2* s = slots + turn * kTeamMostWarps + team * warps;
