@@ -1,39 +1,43 @@
 // Layer norm of the rows of a matrix.
 //
-// The mean is the first sum over the row's registers; the second pass over them sums d = v - mean and d^2, and the first of
-// these takes out what the rounded mean was off by, so that rows far from zero lose nothing.
+// One pass over the row's registers sums v and v^2, joined by one reduction; the variance is their difference where the mean
+// is no larger than the standard deviation.  Other rows (far from zero) take a second pass that sums d = v - mean and d^2, the
+// first of which takes out what the rounded mean was off by, so that they lose nothing.
 #include "deft_norm_rows.cuh"
 
 namespace deft {
 namespace {
 
+template <typename TX, typename TY> constexpr int kColsOf = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
+
 template <bool kAdd, typename TX, typename TY, Feed kFeed, int kGroups, int kThreads>
-__global__ void __launch_bounds__(kThreads, kGroups < 4 ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
+__global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TX, TY> < 32 ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma, beta, the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
-    using Group = RowGroup<kFeed>;
-    using Raw = Raw8<TX, Group::template align<TX>()>;
-    constexpr int kRuns = kGroup * (int)sizeof(TX) / 16, kAll = kGroups * kRuns * (kAdd ? 2 : 1);
-    Team team(shape, slots);
+    constexpr int kC = kColsOf<TX, TY>;
+    using Group = RowGroup<kFeed, kC>;
+    using Raw = typename Group::template Raw<TX>;
+    constexpr int kX = kC * (int)sizeof(TX), kAtAdd = kGroups * kX, kAll = kAtAdd * (kAdd ? 2 : 1);   // bytes of a thread in a stage
+    Team team(shape, kC, slots);
     const int places = shape.places;
-    float *gamma = reinterpret_cast<float*>(smem), *beta = gamma + places * kGroup;
-    Ring<kThreads, kAll> ring(smem + 2 * sizeof(float) * (size_t)(places * kGroup), shape.stages);
+    float *gamma = reinterpret_cast<float*>(smem), *beta = gamma + places * kC;
+    Ring<kThreads, kAll> ring(smem + 2 * sizeof(float) * (size_t)(places * kC), shape.stages);
     const uint32_t rows = (uint32_t)a.rows;
     Group group[kGroups];
 #pragma unroll
     for (int j = 0; j < kGroups; ++j) group[j].set(team.at + j * team.size, team.shift, a.cols);
-    const int col = group[0].col;
-    Walk<const TX> x(static_cast<const TX*>(a.x), a.ld_x, team.row, team.stride, col, team.size);
-    Walk<const TX> add(static_cast<const TX*>(a.add), a.ld_add, team.row, team.stride, col, team.size);
-    Walk<TX> sum_out(static_cast<TX*>(a.sum), a.ld_sum, team.row, team.stride, col, team.size);
-    Walk<TY> y(static_cast<TY*>(a.y), a.ld_y, team.row, team.stride, col, team.size);
+    const int col = team.at * kC - team.shift, across = team.size * kC;
+    Walk<const TX> x(static_cast<const TX*>(a.x), a.ld_x, team.row, team.stride, col, across);
+    Walk<const TX> add(static_cast<const TX*>(a.add), a.ld_add, team.row, team.stride, col, across);
+    Walk<TX> sum_out(static_cast<TX*>(a.sum), a.ld_sum, team.row, team.stride, col, across);
+    Walk<TY> y(static_cast<TY*>(a.y), a.ld_y, team.row, team.stride, col, across);
     uint32_t ahead = team.row;                           // the row that is copied next
     auto copy = [&](uint32_t stage) {
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(x.group(j), ring.target(stage, j * kRuns), ring.kRun);
-                if (kAdd) group[j].copy(add.group(j), ring.target(stage, (kGroups + j) * kRuns), ring.kRun);
+                group[j].copy(x.group(j), ring.target(stage, j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();
@@ -42,9 +46,9 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 4 : 1) k_layer_norm(co
         if (kAdd) add.next();
     };
     if constexpr (kFeed == Feed::kRing)
-        for (uint32_t s = 0; s != ring.fill; s += kAll * ring.kRun) copy(s);
-    fill_places(gamma, a.gamma, a.w_type, a.cols, places, team.shift, 1.0f);
-    fill_places(beta, a.beta, a.w_type, a.cols, places, team.shift, 0.0f);
+        for (uint32_t s = 0; s != ring.fill; s += ring.kStage) copy(s);
+    fill_places<kC>(gamma, a.gamma, a.w_type, a.cols, places, team.shift, 1.0f);
+    fill_places<kC>(beta, a.beta, a.w_type, a.cols, places, team.shift, 0.0f);
     __syncthreads();
     const float each = 1.0f / (float)a.cols;
     // all teams of a CTA take as many turns as its first one
@@ -55,64 +59,83 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 4 : 1) k_layer_norm(co
             copy(ring.fill);
             ring.wait();
         }
-        Eight v[kGroups];
-        uint64_t sum = 0;
+        Cols<kC> v[kGroups];
+        uint64_t s1 = 0, s2 = 0;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
+            v[j] = Cols<kC>{};
+            if (!group[j].any) continue;
             Raw raw, more;
             if constexpr (kFeed == Feed::kRing) {
-                ring.read(j * kRuns, raw);
-                if (kAdd) ring.read((kGroups + j) * kRuns, more);
+                ring.read(j * kX, raw);
+                if (kAdd) ring.read(kAtAdd + j * kX, more);
             } else if (mine) {
                 group[j].load(x.group(j), raw);
                 if (kAdd) group[j].load(add.group(j), more);
             }
             v[j].from(raw);
             if (kAdd) {
-                Eight m;
+                Cols<kC> m;
                 m.from(more);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[j].p[i] = add2(v[j].p[i], m.p[i]);
+                for (int i = 0; i < kC / 2; ++i) v[j].p[i] = add2(v[j].p[i], m.p[i]);
             }
             if (!group[j].whole) v[j].trim(group[j].lo, group[j].hi);
-            sum = add2(sum, v[j].sum());
-            if (kAdd && a.sum && mine && group[j].any) group[j].store(sum_out.group(j), v[j]);
+            if (kAdd && a.sum && mine) group[j].store(sum_out.group(j), v[j]);
+#pragma unroll
+            for (int i = 0; i < kC / 2; ++i) {
+                s1 = add2(s1, v[j].p[i]);
+                s2 = fma2(v[j].p[i], v[j].p[i], s2);
+            }
         }
         if constexpr (kFeed == Feed::kRing) ring.next();
-        const float mean = team.sum(folded(sum), 0.0f).x * each;
-        const uint64_t minus = both(-mean);
-        uint64_t d1 = 0, d2 = 0;
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[j].p[i] = add2(v[j].p[i], minus);
-            if (!group[j].whole) v[j].trim(group[j].lo, group[j].hi);
-            d1 = add2(d1, v[j].sum());
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d2 = fma2(v[j].p[i], v[j].p[i], d2);
-        }
-        const float2 sums = team.sum(folded(d1), folded(d2));
-        const float off = sums.x * each;
-        float var = sums.y * each - off * off;
-        var = (var < 0.0f ? 0.0f : var) + a.eps;
-        float rstd = rsqrtf(var);
-        if (var > 1e-30f && var < 1e30f) rstd = __fmaf_rn(0.5f * rstd, __fmaf_rn(-var * rstd, rstd, 1.0f), rstd);    // (a step of Newton's)
-        if (mine) {
-            const uint64_t minus_off = both(-off), by = both(rstd);
+        float2 sums = team.sum(folded(s1), folded(s2));
+        float mean = sums.x * each, var = __fmaf_rn(-mean, mean, sums.y * each);
+        // (a warp's teams go the same way)
+        bool far = !(mean * mean <= var);
+        if (team.size < 32) far = __any_sync(0xffffffffu, far);
+        if (far) {
+            const float first = mean;
+            const uint64_t minus = both(-first);
+            s1 = s2 = 0;
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
                 if (!group[j].any) continue;
-                Eight w, b;
+                Cols<kC> d;
+#pragma unroll
+                for (int i = 0; i < kC / 2; ++i) d.p[i] = add2(v[j].p[i], minus);
+                if (!group[j].whole) d.trim(group[j].lo, group[j].hi);
+                v[j] = d;
+#pragma unroll
+                for (int i = 0; i < kC / 2; ++i) {
+                    s1 = add2(s1, d.p[i]);
+                    s2 = fma2(d.p[i], d.p[i], s2);
+                }
+            }
+            sums = team.sum(folded(s1), folded(s2));
+            mean = sums.x * each;          // of what is in the registers now
+            var = __fmaf_rn(-mean, mean, sums.y * each);
+            if (var < 0.0f) var = 0.0f;
+            if (team.at == 0 && mine && a.mean) a.mean[r] = first + mean;
+        } else if (team.at == 0 && mine && a.mean) {
+            a.mean[r] = mean;
+        }
+        var += a.eps;
+        float rstd = rsqrtf(var);
+        if (var > 1e-30f && var < 1e30f) rstd = __fmaf_rn(0.5f * rstd, __fmaf_rn(-var * rstd, rstd, 1.0f), rstd);    // (a step of Newton's)
+        if (mine) {
+            const uint64_t by = both(rstd), plus = both(-mean * rstd);
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) {
+                if (!group[j].any) continue;
+                Cols<kC> w, b;
                 read_place(gamma, places, team.at + j * team.size, w);
                 read_place(beta, places, team.at + j * team.size, b);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[j].p[i] = fma2(mul2(add2(v[j].p[i], minus_off), by), w.p[i], b.p[i]);
+                for (int i = 0; i < kC / 2; ++i) v[j].p[i] = fma2(fma2(v[j].p[i], by, plus), w.p[i], b.p[i]);
                 group[j].store(y.group(j), v[j]);
             }
-            if (team.at == 0) {
-                if (a.mean) a.mean[r] = mean + off;
-                if (a.rstd) a.rstd[r] = rstd;
-            }
+            if (team.at == 0 && a.rstd) a.rstd[r] = rstd;
         }
         y.next();
         if (kAdd) sum_out.next();
@@ -126,40 +149,25 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 4 : 1) k_layer_norm(co
 }  // namespace
 
 deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cudaStream_t stream) {
-    ShiftFinder m;
-    m.add(a.x, a.ld_x, type_bytes(x_type));
-    m.add(a.y, a.ld_y, type_bytes(y_type));
-    m.add(a.add, a.ld_add, type_bytes(x_type));
-    m.add(a.sum, a.ld_sum, type_bytes(x_type));
-    const TeamShape s = team_shape(m, a.rows, a.cols, kGroup * (int)type_bytes(x_type) * (a.add ? 2 : 1), 2, 4, 0);
     return with_type(x_type, [&](auto x) {
         return with_type(y_type, [&](auto y) {
-            return with_groups(s.groups, [&](auto g) -> deft_status {
-                using TX = decltype(x);
-                using TY = decltype(y);
-                constexpr int kGroups = decltype(g)::value;
-                auto run = [&](auto kernel) -> deft_status {
-                    if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
-                    kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
-                    DEFT_CUDA_TRY(cudaGetLastError());
-                    return DEFT_OK;
-                };
-                auto fed = [&](auto feed) {
-                    constexpr Feed kFeed = decltype(feed)::value;
-                    auto sized = [&](auto threads) {
-                        constexpr int kThreads = decltype(threads)::value;
-                        return a.add ? run(k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads>) : run(k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads>);
-                    };
-                    if constexpr (kGroups == 4) {
-                        if (s.threads > kTeamThreads) return sized(AlignTag<kTeamMost>{});
-                    }
-                    return sized(AlignTag<kTeamThreads>{});
-                };
-                if constexpr (kGroups == 4) {
-                    if (s.feed == Feed::kElements) return fed(FeedTag<Feed::kElements>{});
-                    if (s.feed == Feed::kLoads) return fed(FeedTag<Feed::kLoads>{});
-                }
-                return fed(FeedTag<Feed::kRing>{});
+            using TX = decltype(x);
+            using TY = decltype(y);
+            constexpr int kC = kColsOf<TX, TY>;
+            Shifts m(kC);
+            m.add(a.x, a.ld_x, sizeof(TX));
+            m.add(a.y, a.ld_y, sizeof(TY));
+            m.add(a.add, a.ld_add, sizeof(TX));
+            m.add(a.sum, a.ld_sum, sizeof(TX));
+            const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 4, 0);
+            return with_shape<kC>(s, [&](auto feed, auto groups, auto threads) -> deft_status {
+                constexpr Feed kFeed = decltype(feed)::value;
+                constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
+                auto kernel = a.add ? k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads> : k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads>;
+                if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+                kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
+                DEFT_CUDA_TRY(cudaGetLastError());
+                return DEFT_OK;
             });
         });
     });

@@ -10,36 +10,39 @@ namespace {
 
 constexpr int kPartials = 2 * 148;   // CTAs that leave partial sums at most; a constant: a call's bits do not depend on the device
 
+template <typename TD, typename TX> constexpr int kColsOf = sizeof(TD) == 4 || sizeof(TX) == 4 ? 4 : 8;
+
 template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads>
-__global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
+__global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TD, TX> < 32 ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma and room for a second vector (at the end the CTA's sums), the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
-    using Group = RowGroup<kFeed>;
-    using RawX = Raw8<TX, Group::template align<TX>()>;
-    using RawD = Raw8<TD, Group::template align<TD>()>;
-    constexpr int kRunsX = kGroup * (int)sizeof(TX) / 16, kRunsD = kGroup * (int)sizeof(TD) / 16;
-    constexpr int kAtX = kGroups * kRunsD, kAtAdd = kAtX + kGroups * kRunsX, kAll = kAtAdd + (kAdd ? kGroups * kRunsX : 0);
-    Team team(shape, slots);
+    constexpr int kC = kColsOf<TD, TX>;
+    using Group = RowGroup<kFeed, kC>;
+    using RawX = typename Group::template Raw<TX>;
+    using RawD = typename Group::template Raw<TD>;
+    // bytes of a thread in a stage
+    constexpr int kX = kC * (int)sizeof(TX), kD = kC * (int)sizeof(TD), kAtX = kGroups * kD, kAtAdd = kAtX + kGroups * kX, kAll = kAtAdd + (kAdd ? kGroups * kX : 0);
+    Team team(shape, kC, slots);
     const int places = shape.places;
-    float *params = reinterpret_cast<float*>(smem), *beta = params + places * kGroup;
-    Ring<kThreads, kAll> ring(smem + 2 * sizeof(float) * (size_t)(places * kGroup), shape.stages);
+    float *params = reinterpret_cast<float*>(smem), *beta = params + places * kC;
+    Ring<kThreads, kAll> ring(smem + 2 * sizeof(float) * (size_t)(places * kC), shape.stages);
     const uint32_t rows = (uint32_t)a.rows;
     Group group[kGroups];
 #pragma unroll
     for (int j = 0; j < kGroups; ++j) group[j].set(team.at + j * team.size, team.shift, a.cols);
-    const int col = group[0].col;
-    Walk<const TD> dy(static_cast<const TD*>(a.dy), a.ld_dy, team.row, team.stride, col, team.size);
-    Walk<const TX> x(static_cast<const TX*>(a.x), a.ld_x, team.row, team.stride, col, team.size);
-    Walk<const TX> add(static_cast<const TX*>(a.add), a.ld_add, team.row, team.stride, col, team.size);
-    Walk<TX> dx(static_cast<TX*>(a.dx), a.ld_dx, team.row, team.stride, col, team.size);
+    const int col = team.at * kC - team.shift, across = team.size * kC;
+    Walk<const TD> dy(static_cast<const TD*>(a.dy), a.ld_dy, team.row, team.stride, col, across);
+    Walk<const TX> x(static_cast<const TX*>(a.x), a.ld_x, team.row, team.stride, col, across);
+    Walk<const TX> add(static_cast<const TX*>(a.add), a.ld_add, team.row, team.stride, col, across);
+    Walk<TX> dx(static_cast<TX*>(a.dx), a.ld_dx, team.row, team.stride, col, across);
     uint32_t ahead = team.row;
     auto copy = [&](uint32_t stage) {
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(dy.group(j), ring.target(stage, j * kRunsD), ring.kRun);
-                group[j].copy(x.group(j), ring.target(stage, kAtX + j * kRunsX), ring.kRun);
-                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kRunsX), ring.kRun);
+                group[j].copy(dy.group(j), ring.target(stage, j * kD, kD));
+                group[j].copy(x.group(j), ring.target(stage, kAtX + j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();
@@ -49,16 +52,16 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
         if (kAdd) add.next();
     };
     if constexpr (kFeed == Feed::kRing)
-        for (uint32_t s = 0; s != ring.fill; s += kAll * ring.kRun) copy(s);
+        for (uint32_t s = 0; s != ring.fill; s += ring.kStage) copy(s);
     float next_mean = 0.0f, next_rstd = 0.0f;
     if (team.row < rows) {
         next_mean = a.mean[team.row];
         next_rstd = a.rstd[team.row];
     }
-    fill_places(params, a.gamma, a.w_type, a.cols, places, team.shift, 1.0f);
+    fill_places<kC>(params, a.gamma, a.w_type, a.cols, places, team.shift, 1.0f);
     __syncthreads();
     const float each = 1.0f / (float)a.cols;
-    Eight dg[kGroups] = {}, db[kGroups] = {};
+    Cols<kC> dg[kGroups] = {}, db[kGroups] = {};
     uint32_t turn_row = team.row - (uint32_t)team.team * (uint32_t)shape.step;
     for (uint32_t r = team.row; turn_row < rows; turn_row += team.stride, r += team.stride) {
         const bool mine = r < rows;
@@ -71,15 +74,15 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
             copy(ring.fill);
             ring.wait();
         }
-        Eight h[kGroups], d[kGroups];
+        Cols<kC> h[kGroups], d[kGroups];
         uint64_t c1 = 0, c2 = 0;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
             RawX raw_x;
             RawD raw_d;
             if constexpr (kFeed == Feed::kRing) {
-                ring.read(j * kRunsD, raw_d);
-                ring.read(kAtX + j * kRunsX, raw_x);
+                ring.read(j * kD, raw_d);
+                ring.read(kAtX + j * kX, raw_x);
             } else if (mine) {
                 group[j].load(dy.group(j), raw_d);
                 group[j].load(x.group(j), raw_x);
@@ -87,26 +90,26 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
             d[j].from(raw_d);
             h[j].from(raw_x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[j].p[i] = mul2(add2(h[j].p[i], minus_mean), by);
+            for (int i = 0; i < kC / 2; ++i) h[j].p[i] = mul2(add2(h[j].p[i], minus_mean), by);
             if (!group[j].whole) {
                 h[j].trim(group[j].lo, group[j].hi);
                 d[j].trim(group[j].lo, group[j].hi);
             }
             if (mine) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < kC / 2; ++i) {
                     db[j].p[i] = add2(db[j].p[i], d[j].p[i]);
                     dg[j].p[i] = fma2(d[j].p[i], h[j].p[i], dg[j].p[i]);
                 }
             }
-            Eight w;
+            Cols<kC> w;
             read_place(params, places, group[j].any ? team.at + j * team.size : 0, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < kC / 2; ++i) {
                 d[j].p[i] = mul2(d[j].p[i], w.p[i]);
+                c1 = add2(c1, d[j].p[i]);
                 c2 = fma2(d[j].p[i], h[j].p[i], c2);
             }
-            c1 = add2(c1, d[j].sum());
         }
         if (a.dx) {
             const float2 c = team.sum(folded(c1), folded(c2));
@@ -116,15 +119,15 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
                 for (int j = 0; j < kGroups; ++j) {
                     if (!group[j].any) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d[j].p[i] = mul2(fma2(h[j].p[i], minus_c2, add2(d[j].p[i], minus_c1)), by);
+                    for (int i = 0; i < kC / 2; ++i) d[j].p[i] = mul2(fma2(h[j].p[i], minus_c2, add2(d[j].p[i], minus_c1)), by);
                     if (kAdd) {
                         RawX raw;
-                        Eight m;
-                        if constexpr (kFeed == Feed::kRing) ring.read(kAtAdd + j * kRunsX, raw);
+                        Cols<kC> m;
+                        if constexpr (kFeed == Feed::kRing) ring.read(kAtAdd + j * kX, raw);
                         else group[j].load(add.group(j), raw);
                         m.from(raw);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) d[j].p[i] = add2(d[j].p[i], m.p[i]);
+                        for (int i = 0; i < kC / 2; ++i) d[j].p[i] = add2(d[j].p[i], m.p[i]);
                     }
                     group[j].store(dx.group(j), d[j]);
                 }
@@ -149,13 +152,13 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
             const int place = team.at + j * team.size;
             if (place >= places) break;
             if (t) {
-                Eight was;
+                Cols<kC> was;
                 read_place(params, places, place, was);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) dg[j].p[i] = add2(dg[j].p[i], was.p[i]);
+                for (int i = 0; i < kC / 2; ++i) dg[j].p[i] = add2(dg[j].p[i], was.p[i]);
                 read_place(beta, places, place, was);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) db[j].p[i] = add2(db[j].p[i], was.p[i]);
+                for (int i = 0; i < kC / 2; ++i) db[j].p[i] = add2(db[j].p[i], was.p[i]);
             }
             write_place(params, places, place, dg[j]);
             write_place(beta, places, place, db[j]);
@@ -166,8 +169,8 @@ __global__ void __launch_bounds__(kThreads, kGroups < 4 ? 2 : 1) k_layer_norm_gr
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
         const int i = c + team.shift;
-        out[c] = params[at_place(places, i >> 3, i & 7)];
-        out[a.cols + c] = beta[at_place(places, i >> 3, i & 7)];
+        out[c] = params[at_place<kC>(places, i)];
+        out[a.cols + c] = beta[at_place<kC>(places, i)];
     }
 }
 
@@ -205,42 +208,26 @@ size_t layer_norm_grad_ws_bytes(int64_t rows, int64_t cols) {
 deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int x_type, cudaStream_t stream) {
     unsigned blocks = 0;
     if (a.rows) {
-        ShiftFinder m;
-        m.add(a.x, a.ld_x, type_bytes(x_type));
-        m.add(a.dy, a.ld_dy, type_bytes(dy_type));
-        m.add(a.add, a.ld_add, type_bytes(x_type));
-        m.add(a.dx, a.ld_dx, type_bytes(x_type));
-        const int elem = (int)type_bytes(x_type);
-        const TeamShape s = team_shape(m, a.rows, a.cols, kGroup * ((int)type_bytes(dy_type) + elem * (a.add ? 2 : 1)), 2, 2, kPartials);
-        blocks = s.blocks;
         const deft_status st = with_type(dy_type, [&](auto d) {
             return with_type(x_type, [&](auto x) {
-                return with_groups(s.groups, [&](auto g) -> deft_status {
-                    using TD = decltype(d);
-                    using TX = decltype(x);
-                    constexpr int kGroups = decltype(g)::value;
-                    auto run = [&](auto kernel) -> deft_status {
-                        if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
-                        kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
-                        DEFT_CUDA_TRY(cudaGetLastError());
-                        return DEFT_OK;
-                    };
-                    auto fed = [&](auto feed) {
-                        constexpr Feed kFeed = decltype(feed)::value;
-                        auto sized = [&](auto threads) {
-                            constexpr int kThreads = decltype(threads)::value;
-                            return a.add ? run(k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads>) : run(k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads>);
-                        };
-                        if constexpr (kGroups == 4) {
-                            if (s.threads > kTeamThreads) return sized(AlignTag<kTeamMost>{});
-                        }
-                        return sized(AlignTag<kTeamThreads>{});
-                    };
-                    if constexpr (kGroups == 4) {
-                        if (s.feed == Feed::kElements) return fed(FeedTag<Feed::kElements>{});
-                        if (s.feed == Feed::kLoads) return fed(FeedTag<Feed::kLoads>{});
-                    }
-                    return fed(FeedTag<Feed::kRing>{});
+                using TD = decltype(d);
+                using TX = decltype(x);
+                constexpr int kC = kColsOf<TD, TX>;
+                Shifts m(kC);
+                m.add(a.x, a.ld_x, sizeof(TX));
+                m.add(a.dy, a.ld_dy, sizeof(TD));
+                m.add(a.add, a.ld_add, sizeof(TX));
+                m.add(a.dx, a.ld_dx, sizeof(TX));
+                const TeamShape s = team_shape(m, a.rows, a.cols, (int)(sizeof(TD) + sizeof(TX) * (a.add ? 2 : 1)), 2, 2, kPartials);
+                blocks = s.blocks;
+                return with_shape<kC>(s, [&](auto feed, auto groups, auto threads) -> deft_status {
+                    constexpr Feed kFeed = decltype(feed)::value;
+                    constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
+                    auto kernel = a.add ? k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads> : k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads>;
+                    if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+                    kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
+                    DEFT_CUDA_TRY(cudaGetLastError());
+                    return DEFT_OK;
                 });
             });
         });

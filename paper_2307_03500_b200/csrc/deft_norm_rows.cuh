@@ -1,7 +1,8 @@
 // How layer norm and its gradient split a matrix, and how its rows reach them.
 //
-// A row belongs to a team of 4 to 512 threads; a thread has up to four of the row's groups of eight columns, every
-// `size`-th one, in registers.  Groups come through a ring of asynchronous copies in shared memory, a few rows ahead of the one that
+// A row belongs to a team of 4 to 512 threads; a thread has some of the row's groups, every `size`-th one, in registers.  A group is
+// what fills 16 bytes: eight columns of 16-bit matrices, four where one of the matrices is fp32 (two such pieces side by
+// side for each thread would make every access touch each 32-byte sector twice: 16384 x 1024 fp32 36 us).  Groups come through a ring of asynchronous copies in shared memory, a few rows ahead of the one that
 // is worked on, each thread its own (no barrier); loads into registers ahead of their use take the registers that the
 // weight sums need, and give half of the bytes in flight.  Groups start on 16-byte boundaries whatever the row's address is: with odd widths the groups of row r are
 // shifted left by (first + r ld) mod 8 columns, which suits 16-bit and 32-bit matrices alike as long as they agree in
@@ -28,65 +29,62 @@ struct TeamShape {
     int size, groups, threads;           // threads of a team, groups of each, threads of a CTA
     int places;                          // groups of a row with its shift: what the parameters in shared memory are laid out by
     int step;                            // rows r, r + step, ... have the same shift
-    int first, ld;                       // the shift of row r is (first + r ld) mod 8
+    int first, ld;                       // the shift of row r is (first + r ld) modulo the length of a group
     unsigned blocks;                     // a multiple of step
     Feed feed;
     int stages;                          // of the ring
     size_t smem;
 };
 
-// The matrices of a call: whether one shift serves all of them.
-struct ShiftFinder {
-    int first = -1, ld = 0;
-    bool any = false, ok = true, half = false;   // half: only 32-bit matrices so far (shifts count modulo 4)
+// The matrices of a call: how long a group is, and whether one shift serves all of them.
+struct Shifts {
+    int cols, first = -1, ld = 0;
+    bool ok = true;
+    explicit Shifts(int cols_) : cols(cols_) {}
     void add(const void* p, int64_t pitch, size_t elem) {
         if (!p) return;
-        const int f = (int)(reinterpret_cast<uintptr_t>(p) / elem & 7), l = (int)(pitch & 7);
-        const bool wide = elem == 4;
-        if (!any) {
-            first = f, ld = l, half = wide, any = true;
-            return;
-        }
-        const int mask = wide || half ? 3 : 7;
-        if (((f ^ first) & mask) || ((l ^ ld) & mask)) ok = false;
-        if (half && !wide) first = f, ld = l, half = false;
+        const int f = (int)(reinterpret_cast<uintptr_t>(p) / elem) & (cols - 1), l = (int)pitch & (cols - 1);
+        if (first >= 0 && (f != first || l != ld)) ok = false;
+        first = f;
+        ld = l;
     }
 };
 
-// row_bytes: bytes of eight columns of all matrices that are read; params: fp32 vectors of the row's length in shared memory; per_sm:
-// CTAs of kTeamThreads threads with up to two groups each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
-// Rows of up to 4096 columns have two groups a thread (their registers leave room for enough warps), longer ones four.
-inline TeamShape team_shape(const ShiftFinder& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks) {
+// row_bytes: bytes of a column of all matrices that are read; params: fp32 vectors of the row's length in shared memory; per_sm:
+// CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
+// Rows of up to 4096 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32.
+inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks) {
     TeamShape s{};
     bool shifted = m.ok;
-    const int count = m.half ? 3 : 7;    // shifts of 32-bit matrices alone count modulo 4
+    const int len = m.cols;
     auto place = [&]() {
-        s.first = shifted ? m.first & count : 0;
-        s.ld = shifted ? m.ld & count : 0;
-        s.step = s.ld == 0 ? 1 : (s.ld == 4 ? 2 : (s.ld & 1 ? 8 : 4));
-        s.places = (cols + (s.step > 1 ? 7 : s.first) + kGroup - 1) / kGroup;
+        s.first = shifted ? m.first : 0;
+        s.ld = shifted ? m.ld : 0;
+        s.step = 1;
+        while ((s.ld * s.step) & (len - 1)) s.step *= 2;
+        s.places = (cols + (s.step > 1 ? len - 1 : s.first) + len - 1) / len;
     };
     place();
-    if (s.places > kTeamMost * 4) {      // the longest rows leave no room for a shift
+    if (s.places * len > kTeamMost * 32) {      // the longest rows leave no room for a shift
         shifted = false;
         place();
     }
-    const int most = s.places <= kTeamThreads * 2 ? 2 : 4;
-    if (most == 4) per_sm = s.places <= kTeamThreads * 4 ? 2 : 1;
+    const bool wide = s.places * len > kTeamThreads * 16;
+    if (wide) per_sm = s.places * len <= kTeamThreads * 32 ? 2 : 1;
+    const int most = (wide ? 32 : 16) / len;
     s.size = 4;
     while (s.size < kTeamMost && s.size * most < s.places) s.size *= 2;
     // few rows: more threads for each, so that all SMs' schedulers have work
     while (s.size < kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
-    const int each = (s.places + s.size - 1) / s.size;
-    s.groups = most == 4 ? 4 : (each <= 1 ? 1 : 2);
+    s.groups = wide || s.size * (most / 2) < s.places ? most : most / 2;
     s.threads = s.size > kTeamThreads ? s.size : kTeamThreads;
     if (most_blocks == 0) most_blocks = (int64_t)sm_count() * per_sm;
     const int64_t teams = s.threads / s.size, needed = ((rows + s.step - 1) / s.step + teams - 1) / teams;   // CTAs for the rows of a shift
     const int64_t most_each = most_blocks / s.step;
     s.blocks = (unsigned)((needed < most_each ? needed : most_each) * s.step);
     // the ring: as many stages as a CTA's share of an SM's shared memory has room for, and as a team has rows
-    const size_t stage = (size_t)s.threads * s.groups * row_bytes;
-    s.smem = (size_t)params * sizeof(float) * (size_t)(s.places * kGroup);
+    const size_t stage = (size_t)s.threads * s.groups * len * row_bytes;
+    s.smem = (size_t)params * sizeof(float) * (size_t)(s.places * len);
     const size_t share = (size_t)220 * 1024 / per_sm;
     const int64_t turns = (needed * s.step + s.blocks - 1) / s.blocks;
     s.stages = share > s.smem ? (int)((share - s.smem) / stage) : 0;
@@ -94,56 +92,51 @@ inline TeamShape team_shape(const ShiftFinder& m, int64_t rows, int cols, int ro
     if (s.stages > turns) s.stages = (int)turns;
     s.feed = !shifted ? Feed::kElements : (s.stages >= 1 ? Feed::kRing : Feed::kLoads);
     if (s.feed == Feed::kRing) s.smem += stage * s.stages;
-    else s.groups = 4;
+    else s.groups = 32 / len;
     return s;
 }
 
 // One of a thread's groups: which of its elements are the row's.  Made once, as a CTA's rows all lie alike.
-template <Feed kFeed>
+template <Feed kFeed, int kC>
 struct RowGroup {
-    int col, lo, hi;                     // first column (may lie before the row); elements lo .. hi are the row's
+    static constexpr bool kPieces = kFeed != Feed::kElements;
+    int lo, hi;                          // elements lo .. hi are the row's
     bool whole, any;
     __device__ __forceinline__ void set(int place, int shift, int cols) {
-        col = place * kGroup - shift;
+        const int col = place * kC - shift;
         lo = col < 0 ? -col : 0;
-        hi = cols - col < kGroup ? cols - col : kGroup;
+        hi = cols - col < kC ? cols - col : kC;
         any = hi > lo;
-        whole = lo == 0 && hi == kGroup;
+        whole = lo == 0 && hi == kC;
     }
-    template <typename T> static __host__ __device__ constexpr int align() { return kFeed != Feed::kElements ? 16 : (int)sizeof(T); }
-    // `row` points to the group's first column throughout.  16-byte pieces that hold an element of the row, to shared memory: the
-    // first piece to `to`, a second one `apart` bytes further.
+    template <typename T> using Raw = RawCols<T, kC, kPieces>;
+    // `row` points to the group's first column throughout (which may lie before the row).  Whole pieces are read where an element of
+    // them is the row's.
     template <typename T>
-    __device__ __forceinline__ void copy(const T* row, uint32_t to, uint32_t apart) const {
-        constexpr int pieces = kGroup * (int)sizeof(T) / 16, per = kGroup / pieces;
-        const char* from = reinterpret_cast<const char*>(row);
-#pragma unroll
-        for (int i = 0; i < pieces; ++i)
-            if (whole || ((i + 1) * per > lo && i * per < hi))
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (uint32_t)i * apart), "l"(from + i * 16) : "memory");
+    __device__ __forceinline__ void copy(const T* row, uint32_t to) const {
+        if (!any) return;
+        if constexpr (kC * sizeof(T) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(row) : "memory");
     }
     // Plain loads: a row may be overwritten by its own threads later.
     template <typename T>
-    __device__ __forceinline__ void load(const T* row, Raw8<T, align<T>()>& raw) const {
-        using R = Raw8<T, align<T>()>;
-        constexpr int per = kGroup / R::kPieces;
-        const typename R::P* p = reinterpret_cast<const typename R::P*>(row);
+    __device__ __forceinline__ void load(const T* row, Raw<T>& raw) const {
+        using R = Raw<T>;
 #pragma unroll
         for (int i = 0; i < R::kPieces; ++i)
-            if (whole || ((i + 1) * per > lo && i * per < hi)) raw.piece[i] = p[i];
+            if ((i + 1) * R::kPer > lo && i * R::kPer < hi) raw.piece[i] = reinterpret_cast<const typename R::P*>(row)[i];
     }
     template <typename T>
-    __device__ __forceinline__ void store(T* row, const Eight& v) const {
-        using R = Raw8<T, align<T>()>;
+    __device__ __forceinline__ void store(T* row, const Cols<kC>& v) const {
+        using R = Raw<T>;
         R raw;
         v.to(raw);
         if (whole) {
-            typename R::P* p = reinterpret_cast<typename R::P*>(row);
 #pragma unroll
-            for (int i = 0; i < R::kPieces; ++i) p[i] = raw.piece[i];
+            for (int i = 0; i < R::kPieces; ++i) reinterpret_cast<typename R::P*>(row)[i] = raw.piece[i];
         } else {
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k)
+            for (int k = 0; k < kC; ++k)
                 if (k >= lo && k < hi) row[k] = reinterpret_cast<const T*>(raw.piece)[k];
         }
     }
@@ -156,29 +149,27 @@ struct Walk {
     T* at;
     int64_t down;                        // elements to the next row of this team
     int across;
-    __device__ __forceinline__ Walk(T* base, int64_t ld, uint32_t row, uint32_t stride, int col, int size)
-        : at(base ? base + (int64_t)row * ld + col : nullptr), down((int64_t)stride * ld), across(size * kGroup) {}
+    __device__ __forceinline__ Walk(T* base, int64_t ld, uint32_t row, uint32_t stride, int col, int across_)
+        : at(base ? base + (int64_t)row * ld + col : nullptr), down((int64_t)stride * ld), across(across_) {}
     __device__ __forceinline__ T* group(int j) const { return at + j * across; }
     __device__ __forceinline__ void next() { at += down; }
 };
 
-// The ring of a CTA.  A stage holds, for each matrix, group and piece, a run of 16 bytes for every thread.
-template <int kThreads, int kAll>
+// The ring of a CTA.  A stage holds, for each matrix and group, a run of kC elements for every thread; kBytes: of a thread in a stage.
+template <int kThreads, int kBytes>
 struct Ring {
-    static constexpr uint32_t kRun = kThreads * 16u;
-    const char* mine;                    // this thread's place in the first run of the first stage, and the same as a shared address
-    uint32_t at;
+    static constexpr uint32_t kStage = kThreads * (uint32_t)kBytes;
+    const char* base;
+    uint32_t at;                         // the same as a shared address
     uint32_t now, fill, end;             // the row's stage, the one that is filled meanwhile, behind the last: offsets
     int ahead;                           // stages that may still be under way
-    __device__ __forceinline__ Ring(const char* base, int stages)
-        : mine(base + threadIdx.x * 16u), at((uint32_t)__cvta_generic_to_shared(base) + threadIdx.x * 16u), now(0), fill((uint32_t)(stages - 1) * kAll * kRun),
-          end((uint32_t)stages * kAll * kRun), ahead(stages - 1) {}
-    __device__ __forceinline__ uint32_t target(uint32_t stage, int run) const { return at + stage + (uint32_t)run * kRun; }
-    template <typename T>
-    __device__ __forceinline__ void read(int run, Raw8<T, 16>& raw) const {
-#pragma unroll
-        for (int i = 0; i < Raw8<T, 16>::kPieces; ++i) raw.piece[i] = *reinterpret_cast<const uint4*>(mine + now + (uint32_t)(run + i) * kRun);
-    }
+    __device__ __forceinline__ Ring(const char* base_, int stages)
+        : base(base_), at((uint32_t)__cvta_generic_to_shared(base_)), now(0), fill((uint32_t)(stages - 1) * kStage), end((uint32_t)stages * kStage), ahead(stages - 1) {}
+    // Where a thread's group lies in a stage: `before` bytes a thread of runs before it, `bytes` of it.
+    static __device__ __forceinline__ uint32_t offset(int before, int bytes) { return kThreads * (uint32_t)before + threadIdx.x * (uint32_t)bytes; }
+    __device__ __forceinline__ uint32_t target(uint32_t stage, int before, int bytes) const { return at + stage + offset(before, bytes); }
+    template <typename R>
+    __device__ __forceinline__ void read(int before, R& raw) const { raw.piece[0] = *reinterpret_cast<const typename R::P*>(base + now + offset(before, (int)sizeof(typename R::P))); }
     static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     // Waits for the row's stage.
     __device__ __forceinline__ void wait() const {
@@ -189,30 +180,37 @@ struct Ring {
     }
     __device__ __forceinline__ void next() {
         fill = now;
-        now += kAll * kRun;
+        now += kStage;
         if (now == end) now = 0;
     }
 };
 
-// Parameters and sums of the places in shared memory: the first halves of all groups, then the second ones, so that
+// Parameters and sums of the places in shared memory: the first four columns of all groups, then the next four, so that
 // consecutive threads' 16-byte accesses are consecutive.
-__device__ __forceinline__ int at_place(int places, int place, int k) { return ((k >> 2) * places + place) * 4 + (k & 3); }
-__device__ __forceinline__ void read_place(const float* s, int places, int place, Eight& v) {
-    const ulonglong2 a = reinterpret_cast<const ulonglong2*>(s)[place], b = reinterpret_cast<const ulonglong2*>(s)[places + place];
-    v.p[0] = a.x, v.p[1] = a.y, v.p[2] = b.x, v.p[3] = b.y;
+template <int kC>
+__device__ __forceinline__ int at_place(int places, int i) { return kC == 4 ? i : (((i >> 2) & 1) * places + (i >> 3)) * 4 + (i & 3); }
+template <int kC>
+__device__ __forceinline__ void read_place(const float* s, int places, int place, Cols<kC>& v) {
+#pragma unroll
+    for (int i = 0; i < kC / 4; ++i) {
+        const ulonglong2 a = reinterpret_cast<const ulonglong2*>(s)[i * places + place];
+        v.p[2 * i] = a.x, v.p[2 * i + 1] = a.y;
+    }
 }
-__device__ __forceinline__ void write_place(float* s, int places, int place, const Eight& v) {
-    reinterpret_cast<ulonglong2*>(s)[place] = make_ulonglong2(v.p[0], v.p[1]);
-    reinterpret_cast<ulonglong2*>(s)[places + place] = make_ulonglong2(v.p[2], v.p[3]);
+template <int kC>
+__device__ __forceinline__ void write_place(float* s, int places, int place, const Cols<kC>& v) {
+#pragma unroll
+    for (int i = 0; i < kC / 4; ++i) reinterpret_cast<ulonglong2*>(s)[i * places + place] = make_ulonglong2(v.p[2 * i], v.p[2 * i + 1]);
 }
 __device__ __forceinline__ float param(const void* p, int type, int i) {
     return type == DEFT_F32 ? static_cast<const float*>(p)[i]
                             : (type == DEFT_BF16 ? to_f32(static_cast<const __nv_bfloat16*>(p)[i]) : to_f32(static_cast<const __half*>(p)[i]));
 }
+template <int kC>
 __device__ __forceinline__ void fill_places(float* s, const void* p, int type, int cols, int places, int shift, float otherwise) {
-    for (int i = threadIdx.x; i < places * kGroup; i += blockDim.x) {
+    for (int i = threadIdx.x; i < places * kC; i += blockDim.x) {
         const int c = i - shift;
-        s[at_place(places, i >> 3, i & 7)] = p && c >= 0 && c < cols ? param(p, type, c) : otherwise;
+        s[at_place<kC>(places, i)] = p && c >= 0 && c < cols ? param(p, type, c) : otherwise;
     }
 }
 
@@ -222,14 +220,14 @@ struct Team {
     uint32_t row, stride;                // first row, distance to the next
     int shift;
     float2* slots;                       // [2][warps of the CTA]
-    __device__ __forceinline__ Team(const TeamShape& s, float2* slots_) : size(s.size), turn(0), slots(slots_) {
+    __device__ __forceinline__ Team(const TeamShape& s, int len, float2* slots_) : size(s.size), turn(0), slots(slots_) {
         team = (int)threadIdx.x / size;
         at = (int)threadIdx.x - team * size;
         teams = (int)blockDim.x / size;
         const uint32_t step = (uint32_t)s.step, same = blockIdx.x / step, rest = blockIdx.x - same * step;
         row = (same * teams + team) * step + rest;
         stride = gridDim.x * teams;      // (CTAs of a shift) x teams x step
-        shift = (int)((uint32_t)s.first + rest * (uint32_t)s.ld) & 7;
+        shift = (int)((uint32_t)s.first + rest * (uint32_t)s.ld) & (len - 1);
     }
     // The sums of a and b over the team.  All threads of a CTA call it equally often.
     __device__ __forceinline__ float2 sum(float a, float b) {
@@ -261,13 +259,15 @@ struct Team {
     }
 };
 
-template <typename F>
-deft_status with_groups(int groups, F&& f) {
-    switch (groups) {
-        case 1: return f(AlignTag<1>{});
-        case 2: return f(AlignTag<2>{});
-        default: return f(AlignTag<4>{});
-    }
+// Calls f with the number of groups of a thread and the threads of a CTA as constants (a ring of short rows; its long ones; other feeds).
+template <int kC, typename F>
+deft_status with_shape(const TeamShape& s, F&& f) {
+    if (s.feed == Feed::kElements) return f(FeedTag<Feed::kElements>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
+    if (s.feed == Feed::kLoads) return f(FeedTag<Feed::kLoads>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
+    if (s.threads > kTeamThreads) return f(FeedTag<Feed::kRing>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
+    if (s.groups * kC == 32) return f(FeedTag<Feed::kRing>{}, AlignTag<32 / kC>{}, AlignTag<kTeamThreads>{});
+    if (s.groups * kC == 16) return f(FeedTag<Feed::kRing>{}, AlignTag<16 / kC>{}, AlignTag<kTeamThreads>{});
+    return f(FeedTag<Feed::kRing>{}, AlignTag<8 / kC>{}, AlignTag<kTeamThreads>{});
 }
 
 }  // namespace deft

@@ -51,54 +51,54 @@ template <> __device__ __forceinline__ uint32_t narrowed<__half>(uint64_t p) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Eight numbers as four pairs.
-struct Eight {
-    uint64_t p[4];
-    template <typename T, int kAlign>
-    __device__ __forceinline__ void from(const Raw8<T, kAlign>& raw) {
-        if constexpr (kAlign == 16 && sizeof(T) == 2) {
-            p[0] = widened<T>(raw.piece[0].x), p[1] = widened<T>(raw.piece[0].y), p[2] = widened<T>(raw.piece[0].z), p[3] = widened<T>(raw.piece[0].w);
-        } else if constexpr (kAlign == 16) {
+// kC consecutive elements as they lie in memory: in one piece of up to 16 bytes (kWhole), or one by one.
+template <typename T, int kC, bool kWhole>
+struct RawCols {
+    static constexpr int kPiece = kWhole ? kC * (int)sizeof(T) : (int)sizeof(T), kPieces = kC * (int)sizeof(T) / kPiece, kPer = kC / kPieces;
+    using P = typename Piece<kPiece>::type;
+    P piece[kPieces];
+};
+// kC numbers as pairs.
+template <int kC>
+struct Cols {
+    static constexpr int kPairs = kC / 2;
+    uint64_t p[kPairs];
+    template <typename T, bool kWhole>
+    __device__ __forceinline__ void from(const RawCols<T, kC, kWhole>& raw) {
+        if constexpr (kWhole && sizeof(T) == 2) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(raw.piece);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                p[2 * i] = pair(__uint_as_float(raw.piece[i].x), __uint_as_float(raw.piece[i].y));
-                p[2 * i + 1] = pair(__uint_as_float(raw.piece[i].z), __uint_as_float(raw.piece[i].w));
-            }
+            for (int i = 0; i < kPairs; ++i) p[i] = widened<T>(w[i]);
         } else {
-            float v[kGroup];
-            raw.unpack(v);
+            const T* e = reinterpret_cast<const T*>(raw.piece);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = pair(v[2 * i], v[2 * i + 1]);
+            for (int i = 0; i < kPairs; ++i) p[i] = pair(to_f32(e[2 * i]), to_f32(e[2 * i + 1]));
         }
     }
-    template <typename T, int kAlign>
-    __device__ __forceinline__ void to(Raw8<T, kAlign>& raw) const {
-        if constexpr (kAlign == 16 && sizeof(T) == 2) {
-            raw.piece[0] = make_uint4(narrowed<T>(p[0]), narrowed<T>(p[1]), narrowed<T>(p[2]), narrowed<T>(p[3]));
-        } else if constexpr (kAlign == 16) {
+    template <typename T, bool kWhole>
+    __device__ __forceinline__ void to(RawCols<T, kC, kWhole>& raw) const {
+        if constexpr (kWhole && sizeof(T) == 2) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(raw.piece);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 u = unpair(p[2 * i]), v = unpair(p[2 * i + 1]);
-                raw.piece[i] = make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(v.x), __float_as_uint(v.y));
-            }
+            for (int i = 0; i < kPairs; ++i) w[i] = narrowed<T>(p[i]);
         } else {
+            T* e = reinterpret_cast<T*>(raw.piece);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < kPairs; ++i) {
                 const float2 v = unpair(p[i]);
-                reinterpret_cast<T*>(raw.piece)[2 * i] = from_f32<T>(v.x);
-                reinterpret_cast<T*>(raw.piece)[2 * i + 1] = from_f32<T>(v.y);
+                e[2 * i] = from_f32<T>(v.x);
+                e[2 * i + 1] = from_f32<T>(v.y);
             }
         }
     }
     // Elements outside lo .. hi become zero.
     __device__ __forceinline__ void trim(int lo, int hi) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kPairs; ++i) {
             const float2 v = unpair(p[i]);
             p[i] = pair(2 * i >= lo && 2 * i < hi ? v.x : 0.0f, 2 * i + 1 >= lo && 2 * i + 1 < hi ? v.y : 0.0f);
         }
     }
-    __device__ __forceinline__ uint64_t sum() const { return add2(add2(p[0], p[1]), add2(p[2], p[3])); }
 };
 __device__ __forceinline__ float folded(uint64_t p) {
     const float2 v = unpair(p);
