@@ -11,7 +11,7 @@ namespace {
 template <typename TX, typename TY> constexpr int kColsOf = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
 
 template <bool kAdd, typename TX, typename TY, Feed kFeed, int kGroups, int kThreads>
-__global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TX, TY> < 32 ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
+__global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma, beta, the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
     constexpr int kC = kColsOf<TX, TY>;

@@ -13,7 +13,7 @@ constexpr int kPartials = 2 * 148;   // CTAs that leave partial sums at most; a 
 template <typename TD, typename TX> constexpr int kColsOf = sizeof(TD) == 4 || sizeof(TX) == 4 ? 4 : 8;
 
 template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads>
-__global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TD, TX> < 32 ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
+__global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma and room for a second vector (at the end the CTA's sums), the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
     constexpr int kC = kColsOf<TD, TX>;
@@ -143,10 +143,25 @@ __global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TD, TX> < 32 ? 2 :
         }
     }
     if (!a.dgamma && !a.dbeta) return;
-    // the teams' sums in order
-    for (int t = 0; t < team.teams; ++t) {
+    // a warp's teams, then the teams or warps in order
+    int units = team.teams, unit = team.team;
+    bool first = true;
+    if (team.size < 32) {
+        for (int o = team.size; o < 32; o *= 2)
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                for (int i = 0; i < kC / 2; ++i) {
+                    dg[j].p[i] = add2(dg[j].p[i], __shfl_xor_sync(0xffffffffu, dg[j].p[i], o));
+                    db[j].p[i] = add2(db[j].p[i], __shfl_xor_sync(0xffffffffu, db[j].p[i], o));
+                }
+        units = (int)blockDim.x >> 5;
+        unit = (int)threadIdx.x >> 5;
+        first = ((int)threadIdx.x & 31) < team.size;
+    }
+    for (int t = 0; t < units; ++t) {
         __syncthreads();
-        if (t != team.team) continue;
+        if (t != unit || !first) continue;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
             const int place = team.at + j * team.size;
@@ -174,8 +189,8 @@ __global__ void __launch_bounds__(kThreads, kGroups * kColsOf<TD, TX> < 32 ? 2 :
     }
 }
 
-// The CTAs' partial sums added up: a lane per column, eight warps that take every eighth CTA's.
-constexpr int kJoinWarps = 8;
+// The CTAs' partial sums added up: a lane per column, sixteen warps that take every sixteenth CTA's.
+constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(kJoinWarps * 32) k_layer_norm_join(const __grid_constant__ LayerNormGradArgs a, const int partials) {
     __shared__ float part[kJoinWarps][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -183,7 +198,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_layer_norm_join(const __gri
     const int64_t both = 2 * (int64_t)a.cols, at = (int64_t)blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (at < both) {
-#pragma unroll 4
+#pragma unroll 8
         for (int p = warp; p < partials; p += kJoinWarps) sum += a.partial[p * both + at];
     }
     part[warp][lane] = sum;

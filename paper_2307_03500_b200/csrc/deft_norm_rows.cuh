@@ -52,7 +52,8 @@ struct Shifts {
 
 // row_bytes: bytes of a column of all matrices that are read; params: fp32 vectors of the row's length in shared memory; per_sm:
 // CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
-// Rows of up to 4096 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32.
+// Rows of up to 8192 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32; from 4096
+// columns on a CTA has a row at a time and an SM one CTA, whose parameters and ring fill its shared memory.
 inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks) {
     TeamShape s{};
     bool shifted = m.ok;
@@ -69,24 +70,24 @@ inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_byt
         shifted = false;
         place();
     }
-    const bool wide = s.places * len > kTeamThreads * 16;
-    if (wide) per_sm = s.places * len <= kTeamThreads * 32 ? 2 : 1;
-    const int most = (wide ? 32 : 16) / len;
+    const bool large = s.places * len > kTeamThreads * 16;
+    if (large) per_sm = 1;
+    const int most = (s.places * len > kTeamMost * 16 ? 32 : 16) / len, need = (s.places + most - 1) / most;
     s.size = 4;
-    while (s.size < kTeamMost && s.size * most < s.places) s.size *= 2;
+    while (s.size < 32 && s.size < need) s.size *= 2;
+    if (need > 32) s.size = large ? kTeamMost : (need + 31) / 32 * 32;
     // few rows: more threads for each, so that all SMs' schedulers have work
-    while (s.size < kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
-    s.groups = wide || s.size * (most / 2) < s.places ? most : most / 2;
-    s.threads = s.size > kTeamThreads ? s.size : kTeamThreads;
+    while (s.size * 2 <= kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
+    s.groups = large || s.size * (most / 2) < s.places ? most : most / 2;
+    s.threads = s.size > kTeamThreads ? s.size : kTeamThreads / s.size * s.size;
     if (most_blocks == 0) most_blocks = (int64_t)sm_count() * per_sm;
     const int64_t teams = s.threads / s.size, needed = ((rows + s.step - 1) / s.step + teams - 1) / teams;   // CTAs for the rows of a shift
-    const int64_t most_each = most_blocks / s.step;
-    s.blocks = (unsigned)((needed < most_each ? needed : most_each) * s.step);
+    const int64_t most_each = most_blocks / s.step, turns = (needed + most_each - 1) / most_each;
+    s.blocks = (unsigned)((needed + turns - 1) / turns * s.step);      // (no more than take as many turns)
     // the ring: as many stages as a CTA's share of an SM's shared memory has room for, and as a team has rows
-    const size_t stage = (size_t)s.threads * s.groups * len * row_bytes;
+    const size_t stage = (size_t)(s.threads > kTeamThreads ? kTeamMost : kTeamThreads) * s.groups * len * row_bytes;
     s.smem = (size_t)params * sizeof(float) * (size_t)(s.places * len);
     const size_t share = (size_t)220 * 1024 / per_sm;
-    const int64_t turns = (needed * s.step + s.blocks - 1) / s.blocks;
     s.stages = share > s.smem ? (int)((share - s.smem) / stage) : 0;
     if (s.stages > kMostStages) s.stages = kMostStages;
     if (s.stages > turns) s.stages = (int)turns;
@@ -264,8 +265,8 @@ template <int kC, typename F>
 deft_status with_shape(const TeamShape& s, F&& f) {
     if (s.feed == Feed::kElements) return f(FeedTag<Feed::kElements>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
     if (s.feed == Feed::kLoads) return f(FeedTag<Feed::kLoads>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
-    if (s.threads > kTeamThreads) return f(FeedTag<Feed::kRing>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{});
-    if (s.groups * kC == 32) return f(FeedTag<Feed::kRing>{}, AlignTag<32 / kC>{}, AlignTag<kTeamThreads>{});
+    if (s.threads > kTeamThreads)
+        return s.groups * kC == 32 ? f(FeedTag<Feed::kRing>{}, AlignTag<32 / kC>{}, AlignTag<kTeamMost>{}) : f(FeedTag<Feed::kRing>{}, AlignTag<16 / kC>{}, AlignTag<kTeamMost>{});
     if (s.groups * kC == 16) return f(FeedTag<Feed::kRing>{}, AlignTag<16 / kC>{}, AlignTag<kTeamThreads>{});
     return f(FeedTag<Feed::kRing>{}, AlignTag<8 / kC>{}, AlignTag<kTeamThreads>{});
 }

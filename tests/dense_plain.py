@@ -57,9 +57,9 @@ def layer_norm_grad(dy, x, mean, rstd, gamma=None, add=None, scale=1.0):
     if add is not None:
         dx = dx + add.double().reshape(-1, n)
         tol = tol + U * 2 * dx.abs()
-    # rows one after the other in a thread, teams of a CTA, 37 CTAs in a warp's lane and eight warps
+    # rows one after the other in a thread, teams of a CTA, up to 37 CTAs in a warp's lane and sixteen warps
     rows = x.shape[0]
-    depth = 3 + rows // 296 + 1 + 64 + 37 + 8
+    depth = 3 + rows // 148 + 1 + 64 + 37 + 16
     return (dx, (dy * h).sum(0) * scale, dy.sum(0) * scale, tol, U * depth * abs(scale) * (dy * h).abs().sum(0),
             U * depth * abs(scale) * dy.abs().sum(0))
 
