@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotSmem = 32 * 1024;
+constexpr int kRotItems = 4;         // heads' vectors a thread takes, where there are tokens enough
 
 // kVec elements of a row, in pieces of up to 16 bytes, or (kSingle) one by one.
 template <typename T, int kVec, bool kSingle>
@@ -29,9 +30,10 @@ struct Vec {
     __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(piece)[i] = from_f32<T>(v); }
 };
 
+// A thread keeps its columns and its token, whose cosines and sines stay in registers, and goes through the heads.
 struct RotarySplit {
-    FastDiv units, heads, per_token;     // of a head: vectors of pairs, then vectors that are copied; heads; their product
-    int turned;                          // units of a head that are turned
+    FastDiv units, lanes;                // of a head: vectors of pairs, then vectors that are copied; heads taken side by side
+    int turned;                          // units that are turned
     int tokens;                          // of a CTA
 };
 
@@ -48,7 +50,8 @@ __device__ __forceinline__ float2 cos_sin(uint64_t turns) {
     return make_float2(quarter == 1 || quarter == 2 ? -cc : cc, quarter == 2 || quarter == 3 ? -ss : ss);
 }
 
-template <typename T, int kVec, bool kPairs, bool kSingle>
+// kAll: no columns are copied.
+template <typename T, int kVec, bool kPairs, bool kSingle, bool kAll>
 __global__ void __launch_bounds__(kRotThreads) k_rotary(const __grid_constant__ RotaryArgs a, const RotarySplit split, const FastDiv tokens) {
     extern __shared__ float2 table[];    // [tokens of the CTA][rot / 2]
     const int half = a.rot >> 1;
@@ -67,61 +70,54 @@ __global__ void __launch_bounds__(kRotThreads) k_rotary(const __grid_constant__ 
     __syncthreads();
     const T* x = static_cast<const T*>(a.x);
     T* y = static_cast<T*>(a.y);
-    const uint32_t items = (uint32_t)have * split.per_token.d;
-    for (uint32_t i = threadIdx.x; i < items; i += kRotThreads) {
-        const uint32_t k = split.per_token.div(i), in = i - k * split.per_token.d;
-        const uint32_t head = split.units.div(in), unit = in - head * split.units.d;
+    using V = Vec<T, kVec, kSingle>;
+    const uint32_t places = split.units.d * split.lanes.d * (uint32_t)have;
+    for (uint32_t i = threadIdx.x; i < places; i += kRotThreads) {
+        const uint32_t r = split.units.div(i), unit = i - r * split.units.d;
+        const uint32_t k = split.lanes.div(r), head = r - k * split.lanes.d;
         const uint32_t token = first + k, b = tokens.div(token), t = token - b * tokens.d;
-        const T* from = x + (int64_t)b * a.x_batch + (int64_t)t * a.x_token + (int64_t)head * a.x_head;
-        T* to = y + (int64_t)b * a.y_batch + (int64_t)t * a.y_token + (int64_t)head * a.y_head;
-        const float2* cs = table + k * half;
-        Vec<T, kVec, kSingle> u, v;
-        if ((int)unit >= split.turned) {
-            const int c = a.rot + ((int)unit - split.turned) * kVec;
-            if (!kSingle || c + kVec <= a.dim) {
-                u.load(from + c);
-                u.store(to + c);
-            } else {
-                for (int e = c; e < a.dim; ++e) to[e] = from[e];
-            }
-        } else if (kPairs) {
-            const int c = (int)unit * kVec;
-            u.load(from + c);
+        const bool turned = kAll || (int)unit < split.turned;
+        const int c = turned ? (int)unit * kVec : a.rot + ((int)unit - split.turned) * kVec;
+        const T* from = x + (int64_t)b * a.x_batch + (int64_t)t * a.x_token + (int64_t)head * a.x_head + c;
+        T* to = y + (int64_t)b * a.y_batch + (int64_t)t * a.y_token + (int64_t)head * a.y_head + c;
+        const int64_t down_x = (int64_t)split.lanes.d * a.x_head, down_y = (int64_t)split.lanes.d * a.y_head;
+        const bool odd = !kAll && kSingle && c + kVec > a.dim;                    // the last one of an odd head
+        constexpr int kTurns = kPairs ? kVec / 2 : kVec;
+        float2 w[kTurns];
+        if (turned) {
 #pragma unroll
-            for (int e = 0; e < kVec; e += 2) {
-                const float2 w = cs[(c + e) >> 1];
-                const float p = u.get(e), q = u.get(e + 1);
-                v.set(e, p * w.x - q * w.y);
-                v.set(e + 1, p * w.y + q * w.x);
+            for (int e = 0; e < kTurns; ++e) w[e] = table[k * half + (kPairs ? c / 2 : c) + e];
+        }
+        for (int h = (int)head; h < a.heads; h += (int)split.lanes.d, from += down_x, to += down_y) {
+            V u, v;
+            if (odd) {
+                to[0] = from[0];
+                continue;
             }
-            v.store(to + c);
-        } else {
-            const int c = (int)unit * kVec;
-            u.load(from + c);
-            v.load(from + half + c);
+            u.load(from);
+            if (!kPairs && turned) v.load(from + half);
+            if (turned) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                const float2 w = cs[c + e];
-                const float p = u.get(e), q = v.get(e);
-                u.set(e, p * w.x - q * w.y);
-                v.set(e, p * w.y + q * w.x);
+                for (int e = 0; e < kTurns; ++e) {
+                    const float m = u.get(kPairs ? 2 * e : e), n = kPairs ? u.get(2 * e + 1) : v.get(e);
+                    u.set(kPairs ? 2 * e : e, m * w[e].x - n * w[e].y);
+                    (kPairs ? u : v).set(kPairs ? 2 * e + 1 : e, m * w[e].y + n * w[e].x);
+                }
+                if (!kPairs) v.store(to + half);
             }
-            u.store(to + c);
-            v.store(to + half + c);
+            u.store(to);
         }
     }
 }
 
-// Elements a thread takes at a time: as many as every head's row and the borders in it are aligned to (strides of dimensions
-// of one element are 0).
+// Elements a thread takes at a time: up to 16 bytes (two such pieces side by side would touch every sector twice), as every head's
+// row and the borders in it are aligned (strides of dimensions of one element are 0).
 inline int vec_of(const RotaryArgs& a, size_t elem) {
     const int64_t inner = (a.interleaved ? a.rot : a.rot / 2) | a.dim;
     const int64_t strides = a.x_head | a.x_token | a.x_batch | a.y_head | a.y_token | a.y_batch;
     const uint64_t bytes = (uint64_t)((inner | strides) * (int64_t)elem) | reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y);
-    for (int v = 8; v > 1; v /= 2) {
-        const size_t piece = v * elem < 16 ? v * elem : 16;
-        if ((inner & (v - 1)) == 0 && (bytes & (piece - 1)) == 0) return v;
-    }
+    for (int v = (int)(16 / elem); v > 1; v /= 2)
+        if ((bytes & (v * elem - 1)) == 0) return v;
     return 1;
 }
 
@@ -136,34 +132,45 @@ deft_status launch_rotary(const RotaryArgs& a, int type, cudaStream_t stream) {
     const int64_t units = s.turned + (a.x == a.y ? 0 : (a.dim - a.rot + step - 1) / step);
     const int64_t all = a.batch * a.tokens;
     const int64_t per_token = units * a.heads;
-    int64_t tokens = (4 * kRotThreads + per_token - 1) / per_token;
+    int64_t tokens = (kRotItems * kRotThreads + per_token - 1) / per_token;
     const int64_t fit = kRotSmem / ((int64_t)half * (int64_t)sizeof(float2));
     if (tokens > fit) tokens = fit;
     if (tokens > all) tokens = all;
     while (tokens > 1 && (all + tokens - 1) / tokens < 2 * 148) tokens = (tokens + 1) / 2;
+    int64_t lanes = kRotThreads / (units * tokens);
+    if (lanes > a.heads) lanes = a.heads;
+    if (lanes < 1) lanes = 1;
     s.tokens = (int)tokens;
     s.units = fast_div((uint32_t)units);
-    s.heads = fast_div((uint32_t)a.heads);
-    s.per_token = fast_div((uint32_t)per_token);
+    s.lanes = fast_div((uint32_t)lanes);
     const unsigned blocks = (unsigned)((all + tokens - 1) / tokens);
     const size_t smem = (size_t)tokens * half * sizeof(float2);
     const FastDiv t = fast_div((uint32_t)a.tokens);
     return with_type(type, [&](auto e) -> deft_status {
         using T = decltype(e);
-        auto run = [&](auto kernel) { kernel<<<blocks, kRotThreads, smem, stream>>>(a, s, t); };
+        auto run = [&](auto vecs, auto pairs, auto single) {
+            constexpr int kVec = decltype(vecs)::value;
+            constexpr bool kPairs = decltype(pairs)::value, kSingle = decltype(single)::value;
+            auto kernel = units == s.turned ? k_rotary<T, kVec, kPairs, kSingle, true> : k_rotary<T, kVec, kPairs, kSingle, false>;
+            kernel<<<blocks, kRotThreads, smem, stream>>>(a, s, t);
+        };
         if (a.interleaved) {
             switch (vec) {
-                case 8: run(k_rotary<T, 8, true, false>); break;
-                case 4: run(k_rotary<T, 4, true, false>); break;
-                case 2: run(k_rotary<T, 2, true, false>); break;
-                default: run(k_rotary<T, 2, true, true>); break;
+                case 8:
+                    if constexpr (sizeof(T) == 2) run(AlignTag<8>{}, AlignTag<1>{}, AlignTag<0>{});
+                    break;
+                case 4: run(AlignTag<4>{}, AlignTag<1>{}, AlignTag<0>{}); break;
+                case 2: run(AlignTag<2>{}, AlignTag<1>{}, AlignTag<0>{}); break;
+                default: run(AlignTag<2>{}, AlignTag<1>{}, AlignTag<1>{}); break;
             }
         } else {
             switch (vec) {
-                case 8: run(k_rotary<T, 8, false, false>); break;
-                case 4: run(k_rotary<T, 4, false, false>); break;
-                case 2: run(k_rotary<T, 2, false, false>); break;
-                default: run(k_rotary<T, 1, false, true>); break;
+                case 8:
+                    if constexpr (sizeof(T) == 2) run(AlignTag<8>{}, AlignTag<0>{}, AlignTag<0>{});
+                    break;
+                case 4: run(AlignTag<4>{}, AlignTag<0>{}, AlignTag<0>{}); break;
+                case 2: run(AlignTag<2>{}, AlignTag<0>{}, AlignTag<0>{}); break;
+                default: run(AlignTag<1>{}, AlignTag<0>{}, AlignTag<1>{}); break;
             }
         }
         DEFT_CUDA_TRY(cudaGetLastError());

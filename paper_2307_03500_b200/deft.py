@@ -797,43 +797,54 @@ ROTARY_MAX_ROT = 4096
 _ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 
+_FLOAT = None                      # torch.float32, once torch is there
+
+
 def _vector(t, name: str, count: int, dtype=None) -> Optional[int]:
     """The pointer of a contiguous vector of `count` elements (None: not given); fp32 unless dtype says otherwise."""
     if t is None:
         return None
     if dtype is None:
-        import torch
-        dtype = torch.float32
-    if t.numel() != count or not t.is_contiguous() or t.dtype != dtype:
+        dtype = _FLOAT or _float()
+    if t.numel() != count or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError("%s: a contiguous %s tensor of %d elements expected" % (name, dtype, count))
     return t.data_ptr()
 
 
-def _like(t, name: str, shape, dtype) -> Tuple[Optional[int], int]:
+def _float():
+    global _FLOAT
+    import torch
+    _FLOAT = torch.float32
+    return _FLOAT
+
+
+def _like(t, name: str, shape, dtype, cols: int) -> Tuple[Optional[int], int]:
     """Pointer and pitch of a matrix of a given shape and type (None: not given)."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError("%s: a %s tensor of %s expected" % (name, dtype, tuple(shape)))
-    return t.data_ptr(), _matrix(t, name)[2]
+    return t.data_ptr(), cols if t.is_contiguous() else _matrix(t, name)[2]
 
 
 def _weights(gamma, beta, cols: int) -> Tuple[Optional[int], Optional[int], int]:
     first = gamma if gamma is not None else beta
     if first is None:
         return None, None, F32
-    return _vector(gamma, "gamma", cols, first.dtype), _vector(beta, "beta", cols, first.dtype), _type(first)
+    dtype = first.dtype
+    return _vector(gamma, "gamma", cols, dtype), _vector(beta, "beta", cols, dtype), _type(first)
 
 
 def deft_layer_norm(x, y, gamma=None, beta=None, eps: float = 1e-5, add=None, sum=None, mean=None, rstd=None, stream=None) -> None:
     """y = layer norm of the rows (the last dimension) of x + add; the sum goes to `sum`, the statistics that the
     gradient needs to mean and rstd (fp32, one number per row)."""
     rows, cols, ld_x = _matrix(x, "x")
-    if y.shape != x.shape:
+    shape, dtype = x.shape, x.dtype
+    if y.shape != shape:
         raise ValueError("x and y disagree")
-    ld_y = _matrix(y, "y")[2]
-    p_add, ld_add = _like(add, "add", x.shape, x.dtype)
-    p_sum, ld_sum = _like(sum, "sum", x.shape, x.dtype)
+    ld_y = cols if y.is_contiguous() else _matrix(y, "y")[2]
+    p_add, ld_add = _like(add, "add", shape, dtype, cols)
+    p_sum, ld_sum = _like(sum, "sum", shape, dtype, cols)
     p_gamma, p_beta, w_type = _weights(gamma, beta, cols)
     dev = _device(y, x, add, sum, gamma, beta, mean, rstd)
     _call("deft_layer_norm", dev, stream, x.data_ptr(), _type(x), ld_x, p_add, ld_add, p_sum, ld_sum, p_gamma, p_beta, w_type, y.data_ptr(),
@@ -859,11 +870,12 @@ def deft_layer_norm_grad(grad_out, x, mean, rstd, grad_x=None, gamma=None, add=N
     gamma and beta into grad_gamma and grad_beta, fp32 vectors (usually views of the flat gradient vector or of the
     residual), written, or with accumulate added to.  What is None is not computed."""
     rows, cols, ld_x = _matrix(x, "x")
-    if grad_out.shape != x.shape:
+    shape, dtype = x.shape, x.dtype
+    if grad_out.shape != shape:
         raise ValueError("grad_out and x disagree")
-    ld_go = _matrix(grad_out, "grad_out")[2]
-    p_add, ld_add = _like(add, "add", x.shape, x.dtype)
-    p_gx, ld_gx = _like(grad_x, "grad_x", x.shape, x.dtype)
+    ld_go = cols if grad_out.is_contiguous() else _matrix(grad_out, "grad_out")[2]
+    p_add, ld_add = _like(add, "add", shape, dtype, cols)
+    p_gx, ld_gx = _like(grad_x, "grad_x", shape, dtype, cols)
     p_gamma, _, w_type = _weights(gamma, None, cols)
     if ws is not None and not ws.is_contiguous():
         raise ValueError("ws: a contiguous tensor")
@@ -894,12 +906,19 @@ _Strides = ctypes.c_int64 * 3
 
 def _heads(t, name: str):
     """(batch, tokens, heads, dim) and the strides of a [batch, tokens, heads, dim] or [tokens, heads, dim] tensor."""
-    if t.dim() not in (3, 4):
+    strides = t.stride()
+    if len(strides) == 4:
+        b, n, h, d = t.shape
+        sb, sn, sh, sd = strides
+    elif len(strides) == 3:
+        b, sb = 1, 0
+        n, h, d = t.shape
+        sn, sh, sd = strides
+    else:
         raise ValueError("%s: a [batch, tokens, heads, dim] or [tokens, heads, dim] tensor" % name)
-    if t.size(-1) > 1 and t.stride(-1) != 1:
+    if sd != 1 and d > 1:
         raise ValueError("%s: the columns of a head must be contiguous" % name)
-    shape, strides = tuple(t.shape), t.stride()
-    return ((1,) + shape, _Strides(0, *strides[:2])) if t.dim() == 3 else (shape, _Strides(*strides[:3]))
+    return b, n, h, d, _Strides(sb, sn, sh)
 
 
 def deft_rotary(x, y, turns, positions=None, interleaved: bool = False, inverse: bool = False, gain: float = 1.0, stream=None) -> None:
@@ -907,21 +926,20 @@ def deft_rotary(x, y, turns, positions=None, interleaved: bool = False, inverse:
     strides of the first ones) turned by position times frequency; the others are copied.  y may be x.  turns:
     deft_rotary_frequencies on the device.  positions: int64 or int32, one per token (None: its number in its sequence).  inverse: the
     gradient with respect to x of the same call, applied to the gradient of y."""
-    import torch
-    shape, xs = _heads(x, "x")
-    if y.shape != x.shape or y.dtype != x.dtype:
+    batch, tokens, heads, dim, xs = _heads(x, "x")
+    if y.shape != x.shape or y.dtype is not x.dtype:
         raise ValueError("x and y disagree")
-    ys = _heads(y, "y")[1]
-    if turns.dim() != 1 or not turns.is_contiguous() or turns.dtype not in (torch.int64, torch.uint64):
+    ys = _heads(y, "y")[4]
+    if turns.dim() != 1 or turns.element_size() != 8 or turns.is_floating_point() or turns.is_complex() or not turns.is_contiguous():
         raise ValueError("turns: a contiguous vector of 64-bit integers")
-    pos_bytes = 0
+    p_pos, pos_bytes = None, 0
     if positions is not None:
         if positions.shape != x.shape[:-2]:
             raise ValueError("positions: one for each token expected")
-        pos_bytes = _ids(positions)
+        p_pos, pos_bytes = positions.data_ptr(), _ids(positions)
     dev = _device(y, x, turns, positions)
-    _call("deft_rotary", dev, stream, x.data_ptr(), xs, y.data_ptr(), ys, _type(x), shape[0], shape[1], shape[2], shape[3], turns.data_ptr(),
-          2 * turns.numel(), 1 if interleaved else 0, 1 if inverse else 0, gain, None if positions is None else positions.data_ptr(), pos_bytes)
+    _call("deft_rotary", dev, stream, x.data_ptr(), xs, y.data_ptr(), ys, _type(x), batch, tokens, heads, dim, turns.data_ptr(), 2 * turns.numel(),
+          1 if interleaved else 0, 1 if inverse else 0, gain, p_pos, pos_bytes)
 
 
 def deft_distill(logits, top_ids, top_logits, loss=None, grad=None, teacher_lse=None, temperature: float = 1.0, weight=None, scale: float = 1.0,
@@ -931,14 +949,15 @@ def deft_distill(logits, top_ids, top_logits, loss=None, grad=None, teacher_lse=
     renormalised over them, or with teacher_lse (its own log-sum-exp at the temperature, one number per row) with one class for
     all other tokens.  weight: fp32, one number per row; rows of weight 0 are not read."""
     rows, vocab, ld = _matrix(logits, "logits")
-    if top_ids.shape != top_logits.shape or top_ids.dim() == 0 or top_ids.shape[:-1] != logits.shape[:-1]:
+    shape, ids_shape = logits.shape, top_ids.shape
+    if ids_shape != top_logits.shape or len(ids_shape) == 0 or ids_shape[:-1] != shape[:-1]:
         raise ValueError("logits, top_ids and top_logits disagree")
-    import torch
-    if top_ids.dtype not in (torch.int64, torch.int32):
+    if top_ids.is_floating_point() or top_ids.element_size() not in (4, 8) or not top_ids.is_signed() or top_ids.is_complex():
         raise ValueError("top_ids: an int64 or int32 tensor")
-    top, ld_ids = _matrix(top_ids, "top_ids")[1:]
-    ld_teacher = _matrix(top_logits, "top_logits")[2]
-    p_grad, ld_grad = _like(grad, "grad", logits.shape, logits.dtype)
+    top = ids_shape[-1]
+    ld_ids = top if top_ids.is_contiguous() else _matrix(top_ids, "top_ids")[2]
+    ld_teacher = top if top_logits.is_contiguous() else _matrix(top_logits, "top_logits")[2]
+    p_grad, ld_grad = _like(grad, "grad", shape, logits.dtype, vocab)
     dev = _device(logits, top_ids, top_logits, loss, grad, teacher_lse, weight)
     _call("deft_distill", dev, stream, logits.data_ptr(), _type(logits), ld, rows, vocab, top_ids.data_ptr(), top_ids.element_size(), ld_ids,
           top_logits.data_ptr(), _type(top_logits), ld_teacher, top, _vector(teacher_lse, "teacher_lse", rows), temperature,
