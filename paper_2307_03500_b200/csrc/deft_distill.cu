@@ -15,6 +15,7 @@ namespace deft {
 namespace {
 
 constexpr int kMostCluster = 8;
+constexpr int kEachThread = 128;          // elements a thread works on at most, where there are threads enough (700 x 33278 fp32: 64 took 30, 128 27 us)
 constexpr int kMostThreads = 512;         // that work on the row
 constexpr int kPartBytes = 52224;         // of a row, per CTA: four CTAs per SM
 
@@ -90,6 +91,12 @@ __device__ __forceinline__ float warp_max(float v) {
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Over groups of eight lanes.
+__device__ __forceinline__ float eight_sum(float v) {
+#pragma unroll
+    for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 // The sum of what the lanes hold (over groups of kLanes), relative to the largest logit among them.
@@ -280,8 +287,9 @@ __device__ __forceinline__ void write_grad(const Granule<T>* cells, int n, int b
     }
 }
 
-// Barriers of a CTA: among the warps that work on the row, between them and the last warp.
-enum { kLanded = 1, kTaken, kSummed, kFactors, kWritten };
+// Barriers of a CTA: between the warps that work on the row and the last one, and among the former.  (An SM has barriers for as many
+// CTAs only as their numbers allow: with three instead of five, small rows run 16 side by side, not ten.)
+enum { kSummed = 1, kFactors, kRow };
 template <int kId>
 __device__ __forceinline__ void bar_sync(int threads) {
     __syncwarp();
@@ -291,6 +299,11 @@ template <int kId>
 __device__ __forceinline__ void bar_arrive(int threads) {
     __syncwarp();
     asm volatile("bar.arrive %0, %1;" ::"n"(kId), "r"(threads) : "memory");
+}
+template <int kMost>
+__device__ __forceinline__ void bar_row(int threads) {
+    if (kMost == 32) __syncwarp();
+    else bar_sync<kRow>(threads);
 }
 __device__ __forceinline__ void cluster_arrive() {
     __syncwarp();
@@ -313,7 +326,7 @@ struct DistillShape {
 
 // kMost: threads that work on the row, at most; four CTAs of 256 fit an SM.
 template <typename T, int kMost>
-__global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(const __grid_constant__ DistillArgs a, const __grid_constant__ DistillShape shape) {
+__global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ? 4 : 1)) k_distill(const __grid_constant__ DistillArgs a, const __grid_constant__ DistillShape shape) {
     constexpr int kPer = Granule<T>::kPer;
     extern __shared__ __align__(16) char smem[];
     Granule<T>* const cells = reinterpret_cast<Granule<T>*>(smem);
@@ -341,9 +354,16 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(co
             return;
         }
         bar_sync<kSummed>(all_threads);
-        Sums s{};
-        if (lane < warps) s = warp_sums[lane];
-        s = joined<32>(s, a.c1, a.by);
+        Sums s = warp_sums[0];
+        if (warps > 8) {
+            s = Sums{};
+            if (lane < warps) s = warp_sums[lane];
+            s = joined<32>(s, a.c1, a.by);
+        } else if (warps > 1) {            // eight lanes, four times over
+            s = Sums{};
+            if ((lane & 7) < warps) s = warp_sums[lane & 7];
+            s = joined<8>(s, a.c1, a.by);
+        }
         if (ctas > 1) {
             cluster_wait();                // all CTAs run: their shared memory may be written
             if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&cta_sums[rank], lane) = s;
@@ -459,7 +479,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(co
     T* const e = reinterpret_cast<T*>(smem) - base;
     if (tid == 0)                          // what the first and last granule hold beside the row
         for (int c = base; c < 0; ++c) e[c] = lowest<T>();
-    bar_sync<kLanded>(threads);
+    bar_row<kMost>(threads);
     for (int c = max(a.vocab, base) + tid; c < base + n * kPer; c += threads) e[c] = lowest<T>();
     Sums s{};
     if (has_entries) {
@@ -487,7 +507,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(co
             if (col >= 0) s.entries.sum += exp2_fast(d * a.c1);
         }
     }
-    bar_sync<kTaken>(threads);
+    bar_row<kMost>(threads);
     // what the powers are relative to: the largest of a granule of every lane, which is seldom far from the largest of all
     float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
     bool careful = false;
@@ -509,9 +529,15 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(co
     }
     s.rest.sum = rest * off;
     if (has_entries) {
-        s.entries.sum = warp_sum(s.entries.sum);
-        s.cross = joined<32>(s.cross);
-        s.q = joined<32>(q_sum);
+        if (a.top <= 8) {                  // (lanes without an entry have nothing to join)
+            s.entries.sum = eight_sum(s.entries.sum);
+            s.cross = joined<8>(s.cross);
+            s.q = joined<8>(q_sum);
+        } else {
+            s.entries.sum = warp_sum(s.entries.sum);
+            s.cross = joined<32>(s.cross);
+            s.q = joined<32>(q_sum);
+        }
     }
     if (lane == 0) warp_sums[warp] = s;
     bar_arrive<kSummed>(all_threads);
@@ -526,7 +552,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 256 ? 4 : 1) k_distill(co
         const float k = rest == 0.0f ? 0.0f * f.A : (f.A * exp2_fast((s.rest.near - f.all) * a.c1) - f.B * exp2_fast((s.rest.near - f.rest) * a.c1)) * off;
         if (careful) write_grad<T, true>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
         else write_grad<T, false>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
-        bar_sync<kWritten>(threads);
+        bar_row<kMost>(threads);
         // the entries' own elements: the probabilities of a column's entries added in their order
         for (int j = tid; j < a.top; j += threads) {
             const int c = entry.col[j];
@@ -555,7 +581,7 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     s.ctas = (int)ctas;
     s.granules = (int)(((bytes + 15) / 16 + ctas - 1) / ctas);
     s.threads = 32;
-    while (s.threads < kMostThreads && s.granules > s.threads * 16) s.threads *= 2;
+    while (s.threads < kMostThreads && s.granules * (16 / elem) > s.threads * kEachThread) s.threads *= 2;
     s.smem = (size_t)s.granules * 16 + (size_t)a.top * kEntryBytes;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -570,7 +596,7 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     cfg.numAttrs = s.ctas > 1 ? 1 : 0;
     return with_type(type, [&](auto t) -> deft_status {
         using T = decltype(t);
-        auto kernel = s.threads > 256 ? k_distill<T, 512> : k_distill<T, 256>;
+        auto kernel = s.threads > 256 ? k_distill<T, 512> : (s.threads > 32 ? k_distill<T, 256> : k_distill<T, 32>);
         if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
         DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, s));
         return DEFT_OK;
