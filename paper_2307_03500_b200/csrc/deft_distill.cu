@@ -483,20 +483,33 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     for (int c = max(a.vocab, base) + tid; c < base + n * kPer; c += threads) e[c] = lowest<T>();
     Sums s{};
     if (has_entries) {
-        float most = -INFINITY;
         for (int j = tid; j < a.top; j += threads) {
             const int col = entry.col[j];
             if (col < 0) continue;
             float own = take(e + col);
             if (own == -INFINITY) {        // another entry of this column was first, or the logit is -inf
                 own = to_f32(z[col]);
-                if (own != -INFINITY) entry.col[j] = -3 - col;
                 twice = (int)row;
-            } else {
-                most = fmaxf(most, own);
             }
             entry.own[j] = own;
         }
+    }
+    bar_row<kMost>(threads);
+    if (has_entries) {
+        if (twice == (int)row) {           // of a column's entries the first one counts: who was first above is a matter of chance
+            for (int j = tid; j < a.top; j += threads) {
+                const int col = entry.col[j];
+                bool earlier = false;
+                for (int m = 0; m < j && col >= 0; ++m) {
+                    const int other = *reinterpret_cast<volatile int*>(entry.col + m);      // (may have become -3 - column meanwhile)
+                    earlier |= other == col || other == -3 - col;
+                }
+                if (earlier) entry.col[j] = -3 - col;
+            }
+        }
+        float most = -INFINITY;
+        for (int j = tid; j < a.top; j += threads)
+            if (entry.col[j] >= 0) most = fmaxf(most, entry.own[j]);
         most = warp_max(most);
         s.entries.near = most == -INFINITY ? 0.0f : most;
         for (int j = tid; j < a.top; j += threads) {
@@ -507,7 +520,6 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             if (col >= 0) s.entries.sum += exp2_fast(d * a.c1);
         }
     }
-    bar_row<kMost>(threads);
     // what the powers are relative to: the largest of a granule of every lane, which is seldom far from the largest of all
     float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
     bool careful = false;

@@ -159,7 +159,7 @@ deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cu
             m.add(a.y, a.ld_y, sizeof(TY));
             m.add(a.add, a.ld_add, sizeof(TX));
             m.add(a.sum, a.ld_sum, sizeof(TX));
-            const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 4, 0);
+            const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 4, 0, 0);
             return with_shape<kC>(s, [&](auto feed, auto groups, auto threads) -> deft_status {
                 constexpr Feed kFeed = decltype(feed)::value;
                 constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;

@@ -33,8 +33,10 @@ struct TeamShape {
     unsigned blocks;                     // a multiple of step
     Feed feed;
     int stages;                          // of the ring
+    bool joined;                         // the CTAs are one cluster (and join their sums themselves)
     size_t smem;
 };
+constexpr int kMostJoined = 8;           // CTAs of a cluster
 
 // The matrices of a call: how long a group is, and whether one shift serves all of them.
 struct Shifts {
@@ -54,7 +56,8 @@ struct Shifts {
 // CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
 // Rows of up to 8192 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32; from 4096
 // columns on a CTA has a row at a time and an SM one CTA, whose parameters and ring fill its shared memory.
-inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks) {
+// join_turns: the call is one cluster of up to kMostJoined CTAs where a team then takes no more rows than that (0: never).
+inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks, int join_turns) {
     TeamShape s{};
     bool shifted = m.ok;
     const int len = m.cols;
@@ -82,6 +85,8 @@ inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_byt
     s.threads = s.size > kTeamThreads ? s.size : kTeamThreads / s.size * s.size;
     if (most_blocks == 0) most_blocks = (int64_t)sm_count() * per_sm;
     const int64_t teams = s.threads / s.size, needed = ((rows + s.step - 1) / s.step + teams - 1) / teams;   // CTAs for the rows of a shift
+    s.joined = needed * s.step <= (int64_t)kMostJoined * join_turns;
+    if (s.joined) most_blocks = kMostJoined;
     const int64_t most_each = most_blocks / s.step, turns = (needed + most_each - 1) / most_each;
     s.blocks = (unsigned)((needed + turns - 1) / turns * s.step);      // (no more than take as many turns)
     // the ring: as many stages as a CTA's share of an SM's shared memory has room for, and as a team has rows

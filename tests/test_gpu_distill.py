@@ -110,6 +110,19 @@ def test_missing_and_repeated_entries(tail, dtype):
     assert torch.equal(again[0][1], again[1][1]) and torch.equal(again[0][0], again[1][0]), "other bits"
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_repeated_entries_of_many_threads(dtype):
+    """Which of a column's entries counts is no matter of chance: the same bits on every call, in one CTA and in a cluster."""
+    for vocab in (5000, 60000):
+        z, ids, teacher, lse = _inputs(40, vocab, 400, dtype)
+        ids = ids[:, torch.randint(0, 150, (400,), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")].contiguous()
+        first = _check(z, ids, teacher, lse + 3.0)
+        for _ in range(10):
+            loss, grad = torch.empty_like(first[0]), torch.empty_like(z)
+            deft.deft_distill(z, ids, teacher, loss=loss, grad=grad, teacher_lse=lse + 3.0)
+            assert torch.equal(loss, first[0]) and torch.equal(grad, first[1]), "other bits"
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32, F16])
 @pytest.mark.parametrize("tail", [False, True])
 def test_masked_vocabulary(dtype, tail):

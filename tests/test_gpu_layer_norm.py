@@ -41,7 +41,7 @@ def _forward(x, y_dtype, add=None, gamma=None, beta=None, eps=1e-5, keep_sum=Tru
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (3, 2), (1, 7), (5, 8), (2, 31), (9, 64), (17, 100), (33, 250), (64, 256), (700, 257), (5, 1000), (300, 1024),
-                                       (37, 1027), (20, 1500), (3000, 48), (11, 2049), (4, 4099), (3, 8184), (3, 8192), (2, 16381), (2, 16384)])
+                                       (37, 1027), (20, 1500), (3000, 48), (11, 2049), (4, 4099), (3, 8184), (3, 8192), (2, 16381), (2, 16384), (3, 16384), (600, 8192), (1300, 72)])
 @pytest.mark.parametrize("xt,yt", [(BF16, BF16), (F32, BF16), (F16, F32)])
 def test_sizes(rows, cols, xt, yt):
     x, add = _rand((rows, cols), xt, 1, 2.0, 0.5), _rand((rows, cols), xt, 2)
@@ -135,7 +135,7 @@ def _backward(dy, x, gamma=None, add=None, scale=1.0, accumulate=False, want_x=T
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (3, 2), (1, 7), (5, 8), (2, 31), (9, 64), (17, 100), (700, 257), (5, 1000), (600, 1024), (37, 1027),
-                                       (700, 1500), (9000, 48), (3000, 16), (11, 2049), (30, 4099), (3, 8184), (3, 8192), (2, 16381), (20, 16384)])
+                                       (700, 1500), (9000, 48), (3000, 16), (11, 2049), (30, 4099), (3, 8184), (3, 8192), (2, 16381), (20, 16384), (3, 16384), (600, 8192), (33, 520), (90, 1030)])
 @pytest.mark.parametrize("dt,xt", [(BF16, BF16), (F32, F32), (F16, F32), (BF16, F16)])
 def test_gradient_sizes(rows, cols, dt, xt):
     x, add = _rand((rows, cols), xt, 1, 2.0, 0.5), _rand((rows, cols), xt, 2)
