@@ -10,12 +10,12 @@ namespace {
 
 template <typename TX, typename TY> constexpr int kColsOf = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
 
-template <bool kAdd, typename TX, typename TY, Feed kFeed, int kGroups, int kThreads>
+template <bool kAdd, typename TX, typename TY, Feed kFeed, int kGroups, int kThreads, bool kPlain>
 __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma, beta, the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
     constexpr int kC = kColsOf<TX, TY>;
-    using Group = RowGroup<kFeed, kC>;
+    using Group = RowGroup<kFeed, kC, kPlain>;
     using Raw = typename Group::template Raw<TX>;
     constexpr int kX = kC * (int)sizeof(TX), kAtAdd = kGroups * kX, kAll = kAtAdd * (kAdd ? 2 : 1);   // bytes of a thread in a stage
     Team team(shape, kC, slots);
@@ -160,10 +160,11 @@ deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cu
             m.add(a.add, a.ld_add, sizeof(TX));
             m.add(a.sum, a.ld_sum, sizeof(TX));
             const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 4, 0, 0);
-            return with_shape<kC>(s, [&](auto feed, auto groups, auto threads) -> deft_status {
+            return with_shape<kC>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
                 constexpr Feed kFeed = decltype(feed)::value;
                 constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
-                auto kernel = a.add ? k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads> : k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads>;
+                constexpr bool kPlain = decltype(plain)::value;
+                auto kernel = a.add ? k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads, kPlain> : k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads, kPlain>;
                 if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
                 kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
                 DEFT_CUDA_TRY(cudaGetLastError());

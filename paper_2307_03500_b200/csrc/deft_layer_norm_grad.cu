@@ -16,12 +16,12 @@ constexpr int kPartials = 2 * 148;   // CTAs that leave partial sums at most; a 
 
 template <typename TD, typename TX> constexpr int kColsOf = sizeof(TD) == 4 || sizeof(TX) == 4 ? 4 : 8;
 
-template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads>
+template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads, bool kPlain>
 __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma and room for a second vector (at the end the CTA's sums), the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
     constexpr int kC = kColsOf<TD, TX>;
-    using Group = RowGroup<kFeed, kC>;
+    using Group = RowGroup<kFeed, kC, kPlain>;
     using RawX = typename Group::template Raw<TX>;
     using RawD = typename Group::template Raw<TD>;
     // bytes of a thread in a stage
@@ -261,10 +261,11 @@ deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int 
                 m.add(a.dx, a.ld_dx, sizeof(TX));
                 const TeamShape s = team_shape(m, a.rows, a.cols, (int)(sizeof(TD) + sizeof(TX) * (a.add ? 2 : 1)), 2, 2, kPartials, a.dgamma || a.dbeta ? kJoinTurns : 0);
                 blocks = s.blocks;
-                return with_shape<kC>(s, [&](auto feed, auto groups, auto threads) -> deft_status {
+                return with_shape<kC>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
                     constexpr Feed kFeed = decltype(feed)::value;
                     constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
-                    auto kernel = a.add ? k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads> : k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads>;
+                    constexpr bool kPlain = decltype(plain)::value;
+                    auto kernel = a.add ? k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads, kPlain> : k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads, kPlain>;
                     if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
                     joined = s.joined;
                     if (joined) {
