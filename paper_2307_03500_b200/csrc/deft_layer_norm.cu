@@ -11,7 +11,7 @@ namespace {
 template <typename TX, typename TY> constexpr int kColsOf = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
 
 template <bool kAdd, typename TX, typename TY, Feed kFeed, int kGroups, int kThreads, bool kPlain>
-__global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
+__global__ void __launch_bounds__(kThreads, kThreads != kTeamThreads ? 1 : (kPlain && kGroups * kColsOf<TX, TY> == 16 ? 4 : 3)) k_layer_norm(const __grid_constant__ LayerNormArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma, beta, the ring
     __shared__ float2 slots[2 * kTeamMostWarps];
     constexpr int kC = kColsOf<TX, TY>;
@@ -36,8 +36,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(x.group(j), ring.target(stage, j * kX, kX));
-                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kX, kX));
+                group[j].copy(x.group(j), a.x, ring.target(stage, j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), a.add, ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();
@@ -63,8 +63,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_
         uint64_t s1 = 0, s2 = 0;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
-            v[j] = Cols<kC>{};
-            if (!group[j].any) continue;
             Raw raw, more;
             if constexpr (kFeed == Feed::kRing) {
                 ring.read(j * kX, raw);
@@ -80,8 +78,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_
 #pragma unroll
                 for (int i = 0; i < kC / 2; ++i) v[j].p[i] = add2(v[j].p[i], m.p[i]);
             }
-            if (!group[j].whole) v[j].trim(group[j].lo, group[j].hi);
-            if (kAdd && a.sum && mine) group[j].store(sum_out.group(j), v[j]);
+            if (j == 0 || kFeed != Feed::kRing) group[j].clear(v[j]);      // (a thread's first group alone may begin before the row)
+            if (kAdd && a.sum && mine && group[j].any) group[j].store(sum_out.group(j), v[j]);
 #pragma unroll
             for (int i = 0; i < kC / 2; ++i) {
                 s1 = add2(s1, v[j].p[i]);
@@ -100,7 +98,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_
             s1 = s2 = 0;
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                if (!group[j].any) continue;
                 Cols<kC> d;
 #pragma unroll
                 for (int i = 0; i < kC / 2; ++i) d.p[i] = add2(v[j].p[i], minus);
@@ -127,13 +124,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 4 : 1) k_
             const uint64_t by = both(rstd), plus = both(-mean * rstd);
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                if (!group[j].any) continue;
                 Cols<kC> w, b;
-                read_place(gamma, places, team.at + j * team.size, w);
-                read_place(beta, places, team.at + j * team.size, b);
+                const int place = kPlain ? team.at + j * team.size : min(team.at + j * team.size, places - 1);
+                read_place(gamma, places, place, w);
+                read_place(beta, places, place, b);
 #pragma unroll
                 for (int i = 0; i < kC / 2; ++i) v[j].p[i] = fma2(fma2(v[j].p[i], by, plus), w.p[i], b.p[i]);
-                group[j].store(y.group(j), v[j]);
+                if (group[j].any) group[j].store(y.group(j), v[j]);
             }
             if (team.at == 0 && a.rstd) a.rstd[r] = rstd;
         }
@@ -159,8 +156,8 @@ deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cu
             m.add(a.y, a.ld_y, sizeof(TY));
             m.add(a.add, a.ld_add, sizeof(TX));
             m.add(a.sum, a.ld_sum, sizeof(TX));
-            const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 4, 0, 0);
-            return with_shape<kC>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
+            const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 3, 4, 0, 0, true);
+            return with_shape<kC, true>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
                 constexpr Feed kFeed = decltype(feed)::value;
                 constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                 constexpr bool kPlain = decltype(plain)::value;

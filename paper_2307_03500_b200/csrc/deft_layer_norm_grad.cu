@@ -44,9 +44,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(dy.group(j), ring.target(stage, j * kD, kD));
-                group[j].copy(x.group(j), ring.target(stage, kAtX + j * kX, kX));
-                if (kAdd) group[j].copy(add.group(j), ring.target(stage, kAtAdd + j * kX, kX));
+                group[j].copy(dy.group(j), a.dy, ring.target(stage, j * kD, kD));
+                group[j].copy(x.group(j), a.x, ring.target(stage, kAtX + j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), a.add, ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();
@@ -95,10 +95,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
             h[j].from(raw_x);
 #pragma unroll
             for (int i = 0; i < kC / 2; ++i) h[j].p[i] = mul2(add2(h[j].p[i], minus_mean), by);
-            if (!group[j].whole) {
-                h[j].trim(group[j].lo, group[j].hi);
-                d[j].trim(group[j].lo, group[j].hi);
-            }
+            // (what lies behind the row's end has come as zeros: d's are enough for all sums)
+            if (kFeed != Feed::kRing) group[j].clear(h[j]);
+            if (j == 0 || kFeed != Feed::kRing) group[j].clear(d[j]);
             if (mine) {
 #pragma unroll
                 for (int i = 0; i < kC / 2; ++i) {
@@ -107,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
                 }
             }
             Cols<kC> w;
-            read_place(params, places, group[j].any ? team.at + j * team.size : 0, w);
+            read_place(params, places, kPlain ? team.at + j * team.size : min(team.at + j * team.size, places - 1), w);
 #pragma unroll
             for (int i = 0; i < kC / 2; ++i) {
                 d[j].p[i] = mul2(d[j].p[i], w.p[i]);
@@ -259,9 +258,9 @@ deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int 
                 m.add(a.dy, a.ld_dy, sizeof(TD));
                 m.add(a.add, a.ld_add, sizeof(TX));
                 m.add(a.dx, a.ld_dx, sizeof(TX));
-                const TeamShape s = team_shape(m, a.rows, a.cols, (int)(sizeof(TD) + sizeof(TX) * (a.add ? 2 : 1)), 2, 2, kPartials, a.dgamma || a.dbeta ? kJoinTurns : 0);
+                const TeamShape s = team_shape(m, a.rows, a.cols, (int)(sizeof(TD) + sizeof(TX) * (a.add ? 2 : 1)), 2, 2, 2, kPartials, a.dgamma || a.dbeta ? kJoinTurns : 0, false);
                 blocks = s.blocks;
-                return with_shape<kC>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
+                return with_shape<kC, false>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
                     constexpr Feed kFeed = decltype(feed)::value;
                     constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                     constexpr bool kPlain = decltype(plain)::value;

@@ -56,11 +56,13 @@ struct Shifts {
 };
 
 // row_bytes: bytes of a column of all matrices that are read; params: fp32 vectors of the row's length in shared memory; per_sm:
-// CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds; most_blocks: of the launch (0: as many as the device holds).
+// CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds (per_sm_plain: without tests); most_blocks: of the launch (0: as many as the device holds).
 // Rows of up to 8192 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32; from 4096
 // columns on a CTA has a row at a time and an SM one CTA, whose parameters and ring fill its shared memory.
+// three: threads may have 24 columns, where that takes fewer of them for a row (768 columns: one warp, no lane idle; 17 -> 15 us at
+// 16384 rows) and the ring still has two stages.
 // join_turns: the call is one cluster of up to kMostJoined CTAs where a team then takes no more rows than that (0: never).
-inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int64_t most_blocks, int join_turns) {
+inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int per_sm_plain, int64_t most_blocks, int join_turns, bool three) {
     TeamShape s{};
     bool shifted = m.ok;
     const int len = m.cols;
@@ -78,14 +80,25 @@ inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_byt
     }
     const bool large = s.places * len > kTeamThreads * 16;
     if (large) per_sm = 1;
-    const int most = (s.places * len > kTeamMost * 16 ? 32 : 16) / len, need = (s.places + most - 1) / most;
-    s.size = 4;
-    while (s.size < 32 && s.size < need) s.size *= 2;
-    if (need > 32) s.size = large ? kTeamMost : (need + 31) / 32 * 32;
+    int most = (s.places * len > kTeamMost * 16 ? 32 : 16) / len;
+    auto size_for = [&](int columns) {
+        const int need = (s.places * len + columns - 1) / columns;
+        int size = 4;
+        while (size < 32 && size < need) size *= 2;
+        return need > 32 ? (need + 31) / 32 * 32 : size;
+    };
+    s.size = large ? kTeamMost : size_for(16);
+    const bool by_three = three && row_bytes <= 2 && s.size >= 64 && s.size <= 96 && size_for(24) < s.size && rows * size_for(24) * 2 > 148 * 512;
+    if (by_three) {
+        s.size = size_for(24);
+        most = 24 / len;
+    }
     // few rows: more threads for each, so that all SMs' schedulers have work
-    while (s.size * 2 <= kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
-    s.groups = large || s.size * (most / 2) < s.places ? most : most / 2;
+    while (!by_three && s.size * 2 <= kTeamThreads && s.size < s.places && rows * s.size * 2 <= 148 * 512) s.size *= 2;
+    s.groups = large || by_three || s.size * (most / 2) < s.places ? most : most / 2;
     s.threads = s.size > kTeamThreads ? s.size : kTeamThreads / s.size * s.size;
+    s.plain = shifted && s.first == 0 && s.ld == 0 && cols % len == 0 && s.places == s.size * s.groups && (s.groups * len == 16 || by_three);
+    if (!large) per_sm = (s.plain && !by_three ? per_sm_plain : per_sm) * kTeamThreads / s.threads;
     if (most_blocks == 0) most_blocks = (int64_t)sm_count() * per_sm;
     const int64_t teams = s.threads / s.size, needed = ((rows + s.step - 1) / s.step + teams - 1) / teams;   // CTAs for the rows of a shift
     s.joined = needed * s.step <= (int64_t)kMostJoined * join_turns;
@@ -99,7 +112,6 @@ inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_byt
     s.stages = share > s.smem ? (int)((share - s.smem) / stage) : 0;
     if (s.stages > kMostStages) s.stages = kMostStages;
     if (s.stages > turns) s.stages = (int)turns;
-    s.plain = shifted && s.first == 0 && s.ld == 0 && cols % len == 0 && s.places == s.size * s.groups && s.groups * len == 16;
     s.feed = !shifted ? Feed::kElements : (s.stages >= 1 ? Feed::kRing : Feed::kLoads);
     if (s.feed == Feed::kRing) s.smem += stage * s.stages;
     else s.groups = 32 / len;
@@ -121,13 +133,26 @@ struct RowGroup {
         whole = lo == 0 && hi == kC;
     }
     template <typename T> using Raw = RawCols<T, kC, kPieces>;
-    // `row` points to the group's first column throughout (which may lie before the row).  Whole pieces are read where an element of
-    // them is the row's.
+    // `row` points to the group's first column throughout (which may lie before the row).  To shared memory: what lies behind the row's
+    // end becomes zero there (`other`: any address that may be read, for groups that have nothing).
     template <typename T>
-    __device__ __forceinline__ void copy(const T* row, uint32_t to) const {
-        if (!any) return;
-        if constexpr (kC * sizeof(T) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row) : "memory");
-        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(row) : "memory");
+    __device__ __forceinline__ void copy(const T* row, const void* other, uint32_t to) const {
+        constexpr int kBytes = kC * (int)sizeof(T);
+        const void* from = any ? static_cast<const void*>(row) : other;
+        const int bytes = any ? hi * (int)sizeof(T) : 0;
+        if constexpr (kPlain && kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row) : "memory");
+        else if constexpr (kPlain) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(row) : "memory");
+        else if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+    }
+    // Of a group that has come through the ring, elements before the row remain to be cleared.
+    template <int kN>
+    __device__ __forceinline__ void clear(Cols<kN>& v) const {
+        if constexpr (kFeed == Feed::kRing) {
+            if (lo > 0) v.trim(lo, kC);
+        } else {
+            if (!whole) v.trim(lo, hi);
+        }
     }
     // Plain loads: a row may be overwritten by its own threads later.
     template <typename T>
@@ -213,16 +238,30 @@ __device__ __forceinline__ void write_place(float* s, int places, int place, con
 #pragma unroll
     for (int i = 0; i < kC / 4; ++i) reinterpret_cast<ulonglong2*>(s)[i * places + place] = make_ulonglong2(v.p[2 * i], v.p[2 * i + 1]);
 }
-__device__ __forceinline__ float param(const void* p, int type, int i) {
-    return type == DEFT_F32 ? static_cast<const float*>(p)[i]
-                            : (type == DEFT_BF16 ? to_f32(static_cast<const __nv_bfloat16*>(p)[i]) : to_f32(static_cast<const __half*>(p)[i]));
+// A vector (NULL: `otherwise` throughout) to its places.  The loads of eight turns are under way together: one after the other they
+// took longer than a row (5003 x 1027 fp32 15 us).
+template <int kC, typename T>
+__device__ __forceinline__ void fill_places(float* s, const T* p, int cols, int places, int shift, float otherwise) {
+    constexpr int kDeep = 8;
+    const int all = places * kC, step = (int)blockDim.x;
+    for (int i0 = threadIdx.x; i0 < all; i0 += kDeep * step) {
+        T v[kDeep];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int c = i0 + k * step - shift;
+            v[k] = from_f32<T>(otherwise);
+            if (p && c >= 0 && c < cols) v[k] = p[c];
+        }
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k)
+            if (i0 + k * step < all) s[at_place<kC>(places, i0 + k * step)] = to_f32(v[k]);
+    }
 }
 template <int kC>
 __device__ __forceinline__ void fill_places(float* s, const void* p, int type, int cols, int places, int shift, float otherwise) {
-    for (int i = threadIdx.x; i < places * kC; i += blockDim.x) {
-        const int c = i - shift;
-        s[at_place<kC>(places, i)] = p && c >= 0 && c < cols ? param(p, type, c) : otherwise;
-    }
+    if (type == DEFT_F32) fill_places<kC>(s, static_cast<const float*>(p), cols, places, shift, otherwise);
+    else if (type == DEFT_BF16) fill_places<kC>(s, static_cast<const __nv_bfloat16*>(p), cols, places, shift, otherwise);
+    else fill_places<kC>(s, static_cast<const __half*>(p), cols, places, shift, otherwise);
 }
 
 // The threads that share a row, the rows they take, and their sums.
@@ -260,7 +299,13 @@ struct Team {
         float2* s = slots + turn * kTeamMostWarps + team * warps;
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[at >> 5] = make_float2(a, b);
-        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
+        // (numbers that the compiler knows: of CTAs with a number in a register an SM holds four)
+        switch (team) {
+            case 0: asm volatile("bar.sync 1, %0;" ::"r"(size) : "memory"); break;
+            case 1: asm volatile("bar.sync 2, %0;" ::"r"(size) : "memory"); break;
+            case 2: asm volatile("bar.sync 3, %0;" ::"r"(size) : "memory"); break;
+            default: asm volatile("bar.sync 4, %0;" ::"r"(size) : "memory"); break;
+        }
         a = b = 0.0f;
         for (int i = 0; i < warps; ++i) {
             a += s[i].x;
@@ -272,7 +317,7 @@ struct Team {
 
 // Calls f with the feed, the number of groups of a thread, the threads of a CTA and `plain` as constants (a ring of short rows; its long
 // ones; other feeds).  Without their tests 16384 x 1024 takes 3 per cent less, 8192 x 4096 7.
-template <int kC, typename F>
+template <int kC, bool kThree, typename F>
 deft_status with_shape(const TeamShape& s, F&& f) {
     using Ring = FeedTag<Feed::kRing>;
     using Small = AlignTag<kTeamThreads>;
@@ -280,6 +325,9 @@ deft_status with_shape(const TeamShape& s, F&& f) {
     if (s.feed == Feed::kElements) return f(FeedTag<Feed::kElements>{}, AlignTag<32 / kC>{}, Large{}, AlignTag<0>{});
     if (s.feed == Feed::kLoads) return f(FeedTag<Feed::kLoads>{}, AlignTag<32 / kC>{}, Large{}, AlignTag<0>{});
     const bool large = s.threads > kTeamThreads;
+    if constexpr (kThree) {
+        if (s.groups * kC == 24) return s.plain ? f(Ring{}, AlignTag<24 / kC>{}, Small{}, AlignTag<1>{}) : f(Ring{}, AlignTag<24 / kC>{}, Small{}, AlignTag<0>{});
+    }
     if (s.plain) return large ? f(Ring{}, AlignTag<16 / kC>{}, Large{}, AlignTag<1>{}) : f(Ring{}, AlignTag<16 / kC>{}, Small{}, AlignTag<1>{});
     if (large) return s.groups * kC == 32 ? f(Ring{}, AlignTag<32 / kC>{}, Large{}, AlignTag<0>{}) : f(Ring{}, AlignTag<16 / kC>{}, Large{}, AlignTag<0>{});
     if (s.groups * kC == 16) return f(Ring{}, AlignTag<16 / kC>{}, Small{}, AlignTag<0>{});
