@@ -47,7 +47,15 @@ struct Exact {
         lo += __fmaf_rn(a, b, -p);
     }
 };
-// d (hi + lo) + c; an infinite d stays what it is (the lower piece may be 0).
+// d (hi + lo) - norm; an infinite d stays what it is (the lower piece may be 0).
+__device__ __forceinline__ Exact log_prob(float d, float hi, float lo, Exact norm) {
+    Exact y{-norm.hi, -norm.lo};
+    if (!isfinite(d)) return Exact{d, 0.0f};
+    y.add_product(d, hi);
+    y.lo += d * lo;
+    return y;
+}
+// d (hi + lo) + c, likewise.
 __device__ __forceinline__ float scaled(float d, float hi, float lo, float c) {
     const float y = __fmaf_rn(d, hi, c);
     return isfinite(d) ? __fmaf_rn(d, lo, y) : y;
@@ -66,17 +74,27 @@ __device__ __forceinline__ Exact log_of(float x) {
 }
 __device__ __forceinline__ Exact shuffled(Exact x, int o) { return Exact{__shfl_xor_sync(0xffffffffu, x.hi, o), __shfl_xor_sync(0xffffffffu, x.lo, o)}; }
 
-// Sums of powers 2^((z - near) c1) relative to a logit; near counts only where the sum is not 0.
-struct Powers {
-    float near, sum;
-};
-// What a warp has summed, and what the CTAs of a row tell each other: of the rest and of the entries the powers; over the
-// entries q (log q - (z - near) / T), and q.
+__device__ __forceinline__ Exact log_of(Exact x) {
+    Exact y = log_of(x.hi);
+    if (x.lo != 0.0f && x.hi > 0.0f && x.hi < INFINITY) y.lo += x.lo / x.hi;
+    return y;
+}
+
+// 2^(d c1) for d <= 0, its argument's rounding made good: that would cost as many units in the last place as the argument has.
+__device__ __forceinline__ float power_near(float d, float c1) {
+    const float p = d * c1, y = exp2_fast(p);
+    return p > -126.0f ? __fmaf_rn(y, 0.693147181f * __fmaf_rn(d, c1, -p), y) : y;
+}
+
+// What a warp has summed: of the rest and of the entries the powers; over the entries q (log q - (z - near) / T), and q.
 struct Sums {
-    Powers rest, entries;
+    float rest_near, rest, entries_near, entries;
     Exact cross, q;
 };
-
+// What the gradient needs of it, for a CTA.
+struct Brief {
+    float rest_near, rest, entries_near, entries, q;
+};
 // What the gradient of a row is formed with: an element's is A 2^((z - all) c1) - B 2^((z - rest) c1), an entry's own
 // A 2^((z - all) c1) - q f.
 struct Factors {
@@ -99,35 +117,32 @@ __device__ __forceinline__ float eight_sum(float v) {
     for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// The sum of what the lanes hold (over groups of kLanes), relative to the largest logit among them.
-template <int kLanes>
-__device__ __forceinline__ Powers joined(Powers p, float c1) {
-    float near = p.sum == 0.0f ? -INFINITY : p.near;
-#pragma unroll
-    for (int o = kLanes / 2; o; o >>= 1) near = fmaxf(near, __shfl_xor_sync(0xffffffffu, near, o));
-    if (near == -INFINITY) near = 0.0f;
-    float sum = p.sum == 0.0f ? 0.0f : p.sum * exp2_fast((p.near - near) * c1);
-#pragma unroll
-    for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return Powers{near, sum};
-}
 template <int kLanes>
 __device__ __forceinline__ Exact joined(Exact x) {
 #pragma unroll
     for (int o = kLanes / 2; o; o >>= 1) x.add(shuffled(x, o));
     return x;
 }
-// ... with the entries' terms, which change with what their logits are relative to: q (near - new near) / T.
+// The sum of what the lanes hold (over groups of kLanes), relative to the largest logit among them, which `near` becomes (0: none).
 template <int kLanes>
-__device__ __forceinline__ Sums joined(const Sums& s, float c1, float by) {
-    Sums o;
-    o.rest = joined<kLanes>(s.rest, c1);
-    o.entries = joined<kLanes>(s.entries, c1);
-    Exact cross = s.cross;
-    if (s.q.hi != 0.0f && s.entries.near != o.entries.near) cross.add_product(-s.q.hi, (s.entries.near - o.entries.near) * by);
-    o.cross = joined<kLanes>(cross);
-    o.q = joined<kLanes>(s.q);
-    return o;
+__device__ __forceinline__ float joined(float& near, float sum, float c1) {
+    float most = sum == 0.0f ? -INFINITY : near;
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (most == -INFINITY) most = 0.0f;
+    sum = sum == 0.0f ? 0.0f : sum * power_near(near - most, c1);
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    near = most;
+    return sum;
+}
+template <int kLanes>
+__device__ __forceinline__ Brief joined(Brief s, float c1) {
+    s.rest = joined<kLanes>(s.rest_near, s.rest, c1);
+    s.entries = joined<kLanes>(s.entries_near, s.entries, c1);
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) s.q += __shfl_xor_sync(0xffffffffu, s.q, o);
+    return s;
 }
 
 // Sixteen bytes of a row as pairs of fp32 numbers.
@@ -203,14 +218,15 @@ __device__ __forceinline__ float value_of(const DistillArgs& a, uint32_t t) {
 // A row's entries in shared memory.
 struct Entries {
     int* col;                              // column; -1: none; -2: another CTA's; -3 - column: not the first of its column
-    float *log_q, *prob, *own;             // own: the student's logit
+    float *log_q, *log_q_lo, *prob, *own;  // log q in two pieces; own: the student's logit
     __device__ __forceinline__ Entries(char* at, int top) : col(reinterpret_cast<int*>(at)) {
         log_q = reinterpret_cast<float*>(col + top);
-        prob = log_q + top;
+        log_q_lo = log_q + top;
+        prob = log_q_lo + top;
         own = prob + top;
     }
 };
-constexpr size_t kEntryBytes = 16;
+constexpr size_t kEntryBytes = 20;
 
 // What stands for an element without a share.
 template <typename T> __device__ __forceinline__ T lowest();
@@ -330,7 +346,8 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     constexpr int kPer = Granule<T>::kPer;
     extern __shared__ __align__(16) char smem[];
     Granule<T>* const cells = reinterpret_cast<Granule<T>*>(smem);
-    __shared__ Sums warp_sums[kMost / 32], cta_sums[kMostCluster];
+    __shared__ Sums warp_sums[kMost / 32];
+    __shared__ Brief briefs[kMostCluster];
     __shared__ Factors factors;
     __shared__ int twice;                  // the last row in which an entry found nothing in its place: another one's column, or -inf
     const int ctas = shape.ctas, threads = shape.threads, warps = threads >> 5, all_threads = threads + 32;
@@ -354,55 +371,79 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             return;
         }
         bar_sync<kSummed>(all_threads);
-        Sums s = warp_sums[0];
+        const int entry_warps = min(warps, (a.top + 31) >> 5);
+        // in short what the gradient waits for
+        Sums* const others = reinterpret_cast<Sums*>(smem + (size_t)shape.granules * 16 + (size_t)a.top * kEntryBytes);   // [ctas][entry_warps], in the first CTA
+        auto brief = [&](int w) { return Brief{warp_sums[w].rest_near, warp_sums[w].rest, warp_sums[w].entries_near, warp_sums[w].entries, warp_sums[w].q.hi}; };
+        Brief s{};
         if (warps > 8) {
-            s = Sums{};
-            if (lane < warps) s = warp_sums[lane];
-            s = joined<32>(s, a.c1, a.by);
+            if (lane < warps) s = brief(lane);
+            s = joined<32>(s, a.c1);
         } else if (warps > 1) {            // eight lanes, four times over
-            s = Sums{};
-            if ((lane & 7) < warps) s = warp_sums[lane & 7];
-            s = joined<8>(s, a.c1, a.by);
+            if ((lane & 7) < warps) s = brief(lane & 7);
+            s = joined<8>(s, a.c1);
+        } else {
+            s = brief(0);
         }
         if (ctas > 1) {
             cluster_wait();                // all CTAs run: their shared memory may be written
-            if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&cta_sums[rank], lane) = s;
+            if (lane < ctas) *cooperative_groups::this_cluster().map_shared_rank(&briefs[rank], lane) = s;
+            if (a.loss && rank != 0 && lane < entry_warps) *cooperative_groups::this_cluster().map_shared_rank(others + rank * entry_warps + lane, 0) = warp_sums[lane];
             cluster_arrive_release();
             cluster_wait();
-            s = Sums{};
-            if ((lane & 7) < ctas) s = cta_sums[lane & 7];
-            s = joined<8>(s, a.c1, a.by);
+            s = Brief{};
+            if ((lane & 7) < ctas) s = briefs[lane & 7];
+            s = joined<8>(s, a.c1);
         }
-        const float all = s.rest.sum == 0.0f ? s.entries.near : (s.entries.sum == 0.0f ? s.rest.near : fmaxf(s.rest.near, s.entries.near));
-        const float total = (s.rest.sum == 0.0f ? 0.0f : s.rest.sum * exp2_fast((s.rest.near - all) * a.c1)) +
-                            (s.entries.sum == 0.0f ? 0.0f : s.entries.sum * exp2_fast((s.entries.near - all) * a.c1));
-        // the teacher's probability outside its entries; none where there is no other logit
-        const float left = a.teacher_lse && !(s.rest.sum == 0.0f) ? fmaxf(0.0f, (1.0f - s.q.hi) - s.q.lo) : 0.0f;
+        const float all = s.rest == 0.0f ? s.entries_near : (s.entries == 0.0f ? s.rest_near : fmaxf(s.rest_near, s.entries_near));
         if (g) {
-            const float f = weight * a.grad_factor;
-            if (lane == 0) factors = Factors{all, s.rest.near, (s.q.hi + (s.q.lo + left)) / total * f, left > 0.0f ? left / s.rest.sum * f : 0.0f};
+            const float total = (s.rest == 0.0f ? 0.0f : s.rest * exp2_fast((s.rest_near - all) * a.c1)) +
+                                (s.entries == 0.0f ? 0.0f : s.entries * exp2_fast((s.entries_near - all) * a.c1));
+            // the teacher's probability outside its entries; none where there is no other logit
+            const float left = a.teacher_lse && !(s.rest == 0.0f) ? fmaxf(0.0f, 1.0f - s.q) : 0.0f, f = weight * a.grad_factor;
+            if (lane == 0) factors = Factors{all, s.rest_near, (s.q + left) / total * f, left > 0.0f ? left / s.rest * f : 0.0f};
             bar_arrive<kFactors>(all_threads);
         }
-        if (a.loss && rank == 0 && lane == 0) {
-            const Exact log_total = log_of(total);
-            Exact loss = s.cross;
-            if (s.q.hi != 0.0f) {
-                loss.add_product(s.q.hi, (all - s.entries.near) * a.by);
-                loss.add_product(s.q.hi, log_total.hi);
-                loss.lo += s.q.hi * log_total.lo;
+        if (a.loss && rank == 0) {         // the loss, from all warps' sums: what remains of terms that nearly cancel
+            Exact cross{0.0f, 0.0f}, q{0.0f, 0.0f};
+            const int all_entry_warps = ctas * entry_warps;
+            for (int i = lane; i < all_entry_warps; i += 32) {
+                const Sums w = i < entry_warps ? warp_sums[i] : others[i];
+                cross.add(w.cross);
+                if (w.q.hi != 0.0f && w.entries_near != s.entries_near) cross.add_product(-w.q.hi, (w.entries_near - s.entries_near) * a.by);
+                q.add(w.q);
             }
-            if (left > 0.0f) {
-                const Exact log_left = log_of(left), log_rest = log_of(s.rest.sum);
-                Exact d = log_left;
-                d.add(Exact{-log_rest.hi, -log_rest.lo});
-                d.add((all - s.rest.near) * a.by);
-                d.add(log_total);
-                loss.add_product(left, d.hi);
-                loss.lo += left * d.lo;
+            if (all_entry_warps > 8) {
+                cross = joined<32>(cross);
+                q = joined<32>(q);
+            } else if (all_entry_warps > 1) {
+                cross = joined<8>(cross);
+                q = joined<8>(q);
             }
-            const float value = loss.hi + loss.lo;
-            // (where a term is infinite, what its roundings have left out is no number)
-            a.loss[row] = (isfinite(loss.hi) ? value : loss.hi) * weight * a.loss_factor;
+            if (lane == 0) {
+                Exact total{0.0f, 0.0f};
+                if (s.rest != 0.0f) total.add_product(s.rest, power_near(s.rest_near - all, a.c1));
+                if (s.entries != 0.0f) total.add_product(s.entries, power_near(s.entries_near - all, a.c1));
+                const float left = a.teacher_lse && !(s.rest == 0.0f) ? fmaxf(0.0f, (1.0f - q.hi) - q.lo) : 0.0f;
+                const Exact log_total = log_of(total);
+                Exact loss = cross;
+                if (q.hi != 0.0f) {
+                    loss.add_product(q.hi, (all - s.entries_near) * a.by);
+                    loss.add_product(q.hi, log_total.hi);
+                    loss.lo += q.hi * log_total.lo;
+                }
+                if (left > 0.0f) {
+                    const Exact log_rest = log_of(s.rest);
+                    Exact d = log_of(left);
+                    d.add(Exact{-log_rest.hi, -log_rest.lo});
+                    d.add((all - s.rest_near) * a.by);
+                    d.add(log_total);
+                    loss.add_product(left, d.hi);
+                    loss.lo += left * d.lo;
+                }
+                // (where a term is infinite, what its roundings have left out is no number)
+                a.loss[row] = (isfinite(loss.hi) ? loss.hi + loss.lo : loss.hi) * weight * a.loss_factor;
+            }
         }
         return;
     }
@@ -430,9 +471,9 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     const bool has_entries = warp * 32 < a.top;
     if (tid == 0) twice = -1;
     RawEntry raw{0, 0, 0};
-    float norm = 0.0f;
+    Exact norm{0.0f, 0.0f};
     if (tid < a.top) raw = entry_at(a, row, tid);
-    if (has_entries && a.teacher_lse) norm = a.teacher_lse[row];
+    if (has_entries && a.teacher_lse) norm.hi = a.teacher_lse[row];
     {
         const T* from = z + base + tid * kPer;
         uint32_t to = (uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)tid * 16u;
@@ -458,19 +499,19 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                     const float d = value_of(a, e.t) - near;
                     if (column_of(a, e) >= 0) sum += expf(scaled(d, a.it_hi, a.it_lo, 0.0f));
                 }
-                const Exact log_sum = log_of(warp_sum(sum));
-                norm = log_sum.hi + log_sum.lo;
+                norm = log_of(warp_sum(sum));
             }
         }
         for (int j = tid; j < a.top; j += threads) {
             if (j >= threads) raw = entry_at(a, row, j);
             const int col = column_of(a, raw);
             const bool valid = col >= 0;
-            const float d = value_of(a, raw.t) - near;
-            const float log_q = scaled(d, a.it_hi, a.it_lo, -norm), q = valid ? expf(log_q) : 0.0f;
+            const Exact log_q = log_prob(value_of(a, raw.t) - near, a.it_hi, a.it_lo, norm);
+            const float q = valid ? expf(log_q.hi + log_q.lo) : 0.0f;
             const bool here = valid && col >= base && col < base + n * kPer;
             entry.col[j] = valid && !here ? -2 : col;
-            entry.log_q[j] = log_q;
+            entry.log_q[j] = log_q.hi;
+            entry.log_q_lo[j] = log_q.lo;
             entry.prob[j] = q;
             if (here) q_sum.add(q);
         }
@@ -511,22 +552,32 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         for (int j = tid; j < a.top; j += threads)
             if (entry.col[j] >= 0) most = fmaxf(most, entry.own[j]);
         most = warp_max(most);
-        s.entries.near = most == -INFINITY ? 0.0f : most;
+        s.entries_near = most == -INFINITY ? 0.0f : most;
         for (int j = tid; j < a.top; j += threads) {
             const int col = entry.col[j];
             if (col == -1 || col == -2) continue;
-            const float own = entry.own[j], q = entry.prob[j], d = own - s.entries.near;
-            if (q != 0.0f) s.cross.add_product(q, scaled(-d, a.by, a.by_lo, entry.log_q[j]));
-            if (col >= 0) s.entries.sum += exp2_fast(d * a.c1);
+            const float own = entry.own[j], q = entry.prob[j], d = own - s.entries_near;
+            if (q != 0.0f) {
+                Exact t{entry.log_q[j], entry.log_q_lo[j]};
+                if (isfinite(d)) {
+                    t.add_product(-d, a.by);
+                    t.lo -= d * a.by_lo;
+                    s.cross.add_product(q, t.hi);
+                    s.cross.lo += q * t.lo;
+                } else {
+                    s.cross.add(-d);       // (an entry without any share: an infinite loss; no number stays none)
+                }
+            }
+            if (col >= 0) s.entries += exp2_fast(d * a.c1);
         }
     }
     // what the powers are relative to: the largest of a granule of every lane, which is seldom far from the largest of all
     float most = warp_max(tid < n ? most_of<T>(cells[tid]) : -INFINITY);
     bool careful = false;
-    s.rest.near = most == -INFINITY ? 0.0f : most;
-    float from = s.rest.near * a.c1;
+    s.rest_near = most == -INFINITY ? 0.0f : most;
+    float from = s.rest_near * a.c1;
     // (from is rounded: what the powers are relative to instead of near)
-    float off = exp2_fast(__fmaf_rn(-s.rest.near, a.c1, from));
+    float off = exp2_fast(__fmaf_rn(-s.rest_near, a.c1, from));
     float rest = warp_sum(sum_powers<T, false>(cells, n, threads, from, a.c1));
     // the sample is too far off (or something is no number).  Powers and factors below 2^-126 are 0: within these bounds
     // no probability above 2^-96 is lost
@@ -535,18 +586,18 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         for (int c = tid; c < n; c += threads) most = fmaxf(most, most_of<T>(cells[c]));
         most = warp_max(most);
         careful = true;
-        s.rest.near = from = most == -INFINITY ? 0.0f : most;
+        s.rest_near = from = most == -INFINITY ? 0.0f : most;
         off = 1.0f;
         rest = warp_sum(sum_powers<T, true>(cells, n, threads, from, a.c1));
     }
-    s.rest.sum = rest * off;
+    s.rest = rest * off;
     if (has_entries) {
         if (a.top <= 8) {                  // (lanes without an entry have nothing to join)
-            s.entries.sum = eight_sum(s.entries.sum);
+            s.entries = eight_sum(s.entries);
             s.cross = joined<8>(s.cross);
             s.q = joined<8>(q_sum);
         } else {
-            s.entries.sum = warp_sum(s.entries.sum);
+            s.entries = warp_sum(s.entries);
             s.cross = joined<32>(s.cross);
             s.q = joined<32>(q_sum);
         }
@@ -561,7 +612,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         bar_sync<kFactors>(all_threads);
         const Factors f = factors;
         // (nothing but -inf: the share is 0, and NaN where the whole row has no other)
-        const float k = rest == 0.0f ? 0.0f * f.A : (f.A * exp2_fast((s.rest.near - f.all) * a.c1) - f.B * exp2_fast((s.rest.near - f.rest) * a.c1)) * off;
+        const float k = rest == 0.0f ? 0.0f * f.A : (f.A * exp2_fast((s.rest_near - f.all) * a.c1) - f.B * exp2_fast((s.rest_near - f.rest) * a.c1)) * off;
         if (careful) write_grad<T, true>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
         else write_grad<T, false>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
         bar_row<kMost>(threads);
@@ -594,7 +645,8 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     s.granules = (int)(((bytes + 15) / 16 + ctas - 1) / ctas);
     s.threads = 32;
     while (s.threads < kMostThreads && s.granules * (16 / elem) > s.threads * kEachThread) s.threads *= 2;
-    s.smem = (size_t)s.granules * 16 + (size_t)a.top * kEntryBytes;
+    const size_t entry_warps = (size_t)((a.top + 31) / 32 < s.threads / 32 ? (a.top + 31) / 32 : s.threads / 32);
+    s.smem = (size_t)s.granules * 16 + (size_t)a.top * kEntryBytes + (s.ctas > 1 ? s.ctas * entry_warps * sizeof(Sums) : 0);
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)s.ctas;
