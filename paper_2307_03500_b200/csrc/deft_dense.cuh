@@ -4,6 +4,10 @@
 
 namespace deft {
 
+// Shared memory that a CTA may ask for.  Every call that needs more than a kernel has by itself sets a kernel's limit to this,
+// not to its own need: another host thread's call of the same kernel may lie between a call's setting and its launch.
+constexpr size_t kMostSmem = 220 * 1024;
+
 struct LayerNormArgs {
     const void *x, *add;                 // add: NULL, or of x's type
     void *sum, *y;                       // sum: NULL, or x + add in x's type

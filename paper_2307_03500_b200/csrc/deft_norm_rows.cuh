@@ -108,7 +108,7 @@ inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_byt
     // the ring: as many stages as a CTA's share of an SM's shared memory has room for, and as a team has rows
     const size_t stage = (size_t)(s.threads > kTeamThreads ? kTeamMost : kTeamThreads) * s.groups * len * row_bytes;
     s.smem = (size_t)params * sizeof(float) * (size_t)(s.places * len);
-    const size_t share = (size_t)220 * 1024 / per_sm;
+    const size_t share = kMostSmem / per_sm;
     s.stages = share > s.smem ? (int)((share - s.smem) / stage) : 0;
     if (s.stages > kMostStages) s.stages = kMostStages;
     if (s.stages > turns) s.stages = (int)turns;

@@ -1,5 +1,6 @@
 """The dense row operators as a model uses them together: lookup, norms, rotary attention and a distillation loss through to the
 sparsification step; captured graphs, other streams, matrices beyond 2^31 elements."""
+import concurrent.futures
 import math
 
 import pytest
@@ -184,6 +185,30 @@ def test_streams():
     deft.deft_distill(want[1], ids, t, grad=want[1])
     deft.deft_rotary(want[1].view(4000, 64, 8), want[1].view(4000, 64, 8), turns)
     assert torch.equal(z, want[1])
+
+
+def test_calls_from_two_threads():
+    """Host threads that call the same kernels with different needs of shared memory, each on a stream of its own."""
+    def calls(cols, vocab, seed):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            x, z = _rand((9, cols), seed), _rand((9, vocab), seed + 1)
+            y, dx, w, g = torch.empty_like(x), torch.empty_like(x), torch.empty((2, cols), device="cuda"), torch.empty_like(z)
+            mean, rstd, loss = torch.empty(9, device="cuda"), torch.empty(9, device="cuda"), torch.empty(9, device="cuda")
+            ids, t = torch.zeros((9, 1), dtype=torch.int64, device="cuda"), torch.zeros((9, 1), device="cuda")
+            ws = deft.alloc_layer_norm_workspace(9, cols)
+            for _ in range(300):
+                deft.deft_layer_norm(x, y, mean=mean, rstd=rstd)
+                deft.deft_layer_norm_grad(x, x, mean, rstd, dx, grad_gamma=w[0], grad_beta=w[1], ws=ws)
+                deft.deft_distill(z, ids, t, loss, g)
+            stream.synchronize()
+        return y, dx, w, g, loss
+    sizes = [(16384, 262144, 1), (8192, 120000, 3), (12288, 180000, 5)]
+    want = [calls(*s) for s in sizes]
+    with concurrent.futures.ThreadPoolExecutor(len(sizes)) as pool:
+        got = list(pool.map(lambda s: calls(*s), sizes))
+    for a, b in zip(want, got):
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
 
 
 def test_matrices_beyond_31_bits():
