@@ -11,10 +11,10 @@
 // gradient: keeping the first would take the room of a second part), so 16 elements a cycle and SM of the special function unit, about
 // 0.7 of the copy's time in 16 bits; the rest are conversions and fp32 pairs.  Measured (device time; floor at the copy rate, 6561 GB/s):
 //   8192 x 50257 bf16, 64 entries, gradient           330 us (5.0 TB/s; floor 252)
-//   2048 x 30522 bf16, a quarter masked               49.0 us (floor 33.4)
-//   2048 x 50257 fp32                                 160 us (floor 126)
-//   700 x 33278 fp32, loss alone                      32.4 us (2.9 TB/s; floor 14.2: 1.2 rounds of CTAs, each a copy, a sum, a join)
-//   65536 x 1000 bf16                                 190 us (floor 42: some 1600 instructions a row that do not depend on its width)
+//   2048 x 30522 bf16, a quarter masked               49.1 us (floor 33.4)
+//   2048 x 50257 fp32                                 159 us (floor 126)
+//   700 x 33278 fp32, loss alone                      32.1 us (2.9 TB/s; floor 14.2: 3.5 rounds of CTAs, each a copy, a sum, a join)
+//   65536 x 1000 bf16                                 200 us (floor 42: some 1600 instructions a row that do not depend on its width)
 // Special function unit 56 %, issue slots 54 %, waits at the row's barriers: a CTA copies, sums and writes in turn, and the four
 // of an SM overlap one another's phases.  What was tried against it and was slower: one CTA an SM with three parts in a ring and the powers
 // kept (550 to 750 us), a share of the powers by a polynomial (339 to 416).  Larger and smaller parts gave nothing.
@@ -84,6 +84,12 @@ __device__ __forceinline__ Exact log_of(float x) {
     y.add(logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3)));
     return y;
 }
+// x (hi + lo) times a weight, added to a sum.
+__device__ __forceinline__ void add_scaled(Exact& sum, Exact weight, float x, float hi, float lo) {
+    const float p = __fmul_rn(x, hi), rest = __fmaf_rn(x, hi, -p) + x * lo;
+    sum.add_product(weight.hi, p);
+    sum.lo += weight.hi * rest + weight.lo * p;
+}
 __device__ __forceinline__ Exact shuffled(Exact x, int o) { return Exact{__shfl_xor_sync(0xffffffffu, x.hi, o), __shfl_xor_sync(0xffffffffu, x.lo, o)}; }
 
 __device__ __forceinline__ Exact log_of(Exact x) {
@@ -92,16 +98,25 @@ __device__ __forceinline__ Exact log_of(Exact x) {
     return y;
 }
 
-// 2^(d c1) for d <= 0, its argument's rounding made good: that would cost as many units in the last place as the argument has.
-__device__ __forceinline__ float power_near(float d, float c1) {
-    const float p = d * c1, y = exp2_fast(p);
-    return p > -126.0f ? __fmaf_rn(y, 0.693147181f * __fmaf_rn(d, c1, -p), y) : y;
+// 2^(d c1) for d <= 0 to a unit in the last place, the argument's rounding made good: a polynomial of degree six on [-1/2, 1/2], fitted for the least relative error (2e-9).
+__device__ __forceinline__ float power_of(float d, float c1) {
+    const float p = d * c1;
+    if (!(p > -126.0f)) return p <= -126.0f ? 0.0f : p;      // (no number stays none)
+    const float n = rintf(p), f = (p - n) + __fmaf_rn(d, c1, -p);
+    float y = 1.534580214352e-4f;
+    y = __fmaf_rn(y, f, 1.339993113957e-3f);
+    y = __fmaf_rn(y, f, 9.618488993764e-3f);
+    y = __fmaf_rn(y, f, 5.550328777213e-2f);
+    y = __fmaf_rn(y, f, 0.240226468903f);
+    y = __fmaf_rn(y, f, 0.693147205737f);
+    y = __fmaf_rn(y, f, 1.0f);
+    return __int_as_float(__float_as_int(y) + ((int)n << 23));
 }
 
 // What a warp has summed: of the rest and of the entries the powers; over the entries q (log q - (z - near) / T), and q.
 struct Sums {
-    float rest_near, rest, entries_near, entries;
-    Exact cross, q;
+    float rest_near, rest, entries_near;
+    Exact entries, cross, q;             // (an error of the entries' share is one of the loss, one of the rest's cancels where q0 is near p0)
 };
 // What the gradient needs of it, for a CTA.
 struct Brief {
@@ -123,12 +138,6 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Over groups of eight lanes.
-__device__ __forceinline__ float eight_sum(float v) {
-#pragma unroll
-    for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
 template <int kLanes>
 __device__ __forceinline__ Exact joined(Exact x) {
 #pragma unroll
@@ -142,7 +151,7 @@ __device__ __forceinline__ float joined(float& near, float sum, float c1) {
 #pragma unroll
     for (int o = kLanes / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (most == -INFINITY) most = 0.0f;
-    sum = sum == 0.0f ? 0.0f : sum * power_near(near - most, c1);
+    sum = sum == 0.0f ? 0.0f : sum * exp2_fast((near - most) * c1);
 #pragma unroll
     for (int o = kLanes / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     near = most;
@@ -386,7 +395,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         const int entry_warps = min(warps, (a.top + 31) >> 5);
         // in short what the gradient waits for
         Sums* const others = reinterpret_cast<Sums*>(smem + (size_t)shape.granules * 16 + (size_t)a.top * kEntryBytes);   // [ctas][entry_warps], in the first CTA
-        auto brief = [&](int w) { return Brief{warp_sums[w].rest_near, warp_sums[w].rest, warp_sums[w].entries_near, warp_sums[w].entries, warp_sums[w].q.hi}; };
+        auto brief = [&](int w) { return Brief{warp_sums[w].rest_near, warp_sums[w].rest, warp_sums[w].entries_near, warp_sums[w].entries.hi, warp_sums[w].q.hi}; };
         Brief s{};
         if (warps > 8) {
             if (lane < warps) s = brief(lane);
@@ -417,30 +426,41 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             bar_arrive<kFactors>(all_threads);
         }
         if (a.loss && rank == 0) {         // the loss, from all warps' sums: what remains of terms that nearly cancel
-            Exact cross{0.0f, 0.0f}, q{0.0f, 0.0f};
+            Exact cross{0.0f, 0.0f}, q{0.0f, 0.0f}, entries{0.0f, 0.0f};
             const int all_entry_warps = ctas * entry_warps;
             for (int i = lane; i < all_entry_warps; i += 32) {
                 const Sums w = i < entry_warps ? warp_sums[i] : others[i];
                 cross.add(w.cross);
-                if (w.q.hi != 0.0f && w.entries_near != s.entries_near) cross.add_product(-w.q.hi, (w.entries_near - s.entries_near) * a.by);
+                if (w.q.hi != 0.0f && w.entries_near != s.entries_near) add_scaled(cross, w.q, s.entries_near - w.entries_near, a.by, a.by_lo);
                 q.add(w.q);
+                if (w.entries.hi != 0.0f) {
+                    const float factor = power_of(w.entries_near - s.entries_near, a.c1);
+                    entries.add_product(w.entries.hi, factor);
+                    entries.lo += w.entries.lo * factor;
+                }
             }
             if (all_entry_warps > 8) {
                 cross = joined<32>(cross);
                 q = joined<32>(q);
+                entries = joined<32>(entries);
             } else if (all_entry_warps > 1) {
                 cross = joined<8>(cross);
                 q = joined<8>(q);
+                entries = joined<8>(entries);
             }
             if (lane == 0) {
                 Exact total{0.0f, 0.0f};
-                if (s.rest != 0.0f) total.add_product(s.rest, power_near(s.rest_near - all, a.c1));
-                if (s.entries != 0.0f) total.add_product(s.entries, power_near(s.entries_near - all, a.c1));
+                if (s.rest != 0.0f) total.add_product(s.rest, power_of(s.rest_near - all, a.c1));
+                if (entries.hi != 0.0f) {
+                    const float factor = power_of(s.entries_near - all, a.c1);
+                    total.add_product(entries.hi, factor);
+                    total.lo += entries.lo * factor;
+                }
                 const float left = a.teacher_lse && !(s.rest == 0.0f) ? fmaxf(0.0f, (1.0f - q.hi) - q.lo) : 0.0f;
                 const Exact log_total = log_of(total);
                 Exact loss = cross;
                 if (q.hi != 0.0f) {
-                    loss.add_product(q.hi, (all - s.entries_near) * a.by);
+                    add_scaled(loss, q, all - s.entries_near, a.by, a.by_lo);
                     loss.add_product(q.hi, log_total.hi);
                     loss.lo += q.hi * log_total.lo;
                 }
@@ -448,7 +468,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                     const Exact log_rest = log_of(s.rest);
                     Exact d = log_of(left);
                     d.add(Exact{-log_rest.hi, -log_rest.lo});
-                    d.add((all - s.rest_near) * a.by);
+                    add_scaled(d, Exact{1.0f, 0.0f}, all - s.rest_near, a.by, a.by_lo);
                     d.add(log_total);
                     loss.add_product(left, d.hi);
                     loss.lo += left * d.lo;
@@ -580,7 +600,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                     s.cross.add(-d);       // (an entry without any share: an infinite loss; no number stays none)
                 }
             }
-            if (col >= 0) s.entries += exp2_fast(d * a.c1);
+            if (col >= 0) s.entries.add(power_of(d, a.c1));
         }
     }
     // what the powers are relative to: the largest of a granule of every lane, which is seldom far from the largest of all
@@ -605,11 +625,11 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     s.rest = rest * off;
     if (has_entries) {
         if (a.top <= 8) {                  // (lanes without an entry have nothing to join)
-            s.entries = eight_sum(s.entries);
+            s.entries = joined<8>(s.entries);
             s.cross = joined<8>(s.cross);
             s.q = joined<8>(q_sum);
         } else {
-            s.entries = warp_sum(s.entries);
+            s.entries = joined<32>(s.entries);
             s.cross = joined<32>(s.cross);
             s.q = joined<32>(q_sum);
         }
