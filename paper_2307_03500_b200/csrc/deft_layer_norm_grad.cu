@@ -7,11 +7,11 @@
 //
 // Bound by memory: grad_out, x and `add` in, grad_x out, 8 bytes a column for each CTA beside it.  Measured (device time, both
 // launches; floor at the copy rate, 6561 GB/s):
-//   131072 x 1024 bf16, weight sums added     131 us (6.16 TB/s; floor 122.9)
-//   16384 x 1024 bf16, branch                 29.0 us (floor 20.5: two CTAs an SM start, and 296 CTAs' sums are added up)
-//   16384 x 1027 bf16, branch                 39.7 us (a CTA takes rows of one shift of eight; element by element at the edges)
-//   700 x 1500 fp32                           12.3 us (floor 2.6; latency: parameters, rows, join over the cluster)
-//   131072 x 64 bf16                          19.5 us (floor 10.4: a row is a few lanes' work, its reductions and statistics stay)
+//   131072 x 1024 bf16, weight sums added     130 us (6.19 TB/s; floor 122.9)
+//   16384 x 1024 bf16, branch                 27.4 us (floor 20.5: two CTAs an SM start, and 296 CTAs' sums are added up)
+//   16384 x 1027 bf16, branch                 41.6 us (a CTA takes rows of one shift of eight; element by element at the edges)
+//   700 x 1500 fp32                           12.1 us (floor 2.6; latency: parameters, rows, join over the cluster)
+//   131072 x 64 bf16                          17.5 us (floor 7.8: a row is a few lanes' work, its reductions and statistics stay)
 // Two CTAs an SM: the sums of sixteen columns in fp32 pairs, the row and its groups take 128 registers, so that bytes in flight
 // have to come from the ring, not from warps.
 #include <cooperative_groups.h>
@@ -223,8 +223,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
     }
 }
 
-// The CTAs' partial sums added up: a lane per column, sixteen warps that take every sixteenth CTA's.
-constexpr int kJoinWarps = 16;
+// The CTAs' partial sums added up: a lane per column, warps that take every kJoinWarps-th CTA's, whose loads are all under way together
+// (sixteen warps with eight loads at a time: 16384 x 1024 29.0 us for both launches).
+constexpr int kJoinWarps = 32, kJoinLoads = (kPartials + kJoinWarps - 1) / kJoinWarps;
 __global__ void __launch_bounds__(kJoinWarps * 32) k_layer_norm_join(const __grid_constant__ LayerNormGradArgs a, const int partials) {
     __shared__ float part[kJoinWarps][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -232,12 +233,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_layer_norm_join(const __gri
     const int64_t both = 2 * (int64_t)a.cols, at = (int64_t)blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (at < both) {
-#pragma unroll 8
-        for (int p = warp; p < partials; p += kJoinWarps) sum += a.partial[p * both + at];
+        float part_of[kJoinLoads];
+#pragma unroll
+        for (int i = 0; i < kJoinLoads; ++i) part_of[i] = warp + i * kJoinWarps < partials ? a.partial[(warp + i * kJoinWarps) * both + at] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kJoinLoads; ++i) sum += part_of[i];
     }
     part[warp][lane] = sum;
     __syncthreads();
     if (warp || at >= both) return;
+#pragma unroll
     for (int w = 1; w < kJoinWarps; ++w) sum += part[w][lane];
     float* out = at < a.cols ? a.dgamma : a.dbeta;
     if (!out) return;
