@@ -13,6 +13,7 @@ struct LayerNormArgs {
     void *sum, *y;                       // sum: NULL, or x + add in x's type
     const void *gamma, *beta;            // NULL: ones, zeros; of w_type
     float *mean, *rstd;                  // NULL, or [rows]
+    const void* idle;                    // a 16-byte boundary that may be read: the granule in which x begins
     int64_t ld_x, ld_add, ld_sum, ld_y;
     int64_t rows;
     int32_t cols, w_type;
@@ -23,6 +24,7 @@ struct LayerNormGradArgs {
     void* dx;                            // NULL, or of x's type
     const void* gamma;                   // NULL: ones; of w_type
     const float *mean, *rstd;
+    const void* idle;                    // as above
     float *dgamma, *dbeta;               // NULL, or [cols]
     int64_t ld_dy, ld_x, ld_add, ld_dx;
     int64_t rows;

@@ -7,6 +7,9 @@ namespace {
 
 constexpr int64_t kMaxRows = 2147483647LL;
 
+// The 16-byte granule that an address lies in.
+const void* granule_of(const void* p) { return reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15); }
+
 // The elements of a [batch, tokens, heads, dim] tensor in bytes: rows of contiguous columns, dimensions by falling stride.
 struct Boxes {
     uintptr_t base;
@@ -90,6 +93,7 @@ deft_status deft_layer_norm(const void* x_d, int32_t x_type, int64_t ld_x, const
     a.beta = beta_d;
     a.mean = mean_d;
     a.rstd = rstd_d;
+    a.idle = granule_of(x_d);
     a.ld_x = ld_x;
     a.ld_add = ld_add;
     a.ld_sum = ld_sum;
@@ -139,6 +143,7 @@ deft_status deft_layer_norm_grad(const void* grad_out_d, int32_t grad_out_type, 
     a.gamma = gamma_d;
     a.mean = mean_d;
     a.rstd = rstd_d;
+    a.idle = granule_of(x_d);
     a.dgamma = grad_gamma_d;
     a.dbeta = grad_beta_d;
     a.ld_dy = ld_grad_out;

@@ -44,8 +44,8 @@ __global__ void __launch_bounds__(kThreads, kThreads != kTeamThreads ? 1 : (kPla
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(x.group(j), a.x, ring.target(stage, j * kX, kX));
-                if (kAdd) group[j].copy(add.group(j), a.add, ring.target(stage, kAtAdd + j * kX, kX));
+                group[j].copy(x.group(j), a.idle, ring.target(stage, j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), a.idle, ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();

@@ -54,9 +54,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
         if (ahead < rows) {
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
-                group[j].copy(dy.group(j), a.dy, ring.target(stage, j * kD, kD));
-                group[j].copy(x.group(j), a.x, ring.target(stage, kAtX + j * kX, kX));
-                if (kAdd) group[j].copy(add.group(j), a.add, ring.target(stage, kAtAdd + j * kX, kX));
+                group[j].copy(dy.group(j), a.idle, ring.target(stage, j * kD, kD));
+                group[j].copy(x.group(j), a.idle, ring.target(stage, kAtX + j * kX, kX));
+                if (kAdd) group[j].copy(add.group(j), a.idle, ring.target(stage, kAtAdd + j * kX, kX));
             }
         }
         ring.commit();

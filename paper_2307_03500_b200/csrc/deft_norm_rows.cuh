@@ -134,7 +134,8 @@ struct RowGroup {
     }
     template <typename T> using Raw = RawCols<T, kC, kPieces>;
     // `row` points to the group's first column throughout (which may lie before the row).  To shared memory: what lies behind the row's
-    // end becomes zero there (`other`: any address that may be read, for groups that have nothing).
+    // end becomes zero there (`other`: for groups that have nothing; no byte is read there, but a copy's address lies on a 16-byte boundary
+    // all the same).
     template <typename T>
     __device__ __forceinline__ void copy(const T* row, const void* other, uint32_t to) const {
         constexpr int kBytes = kC * (int)sizeof(T);
