@@ -105,9 +105,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
             h[j].from(raw_x);
 #pragma unroll
             for (int i = 0; i < kC / 2; ++i) h[j].p[i] = mul2(add2(h[j].p[i], minus_mean), by);
-            // (what lies behind the row's end has come as zeros: d's are enough for all sums)
-            if (kFeed != Feed::kRing) group[j].clear(h[j]);
-            if (j == 0 || kFeed != Feed::kRing) group[j].clear(d[j]);
+            // What lies behind the row's end has come as zeros, for which d's are enough; what lies before it, in a thread's first group alone,
+            // may be no number and is cleared in both.
+            if (j == 0 || kFeed != Feed::kRing) {
+                group[j].clear(h[j]);
+                group[j].clear(d[j]);
+            }
             if (mine) {
 #pragma unroll
                 for (int i = 0; i < kC / 2; ++i) {

@@ -146,9 +146,10 @@ struct RowGroup {
         else if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
         else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
     }
-    // Of a group that has come through the ring, elements before the row remain to be cleared.
+    // Of a group that has come through the ring, elements before the row remain to be cleared (plain rows begin with a group).
     template <int kN>
     __device__ __forceinline__ void clear(Cols<kN>& v) const {
+        if constexpr (kPlain) return;
         if constexpr (kFeed == Feed::kRing) {
             if (lo > 0) v.trim(lo, kC);
         } else {

@@ -60,3 +60,84 @@ def test_lanes_without_columns(rows, cols, offset, dtype):
     want, dg, db, tol, tol_g, tol_b = plain.layer_norm_grad(dy, x, m.float(), r.float(), None, add)
     plain.close(dx, want, tol)
     plain.close(w, torch.cat([dg, db]), torch.cat([tol_g, tol_b]))
+
+
+BAD = [float("nan"), float("inf"), -float("inf")]
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("rows", [9, 700])             # one cluster, partial sums
+@pytest.mark.parametrize("cols", [1027, 99, 1500])
+@pytest.mark.parametrize("dt,xt", [(BF16, BF16), (F32, F32), (F16, F32)])
+def test_a_bad_row_spoils_no_other_gradient(bad, rows, cols, dt, xt):
+    """The last elements of a row share a granule with the next row's first ones: every other row keeps its bits."""
+    dy, x, add = _rand((rows, cols), dt, 1), _rand((rows, cols), xt, 2, 2.0, 0.5), _rand((rows, cols), xt, 3)
+    gamma = _rand((cols,), F32, 4, 0.3, 1.0)
+    _, _, mean, rstd, *_ = plain.layer_norm(x)
+    mean, rstd = mean.float(), rstd.float()
+    clean, w = _grad(dy, x, mean, rstd, gamma, add)
+    others = torch.arange(rows, device="cuda") != 4
+    for t in (dy, x, add):
+        kept = t[4].clone()
+        t[4, -3:] = bad
+        got, w_got = _grad(dy, x, mean, rstd, gamma, add)
+        t[4] = kept
+        assert torch.equal(got[others], clean[others])
+        assert torch.equal(w_got[:cols - 3], w[:cols - 3]) and torch.equal(w_got[cols:-3], w[cols:-3])
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("rows", [9, 700])
+@pytest.mark.parametrize("pad,offset", [(0, 1), (8, 2), (16, 3), (8, 4), (3, 5), (8, 6), (9, 7), (5, 0)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_what_lies_beside_the_rows(bad, rows, pad, offset, dtype):
+    """Norm and gradient of columns of a wider buffer: the bits do not depend on what the buffer holds beside them."""
+    cols = 331
+    x, add, dy = (_rand((rows, cols), dtype, s) for s in (1, 2, 3))
+    gamma = _rand((cols,), F32, 4, 0.3, 1.0)
+
+    def both(fill):
+        xs, adds, dys = (_placed(t, pad, offset, fill) for t in (x, add, dy))
+        y, s, mean, rstd = _norm(xs, adds, gamma)
+        return [y, s, mean, rstd] + list(_grad(dys, xs, mean, rstd, gamma, adds))
+    clean, got = both(0.0), both(bad)
+    assert all(torch.isfinite(t).all() for t in clean) and all(torch.equal(a, b) for a, b in zip(got, clean))
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradient_beside_its_input(bad, dtype):
+    """x and grad_x as columns of one buffer, which nobody has written yet."""
+    rows, cols = 70, 328
+    x, dy = _rand((rows, cols), dtype, 1), _rand((rows, cols), dtype, 2)
+    _, _, mean, rstd, *_ = plain.layer_norm(x)
+    mean, rstd = mean.float(), rstd.float()
+    buf = torch.full((rows, 2 * cols + 8), bad, dtype=dtype, device="cuda")
+    gx, xs = buf[:, 3:3 + cols], buf[:, 3 + cols:3 + 2 * cols]
+    xs.copy_(x)
+    dys = _placed(dy, cols + 8, 3, bad)
+    got, w = _grad(dys, xs, mean, rstd, grad_x=gx)
+    want, dg, db, tol, tol_g, tol_b = plain.layer_norm_grad(dy, x, mean, rstd)
+    plain.close(got, want, tol)
+    plain.close(w, torch.cat([dg, db]), torch.cat([tol_g, tol_b]))
+    assert torch.equal(xs, x)
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("pad,offset", [(0, 1), (3, 3), (8, 7)])
+def test_distillation_and_rotary_beside_bad_numbers(bad, pad, offset):
+    rows, vocab = 5, 2003
+    z = _rand((rows, vocab), BF16, 1)
+    t, ids = _rand((rows, vocab), F32, 2).topk(6, dim=1)
+    lse = t.logsumexp(1) + 0.5
+    turns = torch.from_numpy(deft.deft_rotary_frequencies(60)).cuda()
+
+    def both(fill):
+        zs, gs = _placed(z, pad, offset, fill), _placed(torch.zeros_like(z), pad, offset, fill)
+        loss = torch.empty(rows, device="cuda")
+        deft.deft_distill(zs, ids, t, loss=loss, grad=gs, teacher_lse=lse)
+        heads = zs[:, :1998].unflatten(1, (3, 666))
+        turned = torch.empty((rows, 3, 666), dtype=BF16, device="cuda")
+        deft.deft_rotary(heads, turned, turns)
+        return loss, gs, turned
+    assert all(torch.isfinite(a).all() and torch.equal(a, b) for a, b in zip(both(0.0), both(bad)))
