@@ -182,7 +182,8 @@ deft_status deft_rotary(const void* x_d, const int64_t* x_strides_h, void* y_d, 
     }
     const Boxes x = boxes_of(x_d, elem, counts, xs, dim), y = boxes_of(y_d, elem, counts, ys, dim);
     if (!nested(y)) return DEFT_ERR_INVALID_ARG;
-    if (!(x.base == y.base && same_layout(x, y))) {
+    // element for element the same place: every dimension's own stride, not the same list of them (a transposition)
+    if (!(x.base == y.base && xs[0] == ys[0] && xs[1] == ys[1] && xs[2] == ys[2])) {
         const bool meeting = x.base < y.base ? y.base - x.base < reach(x, 0) : x.base - y.base < reach(y, 0);
         if (meeting && (!same_layout(x, y) || meet(x, 0, x.base < y.base ? y.base - x.base : x.base - y.base))) return DEFT_ERR_INVALID_ARG;
     }

@@ -141,3 +141,15 @@ def test_distillation_and_rotary_beside_bad_numbers(bad, pad, offset):
         deft.deft_rotary(heads, turned, turns)
         return loss, gs, turned
     assert all(torch.isfinite(a).all() and torch.equal(a, b) for a, b in zip(both(0.0), both(bad)))
+
+
+def test_rotary_in_place_of_transposed_heads():
+    """[batch, heads, tokens, dim] storage with equal numbers of all three, turned where it lies."""
+    x = _rand((6, 6, 6, 40), BF16, 1)
+    turns = torch.from_numpy(deft.deft_rotary_frequencies(40)).cuda()
+    want, tol = plain.rotary(x.transpose(1, 2), turns.cpu().numpy(), torch.arange(6).expand(6, 6))
+    view = x.transpose(1, 2)
+    deft.deft_rotary(view, view, turns)
+    plain.close(view, want, tol)
+    with pytest.raises(deft.DeftError):
+        deft.deft_rotary(view, x, turns)
