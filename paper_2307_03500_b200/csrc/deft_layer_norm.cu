@@ -97,12 +97,12 @@ __global__ void __launch_bounds__(kThreads, kThreads != kTeamThreads ? 1 : (kPla
         if constexpr (kFeed == Feed::kRing) ring.next();
         float2 sums = team.sum(folded(s1), folded(s2));
         float mean = sums.x * each, var = __fmaf_rn(-mean, mean, sums.y * each);
-        // (a warp's teams go the same way)
-        bool far = !(mean * mean <= var);
-        if (team.size < 32) far = __any_sync(0xffffffffu, far);
-        if (far) {
-            const float first = mean;
-            const uint64_t minus = both(-first);
+        // A warp's teams go the same way, but only those that have to keep what the second pass gives: a row's bits depend on
+        // neither its neighbours nor on what teams without a row find.
+        const bool own = mine && !(mean * mean <= var);
+        if (team.size < 32 ? __any_sync(0xffffffffu, own) : own) {
+            const float first = own ? mean : 0.0f;
+            const uint64_t minus = both(-first);         // (v - 0 is v)
             s1 = s2 = 0;
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) {
@@ -118,10 +118,12 @@ __global__ void __launch_bounds__(kThreads, kThreads != kTeamThreads ? 1 : (kPla
                 }
             }
             sums = team.sum(folded(s1), folded(s2));
-            mean = sums.x * each;          // of what is in the registers now
-            var = __fmaf_rn(-mean, mean, sums.y * each);
-            if (var < 0.0f) var = 0.0f;
-            if (team.at == 0 && mine && a.mean) a.mean[r] = first + mean;
+            if (team.at == 0 && mine && a.mean) a.mean[r] = own ? first + sums.x * each : mean;
+            if (own) {
+                mean = sums.x * each;      // of what is in the registers now
+                var = __fmaf_rn(-mean, mean, sums.y * each);
+                if (var < 0.0f) var = 0.0f;
+            }
         } else if (team.at == 0 && mine && a.mean) {
             a.mean[r] = mean;
         }

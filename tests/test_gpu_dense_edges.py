@@ -153,3 +153,36 @@ def test_rotary_in_place_of_transposed_heads():
     plain.close(view, want, tol)
     with pytest.raises(deft.DeftError):
         deft.deft_rotary(view, x, turns)
+
+
+@pytest.mark.parametrize("cols", [16, 40, 48, 100, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [50, 40000])
+def test_short_rows_that_share_a_warp(cols, dtype, rows):
+    """A row's bits do not depend on whether its neighbours take the second pass for their variance."""
+    x = _rand((rows, cols), dtype, 1, 1.0, 0.3)
+    y, _, mean, rstd = _norm(x)
+    for row, change in ((3, 100.0), (7, float("nan")), (30, float("inf"))):
+        other = x.clone()
+        other[row] += change
+        got = _norm(other)
+        kept = torch.arange(rows, device="cuda") != row
+        for a, b in ((got[0], y), (got[2], mean), (got[3], rstd)):
+            assert torch.equal(a[kept], b[kept]), "other bits"
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 48), (1, 16), (5, 100), (9, 24)])
+@pytest.mark.parametrize("odd", [False, True])
+def test_few_short_rows_after_other_calls(rows, cols, odd):
+    """Teams without a row have no say: the same bits whatever the shared memory and the registers hold."""
+    x = _rand((rows, cols), F32, 1, 1.0, 0.4)
+    first = None
+    for seed in range(12):
+        far = _rand((20000, cols), F32, seed, 1.0, 1000.0 if seed % 2 else 0.0)
+        _norm(_placed(far, 1, 0, 0.0) if odd else far)
+        y = torch.empty(rows * cols + 1, device="cuda")[1:].view(rows, cols) if odd else torch.empty((rows, cols), device="cuda")   # (odd: no shift serves both)
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        deft.deft_layer_norm(x, y, mean=mean, rstd=rstd)
+        got = [y.clone(), mean, rstd]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first)), "other bits"
