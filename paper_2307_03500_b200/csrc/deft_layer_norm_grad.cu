@@ -26,6 +26,13 @@ constexpr int kPartials = 2 * 148;   // CTAs that leave partial sums at most; a 
 
 template <typename TD, typename TX> constexpr int kColsOf = sizeof(TD) == 4 || sizeof(TX) == 4 ? 4 : 8;
 
+// A column's sum to its place: scaled and rounded, and then (accumulate) added, not both in one operation: what is added is what would
+// be written.
+__device__ __forceinline__ void store_sum(const LayerNormGradArgs& a, float* out, float sum) {
+    sum = __fmul_rn(sum, a.scale);
+    *out = a.accumulate ? __fadd_rn(*out, sum) : sum;
+}
+
 template <bool kAdd, typename TD, typename TX, Feed kFeed, int kGroups, int kThreads, bool kPlain>
 __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_layer_norm_grad(const __grid_constant__ LayerNormGradArgs a, const __grid_constant__ TeamShape shape) {
     extern __shared__ __align__(16) char smem[];         // gamma and room for a second vector (at the end the CTA's sums), the ring
@@ -211,8 +218,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == kTeamThreads ? 2 : 1) k_
             }
             float* out = second ? a.dbeta : a.dgamma;
             if (!out) continue;
-            sum *= a.scale;
-            out[c] = a.accumulate ? out[c] + sum : sum;
+            store_sum(a, out + c, sum);
         }
         cluster.sync();                    // nobody leaves while others read its sums
         return;
@@ -250,8 +256,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_layer_norm_join(const __gri
     float* out = at < a.cols ? a.dgamma : a.dbeta;
     if (!out) return;
     out += at < a.cols ? at : at - a.cols;
-    sum *= a.scale;
-    *out = a.accumulate ? *out + sum : sum;
+    store_sum(a, out, sum);
 }
 
 }  // namespace

@@ -186,3 +186,17 @@ def test_few_short_rows_after_other_calls(rows, cols, odd):
         got = [y.clone(), mean, rstd]
         first = first or got
         assert all(torch.equal(a, b) for a, b in zip(got, first)), "other bits"
+
+
+@pytest.mark.parametrize("rows,cols", [(9, 1024), (700, 1024), (30, 331), (3000, 64), (700, 1500)])
+@pytest.mark.parametrize("scale", [-0.37, 1.0 / 3.0, 1.0])
+def test_accumulation_is_one_rounded_addition(rows, cols, scale):
+    """What is added is what would be written: before + written, rounded once."""
+    x, dy = _rand((rows, cols), F32, 1), _rand((rows, cols), F32, 2)
+    _, _, mean, rstd, *_ = plain.layer_norm(x)
+    mean, rstd = mean.float(), rstd.float()
+    _, written = _grad(dy, x, mean, rstd, scale=scale)
+    before = _rand((2 * cols,), F32, 3)
+    added = before.clone()
+    deft.deft_layer_norm_grad(dy, x, mean, rstd, grad_gamma=added[:cols], grad_beta=added[cols:], ws=deft.alloc_layer_norm_workspace(rows, cols), accumulate=True, scale=scale)
+    assert torch.equal(added, before + written)
