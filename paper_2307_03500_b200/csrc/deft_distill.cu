@@ -550,10 +550,13 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     T* const e = reinterpret_cast<T*>(smem) - base;
-    if (tid == 0)                          // what the first and last granule hold beside the row
+    // what the first and last granule hold beside the row, marked by whoever has copied them: behind the barrier an entry's element may
+    // be taken out of the same word
+    if (tid == 0)
         for (int c = base; c < 0; ++c) e[c] = lowest<T>();
+    if (n > 0 && tid == ((n - 1) & (threads - 1)))     // (a power of two)
+        for (int c = max(a.vocab, base); c < base + n * kPer; ++c) e[c] = lowest<T>();
     bar_row<kMost>(threads);
-    for (int c = max(a.vocab, base) + tid; c < base + n * kPer; c += threads) e[c] = lowest<T>();
     Sums s{};
     if (has_entries) {
         for (int j = tid; j < a.top; j += threads) {

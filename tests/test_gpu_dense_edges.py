@@ -200,3 +200,20 @@ def test_accumulation_is_one_rounded_addition(rows, cols, scale):
     added = before.clone()
     deft.deft_layer_norm_grad(dy, x, mean, rstd, grad_gamma=added[:cols], grad_beta=added[cols:], ws=deft.alloc_layer_norm_workspace(rows, cols), accumulate=True, scale=scale)
     assert torch.equal(added, before + written)
+
+
+@pytest.mark.parametrize("vocab", [1001, 2003, 30011, 60013])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("offset", range(8))
+def test_entries_at_both_ends_of_the_row(vocab, dtype, offset):
+    """The row's first and last elements share words and granules with what does not belong to it."""
+    rows, top = 6, 24
+    z = _placed(_rand((rows, vocab), dtype, 1, 2.0), 0, offset, 5.0)
+    ids = torch.cat([torch.arange(vocab - 16, vocab), torch.arange(8)]).flip(0).expand(rows, top).contiguous().cuda()
+    t = _rand((rows, top), F32, 2, 2.0)
+    loss, grad = torch.empty(rows, device="cuda"), _placed(torch.zeros_like(z), 0, offset, 7.0)
+    for lse in (None, t.logsumexp(1) + 1.0):
+        deft.deft_distill(z, ids, t, loss=loss, grad=grad, teacher_lse=lse)
+        want, want_g, tol, tol_g = plain.distill(z, ids, t, lse)
+        plain.close(loss, want, tol)
+        plain.close(grad, want_g, tol_g)
