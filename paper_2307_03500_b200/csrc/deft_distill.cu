@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     __shared__ Sums warp_sums[kMost / 32];
     __shared__ Brief briefs[kMostCluster];
     __shared__ Factors factors;
-    __shared__ int twice;                  // the last row in which an entry found nothing in its place: another one's column, or -inf
+    __shared__ volatile int twice;         // the last row in which an entry found nothing in its place: another one's column, or -inf (several threads may say so)
     const int ctas = shape.ctas, threads = shape.threads, warps = threads >> 5, all_threads = threads + 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int rank = 0;
@@ -577,10 +577,10 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                 const int col = entry.col[j];
                 bool earlier = false;
                 for (int m = 0; m < j && col >= 0; ++m) {
-                    const int other = *reinterpret_cast<volatile int*>(entry.col + m);      // (may have become -3 - column meanwhile)
+                    const int other = *const_cast<volatile int*>(entry.col + m);      // (may have become -3 - column meanwhile)
                     earlier |= other == col || other == -3 - col;
                 }
-                if (earlier) entry.col[j] = -3 - col;
+                if (earlier) *const_cast<volatile int*>(entry.col + j) = -3 - col;
             }
         }
         float most = -INFINITY;
