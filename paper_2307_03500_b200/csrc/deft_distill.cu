@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
     if (has_entries) {
         float near = 0.0f;
         if (!a.teacher_lse) {              // every warp goes through all entries
-            float most = -INFINITY, sum = 0.0f;
+            float most = -INFINITY;
             for (int j = lane; j < a.top; j += 32) {
                 const RawEntry e = entry_at(a, row, j);
                 if (column_of(a, e) >= 0) most = fmaxf(most, value_of(a, e.t));
@@ -526,12 +526,13 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             most = warp_max(most);
             if (most != -INFINITY) {
                 near = most;
+                Exact sum{0.0f, 0.0f};     // (what it is off by is an error of the loss)
                 for (int j = lane; j < a.top; j += 32) {
                     const RawEntry e = entry_at(a, row, j);
                     const float d = value_of(a, e.t) - near;
-                    if (column_of(a, e) >= 0) sum += expf(scaled(d, a.it_hi, a.it_lo, 0.0f));
+                    if (column_of(a, e) >= 0) sum.add(expf(scaled(d, a.it_hi, a.it_lo, 0.0f)));
                 }
-                norm = log_of(warp_sum(sum));
+                norm = log_of(joined<32>(sum));
             }
         }
         for (int j = tid; j < a.top; j += threads) {

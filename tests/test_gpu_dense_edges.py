@@ -217,3 +217,19 @@ def test_entries_at_both_ends_of_the_row(vocab, dtype, offset):
         want, want_g, tol, tol_g = plain.distill(z, ids, t, lse)
         plain.close(loss, want, tol)
         plain.close(grad, want_g, tol_g)
+
+
+@pytest.mark.parametrize("vocab", [1024, 40000])
+@pytest.mark.parametrize("first", [0, 700])
+def test_normaliser_of_one_large_and_many_small_entries(vocab, first):
+    """A student that agrees with the teacher: 1 and 1023 times e^-17, each below half a step of 1.  The loss is 0; what an entry's power,
+    its logarithm or a probability is off by (at most 2^-21 and 17 times 2^-24 relative) counts by the small entries' share of
+    4.3e-5 alone, which makes 1e-10.  Terms lost from the sum of the powers would make up to 1.3e-6."""
+    t = torch.full((3, 1024), -17.0, device="cuda")
+    t[:, first] = 0.0
+    z = torch.full((3, vocab), -float("inf"), device="cuda")
+    z[:, :1024] = t
+    ids = torch.arange(1024, device="cuda").expand(3, 1024).contiguous()
+    loss = torch.empty(3, device="cuda")
+    deft.deft_distill(z, ids, t, loss=loss)
+    assert loss.abs().max().item() <= 1e-9
