@@ -67,10 +67,10 @@ __device__ __forceinline__ Exact log_prob(float d, float hi, float lo, Exact nor
     y.lo += d * lo;
     return y;
 }
-// d (hi + lo) + c, likewise.
-__device__ __forceinline__ float scaled(float d, float hi, float lo, float c) {
-    const float y = __fmaf_rn(d, hi, c);
-    return isfinite(d) ? __fmaf_rn(d, lo, y) : y;
+// e to the power of both pieces: a piece that the argument's rounding would lose is a relative error of the probability.
+__device__ __forceinline__ float exp_of(Exact x) {
+    const float y = expf(x.hi);
+    return x.lo != 0.0f ? __fmaf_rn(y, x.lo, y) : y;
 }
 // The natural logarithm of a positive number: its exponent's part with ln 2 in two pieces, the first of which times an exponent is
 // exact (Cody and Waite), and the logarithm of the rest, which lies in [sqrt(1/2), sqrt(2)).
@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                 for (int j = lane; j < a.top; j += 32) {
                     const RawEntry e = entry_at(a, row, j);
                     const float d = value_of(a, e.t) - near;
-                    if (column_of(a, e) >= 0) sum.add(expf(scaled(d, a.it_hi, a.it_lo, 0.0f)));
+                    if (column_of(a, e) >= 0) sum.add(exp_of(log_prob(d, a.it_hi, a.it_lo, Exact{0.0f, 0.0f})));
                 }
                 norm = log_of(joined<32>(sum));
             }
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             const int col = column_of(a, raw);
             const bool valid = col >= 0;
             const Exact log_q = log_prob(value_of(a, raw.t) - near, a.it_hi, a.it_lo, norm);
-            const float q = valid ? expf(log_q.hi + log_q.lo) : 0.0f;
+            const float q = valid ? exp_of(log_q) : 0.0f;
             const bool here = valid && col >= base && col < base + n * kPer;
             entry.col[j] = valid && !here ? -2 : col;
             entry.log_q[j] = log_q.hi;

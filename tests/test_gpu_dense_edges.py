@@ -233,3 +233,20 @@ def test_normaliser_of_one_large_and_many_small_entries(vocab, first):
     loss = torch.empty(3, device="cuda")
     deft.deft_distill(z, ids, t, loss=loss)
     assert loss.abs().max().item() <= 1e-9
+
+
+def test_probabilities_of_arguments_between_two_numbers():
+    """The teacher's log q = t - lse lies 4.5e-7 beside an fp32 number, almost half a step (4.8e-7) off: the probabilities hold it all the same.
+    An error of d relative in all of them is one of 4.7 d in the loss of 4.41 (0.249 of the mass, 18.6 between the logarithms, 0.29
+    of the rest's).  Allowed: expf's unit in the last place, 2^-24 relative as e^-8.3228 lies just below a power of two, and half a
+    unit of the product's, 4.7 times 9e-8; the student's exponents of 20 times 1.4e-8 (log2(e) in fp32) on 0.249, 7e-8; the
+    result's own rounding, 2.4e-7: 8e-7.  Without the smaller piece the loss is 4.7 times 4.5e-7 = 2.1e-6 off."""
+    t = torch.full((2, 1024), 4.5e-7, device="cuda")
+    lse = torch.full((2,), 8.32278, device="cuda")
+    z = torch.zeros((2, 2024), device="cuda")
+    z[:, :1024] = -20.0
+    ids = torch.arange(1024, device="cuda").expand(2, 1024).contiguous()
+    loss = torch.empty(2, device="cuda")
+    deft.deft_distill(z, ids, t, loss=loss, teacher_lse=lse)
+    want = plain.distill(z, ids, t, lse)[0]
+    assert (loss.double().cpu() - want).abs().max().item() <= 8e-7
