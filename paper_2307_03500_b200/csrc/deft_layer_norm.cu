@@ -167,11 +167,13 @@ deft_status launch_layer_norm(const LayerNormArgs& a, int x_type, int y_type, cu
             m.add(a.add, a.ld_add, sizeof(TX));
             m.add(a.sum, a.ld_sum, sizeof(TX));
             const TeamShape s = team_shape(m, a.rows, a.cols, (int)sizeof(TX) * (a.add ? 2 : 1), 2, 3, 4, 0, 0, true);
-            return with_shape<kC, true>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
+            return with_shape<kC, sizeof(TX) == 2>(s, [&](auto feed, auto groups, auto threads, auto plain) -> deft_status {
                 constexpr Feed kFeed = decltype(feed)::value;
                 constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                 constexpr bool kPlain = decltype(plain)::value;
-                auto kernel = a.add ? k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads, kPlain> : k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads, kPlain>;
+                auto kernel = k_layer_norm<false, TX, TY, kFeed, kGroups, kThreads, kPlain>;
+                if constexpr (kGroups * kC != 24)        // (24 columns a thread: of one 16-bit matrix)
+                    if (a.add) kernel = k_layer_norm<true, TX, TY, kFeed, kGroups, kThreads, kPlain>;
                 if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
                 kernel<<<s.blocks, s.threads, s.smem, stream>>>(a, s);
                 DEFT_CUDA_TRY(cudaGetLastError());

@@ -287,7 +287,12 @@ deft_status launch_layer_norm_grad(const LayerNormGradArgs& a, int dy_type, int 
                     constexpr Feed kFeed = decltype(feed)::value;
                     constexpr int kGroups = decltype(groups)::value, kThreads = decltype(threads)::value;
                     constexpr bool kPlain = decltype(plain)::value;
-                    auto kernel = a.add ? k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads, kPlain> : k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads, kPlain>;
+                    // a ring of rows beyond 8192 columns: of three matrices it has room for a stage where x and `add` have 16 bits
+                    constexpr bool kAddToo = kFeed != Feed::kRing || kGroups * kC != 32 || sizeof(TX) == 2;
+                    auto kernel = k_layer_norm_grad<false, TD, TX, kFeed, kGroups, kThreads, kPlain>;
+                    if constexpr (kAddToo)
+                        if (a.add) kernel = k_layer_norm_grad<true, TD, TX, kFeed, kGroups, kThreads, kPlain>;
+                    static_assert(kAddToo || kTeamMost * 32 * (sizeof(TD) + 2 * sizeof(TX)) + 2 * sizeof(float) * kTeamMost * 16 > kMostSmem, "no stage fits");
                     if (s.smem > 40 * 1024) DEFT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
                     joined = s.joined;
                     if (joined) {

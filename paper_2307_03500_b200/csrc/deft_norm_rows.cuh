@@ -59,7 +59,7 @@ struct Shifts {
 // CTAs of kTeamThreads threads with up to sixteen columns each that an SM holds (per_sm_plain: without tests); most_blocks: of the launch (0: as many as the device holds).
 // Rows of up to 8192 columns have sixteen columns a thread (their registers leave room for enough warps), longer ones 32; from 4096
 // columns on a CTA has a row at a time and an SM one CTA, whose parameters and ring fill its shared memory.
-// three: threads may have 24 columns, where that takes fewer of them for a row (768 columns: one warp, no lane idle; 17 -> 15 us at
+// three: threads may have 24 columns of one 16-bit matrix, where that takes fewer of them for a row (768 columns: one warp, no lane idle; 17 -> 15 us at
 // 16384 rows) and the ring still has two stages.
 // join_turns: the call is one cluster of up to kMostJoined CTAs where a team then takes no more rows than that (0: never).
 inline TeamShape team_shape(const Shifts& m, int64_t rows, int cols, int row_bytes, int params, int per_sm, int per_sm_plain, int64_t most_blocks, int join_turns, bool three) {
