@@ -250,3 +250,50 @@ def test_probabilities_of_arguments_between_two_numbers():
     deft.deft_distill(z, ids, t, loss=loss, teacher_lse=lse)
     want = plain.distill(z, ids, t, lse)[0]
     assert (loss.double().cpu() - want).abs().max().item() <= 8e-7
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("cols", [4099, 8201, 16381])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_long_rows_beside_bad_numbers(bad, cols, dtype):
+    """Rows of one CTA, with the ring and (fp32, three matrices) without: a bad row and a gap of bad numbers reach no other row."""
+    rows = 40
+    x, add, dy = (_rand((rows, cols), dtype, s) for s in (1, 2, 3))
+    gamma = _rand((cols,), F32, 4, 0.3, 1.0)
+
+    def both(fill, row):
+        xs, adds, dys = (_placed(t, 3, 5, fill) for t in (x, add, dy))
+        y, s, mean, rstd = _norm(xs, adds, gamma)
+        xs[row] = fill
+        return [y, s, mean, rstd] + list(_grad(dys, xs, mean, rstd, gamma, adds))
+    clean, got = both(0.0, 7), both(bad, 7)
+    others = torch.arange(rows, device="cuda") != 7
+    assert all(torch.equal(a, b) for a, b in zip(clean[:4], got[:4]))
+    assert torch.isfinite(clean[4]).all() and torch.equal(clean[4][others], got[4][others])
+
+
+def test_every_kernel_twice_at_once():
+    """Two streams, each with its own workspace and outputs: the same bits as one after the other."""
+    rows, cols, vocab = 3000, 520, 5003
+
+    def calls(seed, stream):
+        with torch.cuda.stream(stream):
+            x, add, dy = (_rand((rows, cols), BF16, seed + s) for s in (1, 2, 3))
+            y, s, mean, rstd = _norm(x, add)
+            dx, w = _grad(dy, s, mean, rstd, add=add)
+            z = _rand((rows, vocab), BF16, seed)
+            t, ids = z.float().topk(9, dim=1)
+            loss, grad = torch.empty(rows, device="cuda"), torch.empty_like(z)
+            deft.deft_distill(z, ids, t, loss=loss, grad=grad, teacher_lse=z.float().logsumexp(1))
+            turned = torch.empty((rows, 8, 65), dtype=BF16, device="cuda")
+            deft.deft_rotary(y.view(rows, 8, 65), turned, torch.from_numpy(deft.deft_rotary_frequencies(64)).cuda())
+        return [y, s, mean, rstd, dx, w, loss, grad, turned]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    want = []
+    for seed in (10, 20):
+        want.append(calls(seed, streams[0]))
+        torch.cuda.synchronize()
+    for _ in range(5):
+        got = [calls(seed, s) for seed, s in zip((10, 20), streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, v in zip(got, want) for a, b in zip(g, v))
