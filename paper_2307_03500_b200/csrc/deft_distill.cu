@@ -72,31 +72,14 @@ __device__ __forceinline__ float exp_of(Exact x) {
     const float y = expf(x.hi);
     return x.lo != 0.0f ? __fmaf_rn(y, x.lo, y) : y;
 }
-// The natural logarithm of a positive number: its exponent's part with ln 2 in two pieces, the first of which times an exponent is
-// exact (Cody and Waite), and the logarithm of the rest, which lies in [sqrt(1/2), sqrt(2)).
-__device__ __forceinline__ Exact log_of(float x) {
-    if (!(x > 0.0f && x < INFINITY)) return Exact{logf(x), 0.0f};
-    int e = 0;
-    if (x < 1.17549435e-38f) x *= 16777216.0f, e = -24;
-    const int bits = __float_as_int(x) - 0x3f3504f3;          // of sqrt(1/2)
-    e += bits >> 23;
-    Exact y{(float)e * 0.693145751953125f, (float)e * 1.42860682030941723212e-6f};
-    y.add(logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3)));
-    return y;
-}
-// x (hi + lo) times a weight, added to a sum.
-__device__ __forceinline__ void add_scaled(Exact& sum, Exact weight, float x, float hi, float lo) {
-    const float p = __fmul_rn(x, hi), rest = __fmaf_rn(x, hi, -p) + x * lo;
-    sum.add_product(weight.hi, p);
-    sum.lo += weight.hi * rest + weight.lo * p;
+// (where it is infinite, what its roundings have left out is no number)
+__device__ __forceinline__ double value_of(Exact x) { return isfinite(x.hi) ? (double)x.hi + (double)x.lo : (double)x.hi; }
+__device__ __forceinline__ Exact log_of(Exact x) {
+    const double y = log(value_of(x));
+    const float hi = (float)y;
+    return Exact{hi, isfinite(hi) ? (float)(y - (double)hi) : 0.0f};
 }
 __device__ __forceinline__ Exact shuffled(Exact x, int o) { return Exact{__shfl_xor_sync(0xffffffffu, x.hi, o), __shfl_xor_sync(0xffffffffu, x.lo, o)}; }
-
-__device__ __forceinline__ Exact log_of(Exact x) {
-    Exact y = log_of(x.hi);
-    if (x.lo != 0.0f && x.hi > 0.0f && x.hi < INFINITY) y.lo += x.lo / x.hi;
-    return y;
-}
 
 // 2^(d c1) for d <= 0 to a unit in the last place, the argument's rounding made good: a polynomial of degree six on [-1/2, 1/2], fitted for the least relative error (2e-9).
 __device__ __forceinline__ float power_of(float d, float c1) {
@@ -137,6 +120,12 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
+}
+template <int kLanes>
+__device__ __forceinline__ double joined(double x) {
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
 }
 template <int kLanes>
 __device__ __forceinline__ Exact joined(Exact x) {
@@ -425,19 +414,17 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
             if (lane == 0) factors = Factors{all, s.rest_near, (s.q + left) / total * f, left > 0.0f ? left / s.rest * f : 0.0f};
             bar_arrive<kFactors>(all_threads);
         }
-        if (a.loss && rank == 0) {         // the loss, from all warps' sums: what remains of terms that nearly cancel
-            Exact cross{0.0f, 0.0f}, q{0.0f, 0.0f}, entries{0.0f, 0.0f};
+        if (a.loss && rank == 0) {         // the loss, from all warps' sums: what remains of terms that nearly cancel, in 64 bits
+            const double c1 = a.c1, by = (double)a.by + (double)a.by_lo;
+            double cross = 0.0, q = 0.0, entries = 0.0;
             const int all_entry_warps = ctas * entry_warps;
             for (int i = lane; i < all_entry_warps; i += 32) {
                 const Sums w = i < entry_warps ? warp_sums[i] : others[i];
-                cross.add(w.cross);
-                if (w.q.hi != 0.0f && w.entries_near != s.entries_near) add_scaled(cross, w.q, s.entries_near - w.entries_near, a.by, a.by_lo);
-                q.add(w.q);
-                if (w.entries.hi != 0.0f) {
-                    const float factor = power_of(w.entries_near - s.entries_near, a.c1);
-                    entries.add_product(w.entries.hi, factor);
-                    entries.lo += w.entries.lo * factor;
-                }
+                const double near = (double)w.entries_near - (double)s.entries_near, of_warp = value_of(w.q);
+                cross += value_of(w.cross);
+                if (near != 0.0) cross -= of_warp * (near * by);
+                q += of_warp;
+                if (w.entries.hi != 0.0f) entries += near != 0.0 ? value_of(w.entries) * exp2(near * c1) : value_of(w.entries);
             }
             if (all_entry_warps > 8) {
                 cross = joined<32>(cross);
@@ -449,32 +436,16 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                 entries = joined<8>(entries);
             }
             if (lane == 0) {
-                Exact total{0.0f, 0.0f};
-                if (s.rest != 0.0f) total.add_product(s.rest, power_of(s.rest_near - all, a.c1));
-                if (entries.hi != 0.0f) {
-                    const float factor = power_of(s.entries_near - all, a.c1);
-                    total.add_product(entries.hi, factor);
-                    total.lo += entries.lo * factor;
-                }
-                const float left = a.teacher_lse && !(s.rest == 0.0f) ? fmaxf(0.0f, (1.0f - q.hi) - q.lo) : 0.0f;
-                const Exact log_total = log_of(total);
-                Exact loss = cross;
-                if (q.hi != 0.0f) {
-                    add_scaled(loss, q, all - s.entries_near, a.by, a.by_lo);
-                    loss.add_product(q.hi, log_total.hi);
-                    loss.lo += q.hi * log_total.lo;
-                }
-                if (left > 0.0f) {
-                    const Exact log_rest = log_of(s.rest);
-                    Exact d = log_of(left);
-                    d.add(Exact{-log_rest.hi, -log_rest.lo});
-                    add_scaled(d, Exact{1.0f, 0.0f}, all - s.rest_near, a.by, a.by_lo);
-                    d.add(log_total);
-                    loss.add_product(left, d.hi);
-                    loss.lo += left * d.lo;
-                }
-                // (where a term is infinite, what its roundings have left out is no number)
-                a.loss[row] = (isfinite(loss.hi) ? loss.hi + loss.lo : loss.hi) * weight * a.loss_factor;
+                // of the rest and of the entries one lies at `all`
+                const double to_rest = (double)all - (double)s.rest_near, to_entries = (double)all - (double)s.entries_near;
+                double total = 0.0;
+                if (s.rest != 0.0f) total += to_rest != 0.0 ? s.rest * exp2(-to_rest * c1) : (double)s.rest;
+                if (entries != 0.0) total += to_entries != 0.0 ? entries * exp2(-to_entries * c1) : entries;
+                const double log_total = log(total), left = a.teacher_lse && !(s.rest == 0.0f) ? 1.0 - q : 0.0;
+                double loss = cross;
+                if (q != 0.0) loss += q * (to_entries * by + log_total);
+                if (left > 0.0) loss += left * (log(left) - log((double)s.rest) + to_rest * by + log_total);
+                a.loss[row] = (float)(loss * weight * a.loss_factor);
             }
         }
         return;

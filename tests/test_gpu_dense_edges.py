@@ -297,3 +297,21 @@ def test_every_kernel_twice_at_once():
         got = [calls(seed, s) for seed, s in zip((10, 20), streams)]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for g, v in zip(got, want) for a, b in zip(g, v))
+
+
+@pytest.mark.parametrize("gap", [0.3, 0.7, 1.1, 2.3, -0.9])
+@pytest.mark.parametrize("temperature", [1.0, 4.0])
+def test_loss_that_is_left_of_logarithms_that_cancel(gap, temperature):
+    """Student and teacher agree on eight entries and the rest of 2000 columns: what is left of the logarithms is T^2 times what the entries'
+    probabilities are off by, at most 2^-23 and 2^-24 relative on their share (below 0.05), 1.8e-7 times 0.05, and what the rest's
+    sum is off by, 2^-22, times the difference of the rest's probabilities, which is of the same size: 1e-8 T^2.  A logarithm or a
+    power in fp32 would be off by up to 6e-8 T^2 itself."""
+    z = torch.zeros((3, 2000), device="cuda")
+    z[:, 5:13] = gap
+    ids = torch.arange(5, 13, device="cuda").expand(3, 8).contiguous()
+    t = z[:, 5:13].contiguous()
+    lse = torch.logsumexp(z.double() / temperature, 1).float()
+    loss = torch.empty(3, device="cuda")
+    deft.deft_distill(z, ids, t, loss=loss, teacher_lse=lse, temperature=temperature)
+    want = plain.distill(z, ids, t, lse, temperature=temperature)[0]
+    assert (loss.double().cpu() - want).abs().max().item() <= 1e-8 * temperature ** 2
