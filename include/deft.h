@@ -560,9 +560,11 @@ DEFT_API deft_status deft_dropout(const void* x_d, int32_t x_type, int64_t ld_x,
 /* ------------------------------------------------------------------------------------------
  * Dense row operators: what lies between a language model's lookup and its loss, as far as it is no contraction.  The
  * conventions are those of the row operators above (matrices with a pitch, any element alignment, whole 16-byte granules
- * read, elements alone written, fp32 arithmetic, one rounding at the end).  Rows whose matrices start on the same
+ * read, elements alone written, fp32 arithmetic, one rounding at the end).  What lies beside a row or in other rows does not reach
+ * its results, infinities and NaN included.  Rows whose matrices start on the same
  * place of a 16-byte granule in every matrix of a call (equal offsets and pitches modulo 8 elements; contiguous ones do) are
- * fastest.  Small vectors (weights, statistics, losses, sums) must not overlap anything the call writes.
+ * fastest: layer norm and its gradient take three to five times as long where they do not.  Small vectors (weights, statistics,
+ * losses, sums) must not overlap anything the call writes.
  * ---------------------------------------------------------------------------------------- */
 
 /*
@@ -575,6 +577,7 @@ DEFT_API deft_status deft_dropout(const void* x_d, int32_t x_type, int64_t ld_x,
  *   y_d       [rows, cols], y_type
  *   mean_d, rstd_d   NULL, or [rows] fp32: m and r for the gradient
  * sum and y may be x or add, element for element (same type and pitch); otherwise, and from each other, they are apart.
+ * A row's squares have to lie, and to add up, within fp32's range (beyond it the variance is infinite and y beta; below it, 0).
  * Errors: INVALID_ARG (eps negative or not finite), TOO_LARGE (cols beyond DEFT_NORM_MAX_COLS, rows beyond 2^31 - 1), CUDA.
  */
 DEFT_API deft_status deft_layer_norm(const void* x_d, int32_t x_type, int64_t ld_x, const void* add_d, int64_t ld_add,
@@ -591,8 +594,8 @@ DEFT_API deft_status deft_layer_norm(const void* x_d, int32_t x_type, int64_t ld
  *   add_d      NULL, or [rows, cols] of x_type: the gradient that reaches x past the norm
  *   grad_x_d   NULL (not wanted), or [rows, cols] of x_type; may be grad_out, x or add, element for element
  *   grad_gamma_d, grad_beta_d  NULL (not wanted), or [cols] fp32: usually their parts of the flat vector.  accumulate = 0:
- *              written; accumulate != 0: added, one fp32 round-to-nearest add per element (the residual, or a
- *              gradient vector that holds other shares).  Sums are fp32 in a fixed order: the same bits on every call.
+ *              written; accumulate != 0: what would be written is added, one fp32 round-to-nearest add per element (the residual,
+ *              or a gradient vector that holds other shares).  Sums are fp32 in a fixed order: the same bits on every call.
  *   scale      finite in fp32; of these two alone
  *   ws_d       deft_layer_norm_workspace_bytes(rows, cols), 256-byte aligned; NULL where neither of the two is wanted.
  *              Holds nothing between calls; calls that share it must not overlap on the GPU.  Enough for fewer rows and columns.
@@ -631,7 +634,7 @@ DEFT_API deft_status deft_rotary_frequencies(int32_t rot, double base, int32_t s
  *   inverse      != 0: angles negated, which is the gradient (of the same gain)
  *   gain         finite in fp32
  *   pos_d        NULL (a token's number within its batch), or [batch * tokens] int32 or int64 (pos_bytes 4 or 8)
- * y may be x, element for element (what is copied stays); otherwise they are apart.  x may repeat elements (stride 0), y not.
+ * y may be x, element for element, with x's strides (what is copied stays); otherwise they are apart.  x may repeat elements (stride 0), y not.
  * Errors: INVALID_ARG (also: outputs that overlap each other, or x without being it; strides that differ between the
  * two count as overlapping where their ranges of memory meet), TOO_LARGE (batch * tokens beyond 2^31 - 1, heads * dim
  * beyond 2^30, rot beyond DEFT_ROTARY_MAX_ROT), CUDA.
@@ -657,6 +660,7 @@ DEFT_API deft_status deft_rotary(const void* x_d, const int64_t* x_strides_h, vo
  *   teacher_d [rows, top], teacher_type
  *   weight_d  NULL (ones), or [rows] fp32: of a row of weight 0 nothing is read, its loss and gradient are 0
  *   loss_d    NULL, or [rows] fp32;  scale: of the gradient alone, finite in fp32 (and times the temperature)
+ * The loss, which is what is left of logarithms that nearly cancel, is formed in two fp32 pieces and 64 bits.
  * An entry with q_j = 0 (t_j = -inf) adds nothing; a row without entries of any q has loss 0 and, without teacher_lse, gradient
  * 0.  Sums run in a fixed order: the same bits on every call.
  * Errors: INVALID_ARG (neither loss nor grad, temperature outside [1e-6, 1e6]), TOO_LARGE (rows beyond 2^28 - 1, vocab beyond

@@ -2,18 +2,25 @@
 //
 // With h = (x - mean) rstd and d = dy gamma:  dx = rstd (d - mean(d) - h mean(d h)) + add, one pass over the row's registers,
 // two sums.  The weight sums dy h and dy stay in registers over all rows of a thread's columns; they leave the CTA once as
-// partial sums, and a second kernel adds those in a fixed order: the same bits on every call.  The CTAs of a call of few rows are a
-// cluster instead and add up each other's sums where they lie (the second launch took a fifth of the call's time).
+// partial sums, and a second kernel adds those in a fixed order: the same bits on every call.  The CTAs of a call of few rows (eight
+// CTAs' teams with up to four rows each: 64 rows of 1024 columns, 32 of 1500) are a cluster instead and add up each other's
+// sums where they lie (the second launch took a fifth of such a call's time).
 //
 // Bound by memory: grad_out, x and `add` in, grad_x out, 8 bytes a column for each CTA beside it.  Measured (device time, both
 // launches; floor at the copy rate, 6561 GB/s):
 //   131072 x 1024 bf16, weight sums added     130 us (6.19 TB/s; floor 122.9)
-//   16384 x 1024 bf16, branch                 27.4 us (floor 20.5: two CTAs an SM start, and 296 CTAs' sums are added up)
-//   16384 x 1027 bf16, branch                 41.6 us (a CTA takes rows of one shift of eight; element by element at the edges)
-//   700 x 1500 fp32                           12.1 us (floor 2.6; latency: parameters, rows, join over the cluster)
-//   131072 x 64 bf16                          17.5 us (floor 7.8: a row is a few lanes' work, its reductions and statistics stay)
+//   65536 x 1024 bf16, branch                 84.5 us (floor 81.9)                16384 x 1024 fp32, branch  47.4 us (floor 40.9)
+//   16384 x 1024 bf16, branch                 28.4 us (floor 20.5: two CTAs an SM start, and 296 CTAs' sums are added up)
+//   16384 x 1027 bf16, branch                 40.3 us (floor 20.5: 130 groups take 65 threads with two each, which are three warps, a third
+//                                             of whose lanes have nothing; rows of one shift of eight a CTA; elements at the edges)
+//   700 x 1500 fp32, branch                   11.2 us (floor 2.6; latency: parameters, four rows a CTA, 175 CTAs' partial sums, the second
+//                                             launch, which begins when the first has ended)
+//   131072 x 64 bf16                          17.1 us (floor 7.8: a row is a few lanes' work, its reductions and statistics stay)
+//   4096 x 16384 bf16                         206 us (floor 61.4), with a branch 325 (81.9); 2048 x 16384 fp32, branch 284 (81.9)
+//   16384 x 1024 bf16, branch, one matrix off the others' place in a granule   142 us (floor 20.5: element by element)
 // Two CTAs an SM: the sums of sixteen columns in fp32 pairs, the row and its groups take 128 registers, so that bytes in flight
-// have to come from the ring, not from warps.
+// have to come from the ring, not from warps.  The last two lines' instances have 32 columns a thread and 512 threads, for whose
+// state 128 registers are too few (300 to 800 bytes spilled).
 #include <cooperative_groups.h>
 
 #include "deft_norm_rows.cuh"

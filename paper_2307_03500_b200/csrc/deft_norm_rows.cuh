@@ -21,8 +21,9 @@ constexpr int kTeamMost = 512;
 constexpr int kTeamMostWarps = kTeamMost / 32;
 constexpr int kMostStages = 4;
 
-// How a thread gets its groups: through the ring, by 16-byte loads (where the ring finds no room), or element by element (rows that
-// no shift suits).
+// How a thread gets its groups: through the ring; by 16-byte loads, where the parameters leave the ring no room for a stage beside as many
+// CTAs as an SM holds (fp32 rows with a branch: of 4096 columns and some widths from 2500 on, and from 11800 on; gradients of the longest rows); or element by element (rows that
+// no shift suits: matrices on different places of a granule).  The last two have one shape, that of the longest rows.
 enum class Feed { kRing, kLoads, kElements };
 template <Feed kFeed> struct FeedTag { static constexpr Feed value = kFeed; };
 
