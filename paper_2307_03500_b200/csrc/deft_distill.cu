@@ -111,10 +111,9 @@ struct Sums {
 struct Brief {
     float rest_near, rest, entries_near, entries, q;
 };
-// What the gradient of a row is formed with: an element's is A 2^((z - all) c1) - B 2^((z - rest) c1), an entry's own
-// A 2^((z - all) c1) - q f.
+// What the gradient of a row is formed with: an element's is K 2^((z - rest) c1), an entry's own A 2^((z - all) c1) - q f.
 struct Factors {
-    float all, rest, A, B;
+    float all, rest, A, K;
 };
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -413,11 +412,16 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         }
         const float all = s.rest == 0.0f ? s.entries_near : (s.entries == 0.0f ? s.rest_near : fmaxf(s.rest_near, s.entries_near));
         if (g) {
-            const float total = (s.rest == 0.0f ? 0.0f : s.rest * exp2_fast((s.rest_near - all) * a.c1)) +
-                                (s.entries == 0.0f ? 0.0f : s.entries * exp2_fast((s.entries_near - all) * a.c1));
+            // (one of the two lies at `all`)
+            const float step = power_of(fminf(s.rest_near, s.entries_near) - all, a.c1);
+            const float rest = s.rest == 0.0f ? 0.0f : (s.rest_near == all ? s.rest : s.rest * step);
+            const float entries = s.entries == 0.0f ? 0.0f : (s.entries_near == all ? s.entries : s.entries * step), total = rest + entries;
             // the teacher's probability outside its entries; none where there is no other logit
             const float left = a.teacher_lse && !(s.rest == 0.0f) ? fmaxf(0.0f, 1.0f - s.q) : 0.0f, f = weight * a.grad_factor;
-            if (lane == 0) factors = Factors{all, s.rest_near, (s.q + left) / total * f, left > 0.0f ? left / s.rest * f : 0.0f};
+            // p (q + left) - left p / p0 of the rest, p0 = rest / total: with the common left rest taken out, as 1 - left / p0 would lose what
+            // lies between the two
+            const float p = left * entries, d = __fmaf_rn(s.q, rest, -p) - __fmaf_rn(left, entries, -p);
+            if (lane == 0) factors = Factors{all, s.rest_near, (s.q + left) / total * f, s.rest == 0.0f ? 0.0f : d / (total * s.rest) * f};
             bar_arrive<kFactors>(all_threads);
         }
         if (a.loss && rank == 0) {         // the loss, from all warps' sums: what remains of terms that nearly cancel, in 64 bits
@@ -625,7 +629,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
         bar_sync<kFactors>(all_threads);
         const Factors f = factors;
         // (nothing but -inf: the share is 0, and NaN where the whole row has no other)
-        const float k = rest == 0.0f ? 0.0f * f.A : (f.A * exp2_fast((s.rest_near - f.all) * a.c1) - f.B * exp2_fast((s.rest_near - f.rest) * a.c1)) * off;
+        const float k = rest == 0.0f ? 0.0f * f.A : f.K * exp2_fast((s.rest_near - f.rest) * a.c1) * off;
         if (careful) write_grad<T, true>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
         else write_grad<T, false>(cells, n, base, lo, hi, threads, a.vocab, g, from, a.c1, k);
         bar_row<kMost>(threads);
@@ -639,7 +643,7 @@ __global__ void __launch_bounds__(kMost + 32, kMost == 32 ? 16 : (kMost == 256 ?
                 for (int m = 0; m < a.top; ++m)
                     if (entry.col[m] == c || entry.col[m] == -3 - c) q += entry.prob[m];
             }
-            g[c] = from_f32<T>(exp2_fast((entry.own[j] - f.all) * a.c1) * f.A - q * (weight * a.grad_factor));
+            g[c] = from_f32<T>(power_of(entry.own[j] - f.all, a.c1) * f.A - q * (weight * a.grad_factor));
         }
     }
     if (ctas > 1) cluster_wait();

@@ -315,3 +315,22 @@ def test_loss_that_is_left_of_logarithms_that_cancel(gap, temperature):
     deft.deft_distill(z, ids, t, loss=loss, teacher_lse=lse, temperature=temperature)
     want = plain.distill(z, ids, t, lse, temperature=temperature)[0]
     assert (loss.double().cpu() - want).abs().max().item() <= 1e-8 * temperature ** 2
+
+
+@pytest.mark.parametrize("gap", [0.3, 0.7, 1.1, -0.9])
+def test_gradient_of_a_rest_that_nearly_agrees(gap):
+    """Teacher's probabilities twice the student's on eight of 2000 columns: the rest's factor 1 - q0 / p0 is some 0.004, of which a difference of
+    fp32 quotients would lose 1e-7 / 0.004.  Allowed, relative: in the numerator q p0 - q0 p_e, whose terms are at most 2 and 1 times
+    it, 3 and 2.5 times 2^-23 (a power each, sums, products), 1e-6; quotients, factors and the element's power (2^-22) 7e-7: 2e-6."""
+    z = torch.zeros((3, 2000), device="cuda")
+    z[:, 5:13] = gap
+    ids = torch.arange(5, 13, device="cuda").expand(3, 8).contiguous()
+    t = z[:, 5:13] + 4.0 * 0.6931472
+    lse = torch.logsumexp(z.double() / 4.0, 1).float()
+    grad = torch.empty_like(z)
+    deft.deft_distill(z, ids, t, grad=grad, teacher_lse=lse, temperature=4.0)
+    want = plain.distill(z, ids, t, lse, temperature=4.0)[1]
+    rest = torch.ones(2000, dtype=torch.bool)
+    rest[5:13] = False
+    err = (grad.double().cpu() - want)[:, rest] / want[:, rest]
+    assert err.abs().max().item() <= 2e-6
