@@ -9,19 +9,19 @@
 // it works out the loss.
 //
 // Of the loss, what an entry adds is held in two fp32 pieces, what joins them in 64 bits: relative errors of 1e-7 to 6e-7 where the rest is
-// a class (T up to 4; fp32 forms of the same terms have 2e-7 to 6e-4), 3e-8 to 6e-8 renormalised (a rounding to fp32 is up to 6e-8).
+// a class (T up to 4; fp32 forms of the same terms have 2e-7 to 6e-4), 2e-8 to 6e-8 renormalised (a rounding to fp32 is up to 6e-8).
 //
 // Bytes: the logits once, the gradient once.  Operations: two powers an element with a gradient (one of the sum, one of the
 // gradient: keeping the first would take the room of a second part), so 16 elements a cycle and SM of the special function unit, about
 // 0.7 of the copy's time in 16 bits; the rest are conversions and fp32 pairs.  Measured (device time; floor at the copy rate, 6561 GB/s):
-//   8192 x 50257 bf16, 64 entries, gradient           330 us (5.0 TB/s; floor 252)
-//   2048 x 30522 bf16, a quarter masked               49.0 us (floor 33.4)
-//   2048 x 50257 fp32                                 162 us (floor 126)
-//   700 x 33278 fp32, loss alone                      33.2 us (2.8 TB/s; floor 14.2: a part is parked and read again, though nothing is
+//   8192 x 50257 bf16, 64 entries, gradient           329 us (5.0 TB/s; floor 252)
+//   2048 x 30522 bf16, a quarter masked               49.2 us (floor 33.4)
+//   2048 x 50257 fp32                                 163 us (floor 126)
+//   700 x 33278 fp32, loss alone                      33.4 us (2.8 TB/s; floor 14.2: a part is parked and read again, though nothing is
 //                                                     written back, and 3.5 rounds of CTAs each copy, sum and join in turn)
-//   65536 x 1000 bf16                                 193 us (floor 41: some 1600 instructions a row that do not depend on its width)
-//   16384 x 4000 bf16                                 93 us (floor 40: likewise)
-// Special function unit 55 %, issue slots 55 %, waits at the row's barriers: a CTA copies, sums and writes in turn, and the four
+//   65536 x 1000 bf16                                 192 us (floor 41: some 1600 instructions a row that do not depend on its width)
+//   16384 x 4000 bf16                                 92 us (floor 40: likewise)
+// Special function unit 56 %, issue slots 55 %, waits at the row's barriers: a CTA copies, sums and writes in turn, and the four
 // of an SM overlap one another's phases.  What was tried against it and was slower: one CTA an SM with three parts in a ring and the powers
 // kept (550 to 750 us), a share of the powers by a polynomial (339 to 416).  Larger and smaller parts gave nothing.
 #include <cooperative_groups.h>

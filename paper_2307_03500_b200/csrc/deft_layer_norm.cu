@@ -7,16 +7,16 @@
 // Bound by memory: each matrix crosses once.  Measured (device time; floor: its bytes at the copy rate, 6561 GB/s):
 //   16384 x 1024 bf16, branch and sum        24.9 us (5.39 TB/s; floor 20.5)      8192 x 4096 bf16, branch   50 us (floor 40.9)
 //   16384 x  768 bf16                        12.5 us (floor 7.7)                  16384 x 1024 fp32          24.2 us (floor 20.5)
-//   65536 x 1024 bf16, branch and sum          96 us (floor 81.9)                 4096 x 8192 bf16, branch   47 us (floor 40.9)
+//   65536 x 1024 bf16, branch and sum          97 us (floor 81.9)                 4096 x 8192 bf16, branch   47 us (floor 40.9)
 //   5003 x 1027 fp32 -> bf16                 11.7 us (floor 4.7; groups shifted with the row, CTAs of one shift, a few rows a team)
 //   65536 x 1027 bf16                          71 us (floor 41)
 //   64 x 1024                                 3.7 us (latency: parameters, one row, one reduction)
 //   8192 x 4096 fp32, branch                  147 us (floor 82: parameters leave four CTAs an SM no room for a ring, so that rows come by loads)
 //   4096 x 16384 bf16, branch                 107 us (floor 82)                   2048 x 16384 fp32, branch 135 us (floor 82: by loads)
 //   16384 x 1024 bf16, branch, y one element off the others' place in a granule   82 us (floor 20.5: element by element)
-// Four CTAs of 256 threads an SM (64 registers) hide one another's reductions; issue slots 52 %.  What keeps it from the copy
+// Four CTAs of 256 threads an SM (64 registers) hide one another's reductions; issue slots 54 %.  What keeps it from the copy
 // rate is what a row waits for (the ring's reads, then the copies); the start and the end less so: 16384 rows, seven a team, take 1.22
-// times their floor, 65536 rows 1.17.
+// times their floor, 65536 rows 1.18.
 #include "deft_norm_rows.cuh"
 
 namespace deft {
